@@ -346,6 +346,132 @@ bacon_status bacon_window_scores_noalloc(int kv_heads, int q_heads, int head_dim
 /* Wait for the stream and report any error latched by a kernel. */
 bacon_status bacon_sync(bacon_ctx* ctx, bacon_stream stream);
 
+/* ------------------------------------------------------------------------
+ * Serving from the kept rows.  The paper ends at the compacted cache; these
+ * calls hold it, and the tokens generated after it, in pages of 8-bit values
+ * and attend to it.
+ *
+ * A unit is one (request, layer, kv-head); each has its own length, since
+ * adaptive head budgets keep another number of rows per head.  A page holds
+ * `page` tokens of one unit, with one fp32 scale for its K rows and one for
+ * its V rows; a value is code * scale.  Arrays of the caller:
+ *
+ *   k, v           [pages][page][d]              8-bit codes
+ *   k_scale,
+ *   v_scale        [pages]                       fp32
+ *   lengths        [requests][layers][Hkv]       int32 tokens of each unit
+ *   table          [requests][layers][Hkv][max_blocks]
+ *                                                int32 page of each block of
+ *                                                `page` tokens
+ *   ring, state    [pages], [2]                  int32 free pages:
+ *                  ring[(state[0] + i) mod pages], 0 <= i < state[1]
+ *   slots                                        int32 page * `page` + row of
+ *                                                a token, -1 for none
+ *
+ * A decoding program plans the new tokens of a step once (bacon_cache_plan),
+ * then per layer stores their K and V (bacon_cache_store) and attends
+ * (bacon_cache_attend).  The calls are asynchronous on `stream` like those
+ * above, allocate nothing and may be captured.  One cache must not be used
+ * from two threads or on two streams at once.  What is found wrong on the
+ * device is latched and returned by bacon_cache_sync. */
+typedef struct bacon_cache bacon_cache;
+
+typedef enum {
+    BACON_E4M3 = 0, /* scale: the least power of two with amax <= 448 scale  */
+    BACON_INT8 = 1  /* scale: amax / 127 rounded up to 8 significant bits    */
+} bacon_cache_format; /* either scale is at least 2^-60 */
+
+typedef enum { BACON_BF16 = 0, BACON_FP16 = 1 } bacon_dtype;
+
+typedef struct {
+    int layers, kv_heads, q_heads, head_dim; /* head_dim 64 or 128            */
+    int page;         /* tokens per page: 16, 32, 64 or 128                  */
+    int pages;        /* pages of the pool; pages * page < 2^31              */
+    int max_requests; /* largest request count of one call                   */
+    int max_blocks;   /* columns of a table                                  */
+    int format;       /* bacon_cache_format                                  */
+    int dtype;        /* bacon_dtype of rows, queries and outputs            */
+    void* k;          /* device arrays as above, kept by the caller for the  */
+    void* v;          /* life of the cache; k and v 16-byte aligned          */
+    float* k_scale;
+    float* v_scale;
+} bacon_cache_desc;
+
+/* Creates a cache over the caller's pools on the current device: holds the
+ * split attention's scratch and the error word. */
+bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc);
+void bacon_cache_destroy(bacon_cache* cache);
+
+/* Pages and slots for the tokens that the units are about to get.  Unit u
+ * (in order r, l, h) with n tokens and a new ones takes
+ * ceil((n + a) / page) - ceil(n / page) pages from the ring, the units one
+ * after the other; they are entered in its row of the table.  lengths_out
+ * receives n + a, state_out the ring's state afterwards; neither may overlap
+ * its input.  With per_unit != 0, `added` is [requests][layers][Hkv] and
+ * slots [rows] takes the units' tokens one after the other: the order of the
+ * rows of bacon_compress_adaptive.  With per_unit == 0, `added` is
+ * [requests], or NULL for one token each, and slots is [layers][rows][Hkv],
+ * the requests' tokens one after the other.  Entries beyond the last token
+ * are -1.  When the ring holds too few pages (BACON_ENOMEM), or a length is
+ * negative or exceeds max_blocks * page, or the tokens exceed `rows`
+ * (BACON_EINVAL, both at bacon_cache_sync), nothing is given: lengths_out
+ * and state_out repeat the input and every slot is -1. */
+bacon_status bacon_cache_plan(bacon_cache* cache, int requests, const int32_t* lengths,
+                              const int32_t* added, int per_unit, int32_t* table,
+                              const int32_t* ring, const int32_t* state, int rows,
+                              int32_t* slots, int32_t* lengths_out, int32_t* state_out,
+                              bacon_stream stream);
+
+/* Slots of the positions [first, first + count) of each unit (first NULL: 0),
+ * the units one after the other; -1 beyond.  Errors as bacon_cache_plan. */
+bacon_status bacon_cache_locate(bacon_cache* cache, int requests, const int32_t* first,
+                                const int32_t* count, const int32_t* table, int rows,
+                                int32_t* slots, bacon_stream stream);
+
+/* Returns the pages of every request with done[r] != 0 to the ring (units in
+ * order, blocks in order); their lengths become 0, their table rows -1.
+ * Nothing changes when an entry is no page or the ring would overflow
+ * (BACON_EINVAL at bacon_cache_sync). */
+bacon_status bacon_cache_release(bacon_cache* cache, int requests, const int32_t* done,
+                                 int32_t* lengths, int32_t* table, int32_t* ring,
+                                 int32_t* state, bacon_stream stream);
+
+/* Quantises rows into their slots.  Row (t, h) of k starts at element
+ * t * k_token_stride + h * k_head_stride, the same for v (strides multiples
+ * of 8 elements, rows 16-byte aligned); slots is [tokens][heads], so heads is
+ * Hkv for token-major rows of one layer and 1 for rows one after the other.
+ * The rows of one page must follow one another in tokens and positions.  A
+ * page that gets its first row has its scale from the new rows; one that is
+ * appended to keeps its scale if that holds them, and its older rows are
+ * quantised again with the larger scale if not.  Infinities saturate; NaN
+ * stays NaN in e4m3 and becomes 0 in int8; neither counts for the scale. */
+bacon_status bacon_cache_store(bacon_cache* cache, int tokens, int heads, const void* k,
+                               long long k_token_stride, long long k_head_stride, const void* v,
+                               long long v_token_stride, long long v_head_stride,
+                               const int32_t* slots, bacon_stream stream);
+
+/* The values of `rows` slots as [rows][d] each; zeros for -1. */
+bacon_status bacon_cache_load(bacon_cache* cache, int rows, const int32_t* slots, void* k_out,
+                              void* v_out, bacon_stream stream);
+
+/* Attention of `tokens` new queries of one layer over their units' tokens
+ * (lengths and table include the new ones): query head g of kv-head
+ * h = g / (Hq / Hkv).  q row (t, g) starts at element t * q_token_stride +
+ * g * q_head_stride (multiples of 8 elements).  Request r has the queries
+ * starts[r] .. starts[r + 1]; starts NULL: tokens / requests each.  With
+ * causal != 0, query j of a request with a sees the positions up to
+ * n - a + j, else all n.  scale multiplies the logits; 0 means 1/sqrt(d).
+ * out is [tokens][Hq][d], lse (may be NULL) fp32 [tokens][Hq] receives the
+ * natural log-sum-exp.  A query that sees nothing gets zeros and -inf. */
+bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int tokens,
+                                const void* q, long long q_token_stride, long long q_head_stride,
+                                const int32_t* starts, const int32_t* lengths,
+                                const int32_t* table, int causal, float scale, void* out,
+                                float* lse, bacon_stream stream);
+
+/* Wait for the stream and report any error latched by these kernels. */
+bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

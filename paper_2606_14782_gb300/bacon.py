@@ -30,10 +30,16 @@ EXPORTS = ("bacon_default_params", "bacon_init", "bacon_destroy", "bacon_last_er
            "bacon_profile_enable", "bacon_profile_read", "bacon_window_scores_noalloc",
            "bacon_compress_layer_budgets", "bacon_pyramid_budgets",
            "bacon_compress_adaptive", "bacon_compress_with_lse", "bacon_sweep",
-           "bacon_sync")
+           "bacon_sync", "bacon_cache_create", "bacon_cache_destroy", "bacon_cache_plan",
+           "bacon_cache_locate", "bacon_cache_release", "bacon_cache_store",
+           "bacon_cache_load", "bacon_cache_attend", "bacon_cache_sync")
 MAX_VARIANTS = 32
 PROFILE_STAGES = ("window_stats", "window_combine", "window_scores", "calibrate_select",
                   "gather")
+
+
+CACHE_FORMATS = {"e4m3": 0, "int8": 1}
+CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
 class BaconError(RuntimeError):
@@ -58,9 +64,18 @@ class Variant(ctypes.Structure):
                 ("use_T", ctypes.c_int)]
 
 
+class CacheDesc(ctypes.Structure):
+    """Mirror of ``bacon_cache_desc``."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("layers", "kv_heads", "q_heads", "head_dim", "page",
+                                             "pages", "max_requests", "max_blocks", "format",
+                                             "dtype")]
+                + [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")])
+
+
 _lib = None
 _vp = ctypes.c_void_p
 _int = ctypes.c_int
+_i64 = ctypes.c_longlong
 
 
 def load() -> ctypes.CDLL:
@@ -113,7 +128,22 @@ def load() -> ctypes.CDLL:
     lib.bacon_profile_enable.argtypes = [_vp, _int]
     lib.bacon_profile_read.argtypes = [_vp, ctypes.POINTER(ctypes.c_double),
                                        ctypes.POINTER(_int), _int]
-    for name in ("bacon_sweep", "bacon_compress_with_lse", "bacon_compress_adaptive",
+    lib.bacon_cache_create.argtypes = [ctypes.POINTER(_vp), ctypes.POINTER(CacheDesc)]
+    lib.bacon_cache_destroy.argtypes = [_vp]
+    lib.bacon_cache_destroy.restype = None
+    lib.bacon_cache_plan.argtypes = [_vp, _int, _vp, _vp, _int, _vp, _vp, _vp, _int, _vp, _vp,
+                                     _vp, _vp]
+    lib.bacon_cache_locate.argtypes = [_vp, _int, _vp, _vp, _vp, _int, _vp, _vp]
+    lib.bacon_cache_release.argtypes = [_vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.bacon_cache_store.argtypes = [_vp, _int, _int, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]
+    lib.bacon_cache_load.argtypes = [_vp, _int, _vp, _vp, _vp, _vp]
+    lib.bacon_cache_attend.argtypes = [_vp, _int, _int, _int, _vp, _i64, _i64, _vp, _vp, _vp,
+                                       _int, ctypes.c_float, _vp, _vp, _vp]
+    lib.bacon_cache_sync.argtypes = [_vp, _vp]
+    for name in ("bacon_cache_create", "bacon_cache_plan", "bacon_cache_locate",
+                 "bacon_cache_release", "bacon_cache_store", "bacon_cache_load",
+                 "bacon_cache_attend", "bacon_cache_sync",
+                 "bacon_sweep", "bacon_compress_with_lse", "bacon_compress_adaptive",
                  "bacon_compress_layer_budgets",
                  "bacon_window_scores_noalloc",
                  "bacon_profile_enable", "bacon_profile_read",
@@ -426,3 +456,193 @@ class State:
         _check(load().bacon_select(self.ctx.handle, self.handle, budget, idx_out.data_ptr(),
                                    _stream_ptr(stream)))
         return idx_out
+
+
+def _int32(t, shape, what):
+    """The address of a contiguous int32 tensor of this shape on the GPU."""
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 cuda tensor of shape {tuple(shape)}")
+    return t.data_ptr()
+
+
+class Cache:
+    """Kept rows and the tokens after them in pages of 8-bit values
+    (``bacon_cache``): block tables, storing, and attention over them.
+
+    A unit is one (request, layer, kv-head).  Per-unit arrays are int32 on the
+    GPU: lengths [R, layers, kv_heads], table [R, layers, kv_heads,
+    max_blocks]; ring [pages] and state [2] hold the free pages.  The pools
+    k, v [pages, page, head_dim] uint8 and their scales [pages] fp32 may be
+    given, else they are allocated here."""
+
+    def __init__(self, layers, kv_heads, q_heads, head_dim, pages, page=64, format="e4m3",
+                 dtype=torch.bfloat16, max_requests=4, max_blocks=None, k=None, v=None,
+                 k_scale=None, v_scale=None):
+        lib = load()
+        if format not in CACHE_FORMATS or dtype not in CACHE_DTYPES:
+            raise ValueError("format must be e4m3 or int8, dtype bfloat16 or float16")
+        self.layers, self.kv_heads, self.q_heads = layers, kv_heads, q_heads
+        self.head_dim, self.pages, self.page = head_dim, pages, page
+        self.format, self.dtype = format, dtype
+        self.max_requests = max_requests
+        self.max_blocks = pages if max_blocks is None else max_blocks
+        codes, scales = (pages, page, head_dim), (pages,)
+        self.k, self.v = (torch.empty(codes, dtype=torch.uint8, device="cuda") if t is None else t
+                          for t in (k, v))
+        self.k_scale, self.v_scale = (torch.empty(scales, device="cuda") if t is None else t
+                                      for t in (k_scale, v_scale))
+        for t, shape, kind in ((self.k, codes, torch.uint8), (self.v, codes, torch.uint8),
+                               (self.k_scale, scales, torch.float32),
+                               (self.v_scale, scales, torch.float32)):
+            if t.shape != shape or t.dtype is not kind or not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"a pool must be a contiguous {kind} cuda tensor of shape {shape}")
+        desc = CacheDesc(layers, kv_heads, q_heads, head_dim, page, pages, max_requests,
+                         self.max_blocks, CACHE_FORMATS[format], CACHE_DTYPES[dtype],
+                         self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                         self.v_scale.data_ptr())
+        h = _vp()
+        _check(lib.bacon_cache_create(ctypes.byref(h), ctypes.byref(desc)))
+        self.handle, self._lib = h, lib
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self._lib.bacon_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def sync(self, stream=None):
+        _check(self._lib.bacon_cache_sync(self.handle, _stream_ptr(stream)))
+
+    def tables(self, requests):
+        """(lengths, table, ring, state) of `requests` empty requests: every
+        page is free."""
+        shape = (requests, self.layers, self.kv_heads)
+        dev = self.k.device
+        return (torch.zeros(shape, dtype=torch.int32, device=dev),
+                torch.full(shape + (self.max_blocks,), -1, dtype=torch.int32, device=dev),
+                torch.arange(self.pages, dtype=torch.int32, device=dev),
+                torch.tensor([0, self.pages], dtype=torch.int32, device=dev))
+
+    def plan(self, lengths, added, table, ring, state, rows, slots=None, lengths_out=None,
+             state_out=None, stream=None):
+        """Pages and slots for the tokens the units are about to get.  added
+        [R, layers, kv_heads]: each unit its own number, slots [rows] in the
+        units' order (that of compress_adaptive's rows); added [R] or None
+        (one): tokens of a request, slots [layers, rows, kv_heads].  rows: the
+        tokens in all.  The table gets the new pages; returns (slots,
+        lengths_out, state_out)."""
+        R = lengths.shape[0]
+        units = (R, self.layers, self.kv_heads)
+        per_unit = added is not None and added.dim() == 3
+        if slots is None:
+            slots = torch.empty((rows,) if per_unit else (self.layers, rows, self.kv_heads),
+                                dtype=torch.int32, device=lengths.device)
+        if lengths_out is None:
+            lengths_out = torch.empty_like(lengths)
+        if state_out is None:
+            state_out = torch.empty_like(state)
+        p_slots = _int32(slots, (rows,) if per_unit else (self.layers, rows, self.kv_heads),
+                         "slots")
+        _check(self._lib.bacon_cache_plan(
+            self.handle, R, _int32(lengths, units, "lengths"),
+            None if added is None else _int32(added, units if per_unit else (R,), "added"),
+            int(per_unit), _int32(table, units + (self.max_blocks,), "table"),
+            _int32(ring, (self.pages,), "ring"), _int32(state, (2,), "state"), rows,
+            p_slots, _int32(lengths_out, units, "lengths_out"),
+            _int32(state_out, (2,), "state_out"), _stream_ptr(stream)))
+        return slots, lengths_out, state_out
+
+    def locate(self, count, table, rows, first=None, slots=None, stream=None):
+        """Slots [rows] of the positions [first, first + count) of each unit
+        (first None: 0), the units one after the other; -1 beyond them."""
+        R = count.shape[0]
+        units = (R, self.layers, self.kv_heads)
+        if slots is None:
+            slots = torch.empty((rows,), dtype=torch.int32, device=count.device)
+        _check(self._lib.bacon_cache_locate(
+            self.handle, R, None if first is None else _int32(first, units, "first"),
+            _int32(count, units, "count"), _int32(table, units + (self.max_blocks,), "table"),
+            rows, _int32(slots, (rows,), "slots"), _stream_ptr(stream)))
+        return slots
+
+    def release(self, done, lengths, table, ring, state, stream=None):
+        """Gives the pages of the requests with done [R] != 0 back, in place."""
+        R = lengths.shape[0]
+        units = (R, self.layers, self.kv_heads)
+        _check(self._lib.bacon_cache_release(
+            self.handle, R, _int32(done, (R,), "done"), _int32(lengths, units, "lengths"),
+            _int32(table, units + (self.max_blocks,), "table"),
+            _int32(ring, (self.pages,), "ring"), _int32(state, (2,), "state"),
+            _stream_ptr(stream)))
+
+    def _rows(self, t, what):
+        """(address, token stride, head stride) of rows [T, H, d] or [T, d]."""
+        if (t.dtype is not self.dtype or not t.is_cuda or t.shape[-1] != self.head_dim
+                or t.dim() not in (2, 3) or t.stride(-1) != 1):
+            raise ValueError(f"{what} must be {self.dtype} cuda rows of {self.head_dim} values, "
+                             "[tokens, heads, d] or [tokens, d], the last dimension contiguous")
+        return t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0
+
+    def store(self, k, v, slots, stream=None):
+        """Rows k, v [T, H, d] (slots [T, H]) or [T, d] (slots [T]) into their
+        slots; any strides with contiguous rows."""
+        if k.shape != v.shape:
+            raise ValueError("k and v must have the same shape")
+        kp, vp = self._rows(k, "k"), self._rows(v, "v")
+        _check(self._lib.bacon_cache_store(
+            self.handle, k.shape[0], k.shape[1] if k.dim() == 3 else 1, *kp, *vp,
+            _int32(slots, k.shape[:-1], "slots"), _stream_ptr(stream)))
+
+    def load(self, slots, k_out=None, v_out=None, stream=None):
+        """The values of the slots' rows, shape [*slots.shape, d] each."""
+        shape = slots.shape + (self.head_dim,)
+        if k_out is None:
+            k_out = torch.empty(shape, dtype=self.dtype, device=slots.device)
+        if v_out is None:
+            v_out = torch.empty(shape, dtype=self.dtype, device=slots.device)
+        for t in (k_out, v_out):
+            if t.shape != shape or t.dtype is not self.dtype or not t.is_contiguous():
+                raise ValueError(f"outputs must be contiguous {self.dtype} of shape {tuple(shape)}")
+        _check(self._lib.bacon_cache_load(self.handle, slots.numel(),
+                                          _int32(slots, slots.shape, "slots"), k_out.data_ptr(),
+                                          v_out.data_ptr(), _stream_ptr(stream)))
+        return k_out, v_out
+
+    def attend(self, layer, q, lengths, table, starts=None, causal=True, scale=None, out=None,
+               lse=None, stream=None):
+        """Attention of the queries q [T, q_heads, d] of one layer's new tokens
+        (already stored) over their units.  starts [R + 1] int32: where each
+        request's queries begin; None: T / R each.  Returns out [T, q_heads,
+        d], with lse=True (or a tensor) also the log-sum-exp [T, q_heads]."""
+        R, T = lengths.shape[0], q.shape[0]
+        units = (R, self.layers, self.kv_heads)
+        if q.dim() != 3 or q.shape[1] != self.q_heads:
+            raise ValueError(f"q must be [tokens, {self.q_heads}, {self.head_dim}]")
+        qp = self._rows(q, "q")
+        if out is None:
+            out = torch.empty((T, self.q_heads, self.head_dim), dtype=self.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype is not self.dtype or not out.is_contiguous():
+            raise ValueError("out must be contiguous and of q's shape and type")
+        if lse is True:
+            lse = torch.empty((T, self.q_heads), dtype=torch.float32, device=q.device)
+        elif lse is not None and (lse.shape != q.shape[:2] or lse.dtype is not torch.float32
+                                  or not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [tokens, q_heads]")
+        _check(self._lib.bacon_cache_attend(
+            self.handle, R, layer, T, *qp,
+            None if starts is None else _int32(starts, (R + 1,), "starts"),
+            _int32(lengths, units, "lengths"),
+            _int32(table, units + (self.max_blocks,), "table"), int(causal),
+            0.0 if scale is None else scale, out.data_ptr(), _ptr(lse), _stream_ptr(stream)))
+        return out if lse is None else (out, lse)

@@ -13,11 +13,12 @@
 
 #include "bacon.h"
 #include "common.cuh"
+#include "host.h"
 #include "window_tc.h"
 
 using namespace bacon;
 
-namespace {
+namespace bacon {
 
 thread_local std::string g_last_error;
 
@@ -37,33 +38,13 @@ bacon_status cuda_fail(cudaError_t e, const char* what)
     return fail(BACON_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 
-#define BACON_CUDA(call, what)                         \
-    do {                                               \
-        cudaError_t e_ = (call);                       \
-        if (e_ != cudaSuccess) return cuda_fail(e_, what); \
-    } while (0)
+}  // namespace bacon
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+namespace {
 
 constexpr int kChunkTokens = 1024;  // pass-1 token chunk (multiple of the 128-token tile)
 constexpr size_t kLastBytes = 24ull << 20;  // host path: keys of the last pipelined part, at most
 static_assert(kMaxVariants == BACON_MAX_VARIANTS, "variant table size");
-
-// Makes the context's device current for the duration of a call.
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) ok = cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
 
 template <typename T>
 cudaError_t dalloc(T** p, size_t count)

@@ -1,0 +1,68 @@
+// Kernel interfaces of the 8-bit paged cache.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace bacon {
+
+// Codes of the cache's error word (bacon_cache_sync names them).
+constexpr int kCacheBadIndex = 1;   // a slot, page, length or query range outside its array
+constexpr int kCacheNoPages = 2;    // the ring holds too few pages
+constexpr int kCacheTimeout = 3;    // a bounded pipeline wait ran out
+
+// Geometry and pools of a cache.
+struct CacheGeom {
+    int layers, hkv, hq, group, d;
+    int page, page_log2, pages, max_blocks;
+    int format, dtype;  // bacon_cache_format, bacon_dtype
+    uint8_t* k;
+    uint8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int* err;
+};
+
+struct PlanArgs {
+    int units, requests;
+    const int32_t* lengths;  // null: 0 (locate only)
+    const int32_t* added;    // null: 1 (per request only)
+    int per_unit;
+    int32_t* table;
+    const int32_t* ring;     // null: pages are there already (locate)
+    const int32_t* state;
+    int rows;
+    int32_t* slots;
+    int32_t* lengths_out;
+    int32_t* state_out;
+};
+cudaError_t launch_cache_plan(const CacheGeom& g, const PlanArgs& a, cudaStream_t st);
+cudaError_t launch_cache_release(const CacheGeom& g, int units, const int32_t* done,
+                                 int32_t* lengths, int32_t* table, int32_t* ring, int32_t* state,
+                                 cudaStream_t st);
+
+struct StoreArgs {
+    int tokens, heads;
+    const uint16_t* rows[2];      // K, V
+    long long token_stride[2];
+    long long head_stride[2];
+    const int32_t* slots;
+};
+cudaError_t launch_cache_store(const CacheGeom& g, const StoreArgs& a, cudaStream_t st);
+cudaError_t launch_cache_load(const CacheGeom& g, int rows, const int32_t* slots, void* k_out,
+                              void* v_out, cudaStream_t st);
+
+struct AttendArgs {
+    int requests, layer, tokens, causal;
+    const uint16_t* q;
+    long long q_token_stride, q_head_stride;
+    const int32_t* starts;
+    const int32_t* lengths;
+    const int32_t* table;
+    float scale;
+    uint16_t* out;
+    float* lse;
+};
+cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, cudaStream_t st);
+
+}  // namespace bacon

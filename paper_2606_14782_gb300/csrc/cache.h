@@ -1,6 +1,7 @@
 // Kernel interfaces of the 8-bit paged cache.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -63,6 +64,20 @@ struct AttendArgs {
     uint16_t* out;
     float* lse;
 };
-cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, cudaStream_t st);
+// What a cache keeps for its attention calls: descriptors of the pools (rows
+// of d bytes) and room for the partial sums of items that lie in several
+// blocks, two a block.
+constexpr int kBlocksPerSm = 3;
+struct SplitScratch {
+    CUtensorMap kmap, vmap;
+    int sms;
+    float* out;    // [2 sms kBlocksPerSm][32 columns][128]
+    float* sums;   // [2 sms kBlocksPerSm][32 columns][maximum, sum]
+    int* arrived;  // [sms kBlocksPerSm] parts that are there, 0 between calls
+};
+cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                                cudaStream_t st);
+// One descriptor over a pool of `rows` rows of d bytes, 16 of them a load.
+bool encode_pool_map(CUtensorMap* out, const void* base, int d, long long rows);
 
 }  // namespace bacon

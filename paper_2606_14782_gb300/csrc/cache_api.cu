@@ -13,6 +13,7 @@ struct bacon_cache {
     int device = 0;
     int max_requests = 0;
     CacheGeom g{};
+    SplitScratch sc{};
 };
 
 namespace {
@@ -85,12 +86,31 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
     g.k_scale = d.k_scale;
     g.v_scale = d.v_scale;
     cudaError_t e = cudaGetDevice(&c->device);
-    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&g.err), sizeof(int));
-    if (e == cudaSuccess) e = cudaMemset(g.err, 0, sizeof(int));
+    SplitScratch& sc = c->sc;
+    if (e == cudaSuccess)
+        e = cudaDeviceGetAttribute(&sc.sms, cudaDevAttrMultiProcessorCount, c->device);
+    // one allocation: partial outputs, their sums, arrival counts, error word
+    const size_t blocks = (size_t)sc.sms * kBlocksPerSm;
+    const size_t out_bytes = 2 * blocks * 32 * 128 * sizeof(float);
+    const size_t sum_bytes = 2 * blocks * 32 * 2 * sizeof(float);
+    const size_t word_bytes = (blocks + 1) * sizeof(int);
+    if (e == cudaSuccess)
+        e = cudaMalloc(reinterpret_cast<void**>(&sc.out), out_bytes + sum_bytes + word_bytes);
+    if (e == cudaSuccess) {
+        sc.sums = sc.out + out_bytes / sizeof(float);
+        sc.arrived = reinterpret_cast<int*>(sc.sums + sum_bytes / sizeof(float));
+        g.err = sc.arrived + blocks;
+        e = cudaMemset(sc.arrived, 0, word_bytes);
+    }
     if (e != cudaSuccess) {
         bacon_cache_destroy(c);
         return e == cudaErrorMemoryAllocation ? fail(BACON_ENOMEM, "device allocation failed")
                                               : cuda_fail(e, "cache creation");
+    }
+    const long long rows = (long long)g.pages * g.page;
+    if (!encode_pool_map(&sc.kmap, g.k, g.d, rows) || !encode_pool_map(&sc.vmap, g.v, g.d, rows)) {
+        bacon_cache_destroy(c);
+        return fail(BACON_ECUDA, "cuTensorMapEncodeTiled failed");
     }
     *out = c;
     return BACON_OK;
@@ -100,7 +120,7 @@ void bacon_cache_destroy(bacon_cache* cache)
 {
     if (!cache) return;
     DeviceGuard dg(cache->device);
-    if (cache->g.err) cudaFree(cache->g.err);
+    if (cache->sc.out) cudaFree(cache->sc.out);
     delete cache;
 }
 
@@ -220,7 +240,7 @@ bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int
                  q_token_stride, q_head_stride, starts, lengths, table, scale,
                  static_cast<uint16_t*>(out), lse};
     DeviceGuard dg(cache->device);
-    BACON_CUDA(launch_cache_attend(g, a, static_cast<cudaStream_t>(stream)), "attend launch");
+    BACON_CUDA(launch_cache_attend(g, a, cache->sc, static_cast<cudaStream_t>(stream)), "attend launch");
     return BACON_OK;
 }
 

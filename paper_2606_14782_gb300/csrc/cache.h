@@ -63,6 +63,8 @@ struct AttendArgs {
     float scale;
     uint16_t* out;
     float* lse;
+    long long above, upto;  // requests with more than `above` and at most `upto` rows
+                            // (queries x heads of a kv-head) are the kernel's
 };
 // What a cache keeps for its attention calls: descriptors of the pools (rows
 // of d bytes) and room for the partial sums of items that lie in several
@@ -74,9 +76,16 @@ struct SplitScratch {
     float* out;    // [2 sms kBlocksPerSm][32 columns][128]
     float* sums;   // [2 sms kBlocksPerSm][32 columns][maximum, sum]
     int* arrived;  // [sms kBlocksPerSm] parts that are there, 0 between calls
+    float* many_out;    // [2 sms][2 row tiles][128 dims][128 rows]
+    float2* many_sums;  // [2 sms][2][128] maximum, sum
+    int* many_arrived;  // [sms][2]
 };
-cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
-                                cudaStream_t st);
+// Requests of up to kFewRows rows (queries x heads of a kv-head), and of more.
+constexpr int kFewRows = 32;
+cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                             cudaStream_t st);
+cudaError_t launch_cache_many(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                              cudaStream_t st);
 // One descriptor over a pool of `rows` rows of d bytes, 16 of them a load.
 bool encode_pool_map(CUtensorMap* out, const void* base, int d, long long rows);
 

@@ -93,13 +93,19 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
     const size_t blocks = (size_t)sc.sms * kBlocksPerSm;
     const size_t out_bytes = 2 * blocks * 32 * 128 * sizeof(float);
     const size_t sum_bytes = 2 * blocks * 32 * 2 * sizeof(float);
-    const size_t word_bytes = (blocks + 1) * sizeof(int);
+    const size_t many_out_bytes = (size_t)sc.sms * 4 * 128 * 128 * sizeof(float);
+    const size_t many_sum_bytes = (size_t)sc.sms * 4 * 128 * sizeof(float2);
+    const size_t word_bytes = (blocks + 2 * (size_t)sc.sms + 1) * sizeof(int);
     if (e == cudaSuccess)
-        e = cudaMalloc(reinterpret_cast<void**>(&sc.out), out_bytes + sum_bytes + word_bytes);
+        e = cudaMalloc(reinterpret_cast<void**>(&sc.out),
+                       out_bytes + sum_bytes + many_out_bytes + many_sum_bytes + word_bytes);
     if (e == cudaSuccess) {
         sc.sums = sc.out + out_bytes / sizeof(float);
-        sc.arrived = reinterpret_cast<int*>(sc.sums + sum_bytes / sizeof(float));
-        g.err = sc.arrived + blocks;
+        sc.many_out = sc.sums + sum_bytes / sizeof(float);
+        sc.many_sums = reinterpret_cast<float2*>(sc.many_out + many_out_bytes / sizeof(float));
+        sc.arrived = reinterpret_cast<int*>(sc.many_sums + many_sum_bytes / sizeof(float2));
+        sc.many_arrived = sc.arrived + blocks;
+        g.err = sc.many_arrived + 2 * (size_t)sc.sms;
         e = cudaMemset(sc.arrived, 0, word_bytes);
     }
     if (e != cudaSuccess) {
@@ -238,9 +244,25 @@ bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int
     if (scale == 0.0f) scale = 1.0f / std::sqrt((float)g.d);
     AttendArgs a{requests, layer, tokens, causal != 0, static_cast<const uint16_t*>(q),
                  q_token_stride, q_head_stride, starts, lengths, table, scale,
-                 static_cast<uint16_t*>(out), lse};
+                 static_cast<uint16_t*>(out), lse, 0, 0};
     DeviceGuard dg(cache->device);
-    BACON_CUDA(launch_cache_attend(g, a, cache->sc, static_cast<cudaStream_t>(stream)), "attend launch");
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // each request goes by its own number of rows; with the same for all, or
+    // too few in the call for any to have many, one kernel has them all
+    const long long rows = (long long)tokens * g.group;
+    const bool same = starts == nullptr;
+    if (same ? rows / requests <= kFewRows : rows <= kFewRows) {
+        a.upto = kFewRows;
+        BACON_CUDA(launch_cache_few(g, a, cache->sc, st), "attend launch");
+        return BACON_OK;
+    }
+    if (!same) {
+        a.upto = kFewRows;
+        BACON_CUDA(launch_cache_few(g, a, cache->sc, st), "attend launch");
+    }
+    a.above = kFewRows;
+    a.upto = 1ll << 62;
+    BACON_CUDA(launch_cache_many(g, a, cache->sc, st), "attend launch");
     return BACON_OK;
 }
 

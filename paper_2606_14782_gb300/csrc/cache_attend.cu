@@ -55,26 +55,13 @@ struct Shared {
     float top[kWarps][32], sum[kWarps][32];
     uint64_t full[kStages], empty[kStages];
     long long scan[kWarps + 1];
-    long long total, at;    // tiles of the call; the tile where `unit`, `block`'s item starts
-    int unit, block;
-    int abort, last;
+    Found found;
+    int abort;
     int nan_at[128];        // per dim: first position of a NaN of V that not every column sees
     int nan_any;
 };
 static_assert(sizeof(Shared) <= 2048, "shared record");
 
-__device__ __forceinline__ void ldmatrix4(uint32_t* r, uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                 : "r"(addr));
-}
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
     uint32_t y;
@@ -90,87 +77,6 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A word of a transposed V load: token 2t's codes of dims 2g and 2g + 1, then
-// token 2t + 1's.  lo: both tokens of dim 2g, hi: of dim 2g + 1.
-template <int FORMAT>
-__device__ __forceinline__ void pairs_half(uint32_t w, uint32_t& lo, uint32_t& hi)
-{
-    if (FORMAT == BACON_E4M3) {
-        codes_half<FORMAT>(__byte_perm(w, 0, 0x3120), lo, hi);
-    } else {
-        const uint32_t u = w ^ 0x80808080u;
-        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4240);
-        const uint32_t b = __byte_perm(u, 0x64646464u, 0x4341);
-        const uint32_t off = 0x64806480u;
-        asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(lo) : "r"(a), "r"(off));
-        asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(hi) : "r"(b), "r"(off));
-    }
-}
-
-// 8 NT columns of a unit; column c is query c / group, head c % group.
-struct Item {
-    int r, h, block;
-    int n, start, asked;
-    int seen;   // positions that some column sees
-    int tiles;  // at least one, so that an item of no token writes its outputs
-};
-
-template <int NT>
-__device__ __forceinline__ int blocks_of(const CacheGeom& g, int asked)
-{
-    return (int)(((long long)asked * g.group + 8 * NT - 1) / (8 * NT));
-}
-
-template <int NT>
-__device__ __forceinline__ void set_block(const CacheGeom& g, const AttendArgs& a, Item& it, int block)
-{
-    it.block = block;
-    const int last = min(it.asked - 1, (block * 8 * NT + 8 * NT - 1) / g.group);
-    it.seen = seen_by(a, it.n, it.asked, last);
-    it.tiles = max(1, (it.seen + kTile - 1) / kTile);
-}
-
-template <int NT>
-__device__ __forceinline__ Item item_of(const CacheGeom& g, const AttendArgs& a, int unit, int block,
-                                        bool& bad)
-{
-    Item it;
-    it.r = unit / g.hkv;
-    it.h = unit - it.r * g.hkv;
-    const Asked q = asked_of(a, it.r);
-    it.start = q.start;
-    it.asked = q.asked;
-    it.n = length_of(g, a, it.r, it.h, bad);
-    set_block<NT>(g, a, it, block);
-    return it;
-}
-
-// The item after `it` that has columns; false at the end of the call's.
-template <int NT>
-__device__ __forceinline__ bool next_item(const CacheGeom& g, const AttendArgs& a, int& unit, Item& it)
-{
-    if (it.block + 1 < blocks_of<NT>(g, it.asked)) {
-        set_block<NT>(g, a, it, it.block + 1);
-        return true;
-    }
-    bool bad = false;
-    while (++unit < a.requests * g.hkv) {
-        it = item_of<NT>(g, a, unit, 0, bad);
-        if (it.asked > 0) return true;
-    }
-    return false;
-}
-
-// First tile of block b of E, and the block that has tile t.
-__device__ __forceinline__ long long first_tile(long long total, int b, int blocks)
-{
-    return total * b / blocks;
-}
-__device__ __forceinline__ int owner_of(long long total, long long t, int blocks)
-{
-    return (int)(((t + 1) * blocks - 1) / total);
-}
-
 template <int FORMAT, int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1)
 few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
@@ -182,7 +88,6 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     Shared& sh = *reinterpret_cast<Shared*>(smem + S::kMeta);
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int units = a.requests * g.hkv;
 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
@@ -194,57 +99,15 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     }
     for (int i = tid; i < 128; i += kThreads) sh.nan_at[i] = 0x7FFFFFFF;
 
-    // this block's tiles
-    const int per = (units + kThreads - 1) / kThreads, u0 = tid * per;
-    long long mine = 0;
-    bool bad = blockIdx.x == 0 && starts_are_bad(a, tid, kThreads);
-    for (int u = u0; u < min(units, u0 + per); ++u) {
-        Item it = item_of<NT>(g, a, u, 0, bad);
-        const int blocks = blocks_of<NT>(g, it.asked);
-        for (int c = 0; c < blocks; ++c) {
-            set_block<NT>(g, a, it, c);
-            mine += it.tiles;
-        }
-    }
-    if (bad) atomicCAS(g.err, 0, kCacheBadIndex);
-    long long x = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 31) sh.scan[warp] = x;
-    __syncthreads();
-    long long total = 0;
-    for (int w = 0; w <= kWarps; ++w) {
-        if (w == warp) x += total;
-        total += sh.scan[w];
-    }
-    const int blocks = total < (long long)gridDim.x ? (int)total : (int)gridDim.x;
-    const int b = blockIdx.x;
-    if (b >= blocks) return;
-    const long long lo = first_tile(total, b, blocks), hi = first_tile(total, b + 1, blocks);
-    if (lo >= x - mine && lo < x) {
-        long long at = x - mine;
-        for (int u = u0; u < min(units, u0 + per); ++u) {
-            Item it = item_of<NT>(g, a, u, 0, bad);
-            const int n = blocks_of<NT>(g, it.asked);
-            for (int c = 0; c < n; ++c) {
-                set_block<NT>(g, a, it, c);
-                if (at <= lo && lo < at + it.tiles) {
-                    sh.unit = u;
-                    sh.block = c;
-                    sh.at = at;
-                }
-                at += it.tiles;
-            }
-        }
-    }
-    __syncthreads();
+    Place place;
+    if (!find_place<8 * NT, kTile, kThreads>(g, a, sh.scan, sh.found, place)) return;
+    const int b = blockIdx.x, blocks = place.blocks;
+    const long long total = place.total, lo = place.lo, hi = place.hi;
+    bool bad = false;
 
-    int unit = sh.unit;
-    Item it = item_of<NT>(g, a, unit, sh.block, bad);
-    long long at = sh.at;  // the item's first tile
+    int unit = place.unit;
+    Item it = item_of<8 * NT, kTile>(g, a, unit, place.block, bad);
+    long long at = place.at;  // the item's first tile
     const uint32_t abort_flag = smem_u32(&sh.abort);
 
     if (warp == kWarps) {
@@ -301,7 +164,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 }
             }
             at += it.tiles;
-            if (t < hi && !stop && !next_item<NT>(g, a, unit, it)) break;
+            if (t < hi && !stop && !next_item<8 * NT, kTile>(g, a, unit, it)) break;
         }
         if (stop) {
             // the block's copies end before it does
@@ -701,7 +564,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
         }
         t = at + end;
         at += it.tiles;
-        if (t < hi && !next_item<NT>(g, a, unit, it)) break;
+        if (t < hi && !next_item<8 * NT, kTile>(g, a, unit, it)) break;
     }
 }
 
@@ -728,8 +591,8 @@ cudaError_t by_columns(const CacheGeom& g, const AttendArgs& a, const SplitScrat
 
 }  // namespace
 
-cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
-                                cudaStream_t st)
+cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                             cudaStream_t st)
 {
     if (g.format == BACON_E4M3)
         return g.d == 128 ? by_columns<BACON_E4M3, 128>(g, a, sc, st) : by_columns<BACON_E4M3, 64>(g, a, sc, st);

@@ -26,20 +26,25 @@ constexpr float kWeightTop = 14.0f;
 constexpr int kQueryTop = 14;
 constexpr int kBoxRows = 16;  // rows of one TMA load: the least page
 
-// The queries of one request: [start, start + asked) of the call's tokens.
+// The queries of one request: [start, start + asked) of the call's tokens; none
+// when they are the other kernel's.
 struct Asked {
     int start, asked;
 };
 
-__device__ __forceinline__ Asked asked_of(const AttendArgs& a, int r)
+__device__ __forceinline__ Asked asked_of(const CacheGeom& g, const AttendArgs& a, int r)
 {
+    Asked q;
     if (!a.starts) {
-        const int each = a.tokens / a.requests;
-        return Asked{r * each, each};
+        q.asked = a.tokens / a.requests;
+        q.start = r * q.asked;
+    } else {
+        const int s = a.starts[r], e = a.starts[r + 1];
+        if (s < 0 || e < s || e > a.tokens) return Asked{0, 0};
+        q = Asked{s, e - s};
     }
-    const int s = a.starts[r], e = a.starts[r + 1];
-    if (s < 0 || e < s || e > a.tokens) return Asked{0, 0};
-    return Asked{s, e - s};
+    const long long rows = (long long)q.asked * g.group;
+    return rows > a.above && rows <= a.upto ? q : Asked{0, 0};
 }
 
 // Whether the queries' ranges are what they have to be.
@@ -111,6 +116,167 @@ __device__ __forceinline__ float2 unpack16(int dtype, uint32_t w)
 __device__ __forceinline__ uint32_t pack16(int dtype, float x, float y)
 {
     return dtype == BACON_BF16 ? pack16<BACON_BF16>(x, y) : pack16<BACON_FP16>(x, y);
+}
+
+__device__ __forceinline__ void ldmatrix4(uint32_t* r, uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t* r, uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr));
+}
+// A word of a transposed V load: token 2t's codes of dims 2g and 2g + 1, then
+// token 2t + 1's.  lo: both tokens of dim 2g, hi: of dim 2g + 1.
+template <int FORMAT>
+__device__ __forceinline__ void pairs_half(uint32_t w, uint32_t& lo, uint32_t& hi)
+{
+    if (FORMAT == BACON_E4M3) {
+        codes_half<FORMAT>(__byte_perm(w, 0, 0x3120), lo, hi);
+    } else {
+        const uint32_t u = w ^ 0x80808080u;
+        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4240);
+        const uint32_t b = __byte_perm(u, 0x64646464u, 0x4341);
+        const uint32_t off = 0x64806480u;
+        asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(lo) : "r"(a), "r"(off));
+        asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(hi) : "r"(b), "r"(off));
+    }
+}
+
+// ROWS rows (columns, where the tokens are the rows) of a unit's queries: row c
+// is query c / group, head c % group.
+struct Item {
+    int r, h, block;
+    int n, start, asked;
+    int seen;   // positions that some row sees
+    int tiles;  // at least one, so that an item of no token writes its outputs
+};
+
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const CacheGeom& g, int asked)
+{
+    return (int)(((long long)asked * g.group + ROWS - 1) / ROWS);
+}
+
+template <int ROWS, int TILE>
+__device__ __forceinline__ void set_block(const CacheGeom& g, const AttendArgs& a, Item& it, int block)
+{
+    it.block = block;
+    const int last = min(it.asked - 1, (block * ROWS + ROWS - 1) / g.group);
+    it.seen = seen_by(a, it.n, it.asked, last);
+    it.tiles = max(1, (int)(((long long)it.seen + TILE - 1) / TILE));
+}
+
+template <int ROWS, int TILE>
+__device__ __forceinline__ Item item_of(const CacheGeom& g, const AttendArgs& a, int unit, int block,
+                                        bool& bad)
+{
+    Item it;
+    it.r = unit / g.hkv;
+    it.h = unit - it.r * g.hkv;
+    const Asked q = asked_of(g, a, it.r);
+    it.start = q.start;
+    it.asked = q.asked;
+    it.n = length_of(g, a, it.r, it.h, bad);
+    set_block<ROWS, TILE>(g, a, it, block);
+    return it;
+}
+
+// The item after `it` that has rows; false at the end of the call's.
+template <int ROWS, int TILE>
+__device__ __forceinline__ bool next_item(const CacheGeom& g, const AttendArgs& a, int& unit, Item& it)
+{
+    if (it.block + 1 < blocks_of<ROWS>(g, it.asked)) {
+        set_block<ROWS, TILE>(g, a, it, it.block + 1);
+        return true;
+    }
+    bool bad = false;
+    while (++unit < a.requests * g.hkv) {
+        it = item_of<ROWS, TILE>(g, a, unit, 0, bad);
+        if (it.asked > 0) return true;
+    }
+    return false;
+}
+
+// First tile of block b of `blocks`, and the block that has tile t.
+__device__ __forceinline__ long long first_tile(long long total, int b, int blocks)
+{
+    return total * b / blocks;
+}
+__device__ __forceinline__ int owner_of(long long total, long long t, int blocks)
+{
+    return (int)(((t + 1) * blocks - 1) / total);
+}
+
+// Tiles [lo, hi) of the call's `total`, all items' one after the other, are
+// this block's, one of `blocks`; the first of them is in item (unit, block),
+// whose first tile is `at`.
+struct Place {
+    long long total, lo, hi, at;
+    int blocks, unit, block;
+};
+struct Found {
+    long long at;
+    int unit, block;
+};
+
+// Scan of the units' tiles by the whole block; false when it has none.
+template <int ROWS, int TILE, int THREADS>
+__device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs& a, long long* scan,
+                                           Found& found, Place& p)
+{
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int units = a.requests * g.hkv;
+    const int per = (units + THREADS - 1) / THREADS, u0 = tid * per, u1 = min(units, u0 + per);
+    long long mine = 0;
+    bool bad = blockIdx.x == 0 && starts_are_bad(a, tid, THREADS);
+    for (int u = u0; u < u1; ++u) {
+        Item it = item_of<ROWS, TILE>(g, a, u, 0, bad);
+        const int blocks = blocks_of<ROWS>(g, it.asked);
+        for (int c = 0; c < blocks; ++c) {
+            set_block<ROWS, TILE>(g, a, it, c);
+            mine += it.tiles;
+        }
+    }
+    if (bad) atomicCAS(g.err, 0, kCacheBadIndex);
+    long long x = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 31) scan[warp] = x;
+    __syncthreads();
+    p.total = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w == warp) x += p.total;
+        p.total += scan[w];
+    }
+    p.blocks = p.total < (long long)gridDim.x ? (int)p.total : (int)gridDim.x;
+    if ((int)blockIdx.x >= p.blocks) return false;
+    p.lo = first_tile(p.total, blockIdx.x, p.blocks);
+    p.hi = first_tile(p.total, blockIdx.x + 1, p.blocks);
+    if (p.lo >= x - mine && p.lo < x) {
+        long long at = x - mine;
+        for (int u = u0; u < u1; ++u) {
+            Item it = item_of<ROWS, TILE>(g, a, u, 0, bad);
+            const int blocks = blocks_of<ROWS>(g, it.asked);
+            for (int c = 0; c < blocks; ++c) {
+                set_block<ROWS, TILE>(g, a, it, c);
+                if (at <= p.lo && p.lo < at + it.tiles) found = Found{at, u, c};
+                at += it.tiles;
+            }
+        }
+    }
+    __syncthreads();
+    p.at = found.at;
+    p.unit = found.unit;
+    p.block = found.block;
+    return true;
 }
 
 }  // namespace bacon

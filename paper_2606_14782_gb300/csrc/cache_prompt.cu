@@ -1,0 +1,710 @@
+// Attention of many queries per unit over the 8-bit pages: a follow-up turn,
+// or a prompt over a cache.
+//
+// Bound by the tensor cores: 4 d flops for every query head and token it sees.
+// An item is 256 rows (query x head of the kv-head) of a unit, two 128-row
+// tiles of S = Q K^T and O = P V on tcgen05 (fp16 in, fp32 in tensor memory),
+// against tiles of 128 tokens.  Codes cannot be operands beside 16-bit
+// queries, so four warps turn each page tile into fp16 once for all 256 rows:
+// K as it lies, V transposed to [dim][token] by 8x8 matrix loads and stores.
+// Two row tiles are what makes that pay: 1024 cycles of products a row tile
+// and token tile against some 900 issue slots of softmax and conversion for
+// one row tile, 1400 in 2048 for two.
+//
+// Roles: warps 0-3 and 4-7 take a row tile each, a thread a row: it reads its
+// logits from tensor memory, forms the weights w (cache_attend.cuh) and writes
+// them over the logits as the second product's operand; warps 8-11 convert;
+// one thread issues products, in the order P0 V, Q0 K', P1 V, Q1 K' (K' the
+// next tile), so that one row tile's softmax runs beside the other's products;
+// one warp loads.  A row's reference M follows its maximum when that has grown
+// by more than a factor of two; only then O is scaled, in tensor memory, which
+// is idle for this row tile while its softmax runs.
+//
+// Tiles are dealt out and cut items joined as in cache_attend.cu.
+#include <cmath>
+
+#include "cache_attend.cuh"
+
+namespace bacon {
+namespace {
+
+using namespace tc;
+
+constexpr int kRows = 256;   // of an item
+constexpr int kHalf = 128;   // rows of a row tile
+constexpr int kTile = 128;   // tokens
+constexpr int kGroups = kTile / 16;
+constexpr int kConvert = 8, kIssue = 12;  // first warps of the roles; the loads are last
+constexpr int kThreads = 14 * 32;
+
+template <int D>
+struct Smem {
+    static constexpr int kPanel = 128 * 128;         // 64 fp16 columns of 128 rows
+    static constexpr int kQHalf = kHalf * D * 2;
+    static constexpr int kKeys = 2 * kQHalf;         // two tiles of K in fp16
+    static constexpr int kKeysTile = kTile * D * 2;
+    static constexpr int kValues = kKeys + 2 * kKeysTile;  // two of V, [dim][token]
+    static constexpr int kValuesTile = D * kTile * 2;
+    static constexpr int kRawK = kValues + 2 * kValuesTile;
+    static constexpr int kRawV = kRawK + kTile * D;
+    static constexpr int kShared = kRawV + kTile * D;
+    static constexpr int kBytes = kShared + 3072;
+};
+
+template <int D>
+struct Shared {
+    float k_scale[4][kGroups], v_log2[4][kGroups], v_inv[4][kGroups];
+    uint64_t rawk_full, rawk_empty, rawv_full, rawv_empty;
+    uint64_t key_full[2], key_empty[2], value_full[2], value_empty[2];
+    uint64_t s_full[2], p_full[2], o_full[2], q_full[2];
+    uint64_t meta_full[4], item_done[4], drain;
+    long long scan[kThreads / 32];
+    Found found;
+    uint32_t tmem;
+    int abort, last[2];
+    int nan_any[4];
+    int nan_at[4][D];  // of an item, per dim: first position of a NaN of V that not every row sees
+};
+static_assert(sizeof(Shared<128>) <= 3072, "shared record");
+
+__device__ __forceinline__ uint32_t bar(uint64_t& b) { return smem_u32(&b); }
+
+// 8x8 matrices of 16-bit elements to shared memory, a row address a lane.
+__device__ __forceinline__ void stmatrix4(uint32_t addr, const uint32_t* r)
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1,%2,%3,%4};\n" ::"r"(addr),
+                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+                 : "memory");
+}
+
+__host__ __device__ constexpr uint32_t idesc_f16(int M, int N)
+{
+    return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// D[tmem] (+)= A[tmem] * B[smem]^T
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi,
+                                        uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n .reg .pred p;\n .reg .b64 db;\n setp.ne.b32 p, %5, 0;\n mov.b64 db, {%2, %3};\n"
+        " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(d),
+        "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+template <int D>
+__device__ __forceinline__ void give_up(Shared<D>& sh, int* err)
+{
+    st_shared_volatile(smem_u32(&sh.abort), 1);
+    atomicCAS(err, 0, kCacheTimeout);
+}
+
+// Bounded wait of a role's thread: one that runs out raises the abort flag, at
+// which every other wait ends at once and the roles run through to their ends.
+template <int D>
+__device__ __forceinline__ bool wait(Shared<D>& sh, uint32_t b, uint32_t parity, int* err)
+{
+    if (mbar_wait(b, parity, smem_u32(&sh.abort))) return true;
+    give_up(sh, err);
+    return false;
+}
+
+// ------------------------------------------------------------------ loads
+
+template <int D>
+__device__ __forceinline__ void load(const CUtensorMap* kmap, const CUtensorMap* vmap,
+                                     const CacheGeom& g, const AttendArgs& a, const Place& p,
+                                     Shared<D>& sh, uint32_t base)
+{
+    using S = Smem<D>;
+    const int lane = threadIdx.x & 31, group = lane & 7;
+    const bool of_v = lane >= 8;
+    int unit = p.unit, k = 0;
+    bool bad = false, ok = true;
+    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    long long at = p.at, t = p.lo;
+    uint32_t seq = 0;
+    while (t < p.hi && ok) {
+        if (k >= 4) ok = wait(sh, bar(sh.item_done[k & 3]), (k >> 2 & 1) ^ 1, g.err);
+        for (int i = lane; i < D; i += 32) sh.nan_at[k & 3][i] = 0x7FFFFFFF;
+        if (lane == 0) sh.nan_any[k & 3] = 0;
+        const int32_t* const table =
+            a.table + (((size_t)it.r * g.layers + a.layer) * g.hkv + it.h) * g.max_blocks;
+        const int end = (int)min((long long)it.tiles, p.hi - at);
+        for (int i = (int)(t - at); i < end && ok; ++i, ++t, ++seq) {
+            const int pos = i * kTile + group * 16;
+            const bool live = lane < 16 && pos < it.seen;
+            int page = 0;
+            if (live) {
+                page = table[pos >> g.page_log2];
+                if (page < 0 || page >= g.pages) {
+                    atomicCAS(g.err, 0, kCacheBadIndex);
+                    page = 0;
+                }
+            }
+            const int row = (page << g.page_log2) + (pos & (g.page - 1));
+            const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, live && !of_v));
+            const uint32_t parity = (seq & 1) ^ 1;
+            ok = wait(sh, bar(sh.rawk_empty), parity, g.err);
+            if (!ok) break;
+            if (lane == 0 && boxes) mbar_expect_tx(bar(sh.rawk_full), boxes * kBoxRows * D);
+            __syncwarp();
+            if (live && !of_v) load_rows(base + S::kRawK + group * 16 * D, kmap, row, bar(sh.rawk_full));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.rawk_full));
+            const int slot = seq & 3;
+            if (lane < 16) {
+                const float s = live ? (of_v ? g.v_scale : g.k_scale)[page] : 1.0f;
+                if (of_v) {
+                    sh.v_log2[slot][group] = log2f(s);
+                    sh.v_inv[slot][group] = 1.0f / s;
+                } else {
+                    sh.k_scale[slot][group] = s;
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.meta_full[slot]));
+            ok = wait(sh, bar(sh.rawv_empty), parity, g.err);
+            if (!ok) break;
+            if (lane == 0 && boxes) mbar_expect_tx(bar(sh.rawv_full), boxes * kBoxRows * D);
+            __syncwarp();
+            if (live && of_v) load_rows(base + S::kRawV + group * 16 * D, vmap, row, bar(sh.rawv_full));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.rawv_full));
+        }
+        at += it.tiles;
+        ++k;
+        if (t < p.hi && ok && !next_item<kRows, kTile>(g, a, unit, it)) break;
+    }
+    if (!ok) {
+        // the block's copies end before it does: K's of tile seq may be on
+        // their way, V's of tile seq - 1
+        mbar_wait(bar(sh.rawk_full), seq & 1, 0);
+        if (seq) mbar_wait(bar(sh.rawv_full), (seq - 1) & 1, 0);
+    }
+}
+
+// -------------------------------------------------------------- conversion
+
+template <int FORMAT, int D>
+__device__ __forceinline__ void convert(const CacheGeom& g, const AttendArgs& a, const Place& p,
+                                        Shared<D>& sh, uint8_t* smem, uint32_t base)
+{
+    using S = Smem<D>;
+    constexpr int kChunks = D / 16;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kConvert;
+    const int gr = lane >> 2, tq = lane & 3;
+    int unit = p.unit, k = 0;
+    bool bad = false;
+    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    long long at = p.at, t = p.lo;
+    uint32_t seq = 0;
+    while (t < p.hi) {
+        const int all = seen_by(a, it.n, it.asked, it.block * kRows / g.group);
+        const int end = (int)min((long long)it.tiles, p.hi - at);
+        for (int i = (int)(t - at); i < end; ++i, ++t, ++seq) {
+            const int buf = seq & 1;
+            const uint32_t parity = seq & 1, reuse = (seq >> 1 & 1) ^ 1;
+            // K: a row of the tile a lane, 16 codes at a time
+            wait(sh, bar(sh.rawk_full), parity, g.err);
+            wait(sh, bar(sh.key_empty[buf]), reuse, g.err);
+            {
+                const int row = warp * 32 + lane;
+                const uint32_t swizzle = D == 128 ? row & 7 : row >> 1 & 3;
+                const uint8_t* const src = smem + S::kRawK + row * D;
+                uint8_t* const dst = smem + S::kKeys + buf * S::kKeysTile + row * 128;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(src + ((c ^ swizzle) << 4));
+                    uint4 x, y;
+                    codes_half<FORMAT>(w.x, x.x, x.y);
+                    codes_half<FORMAT>(w.y, x.z, x.w);
+                    codes_half<FORMAT>(w.z, y.x, y.y);
+                    codes_half<FORMAT>(w.w, y.z, y.w);
+                    const int q = 2 * c & 7;
+                    uint8_t* const panel = dst + (c >> 2) * S::kPanel;
+                    *reinterpret_cast<uint4*>(panel + ((q ^ (row & 7)) << 4)) = x;
+                    *reinterpret_cast<uint4*>(panel + (((q + 1) ^ (row & 7)) << 4)) = y;
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(sh.key_full[buf]));
+                mbar_arrive(bar(sh.rawk_empty));
+            }
+            // V: 16 tokens x 32 dims at a time; row n of a chunk's 16 is dim
+            // 2 n for n < 8, 2 (n - 8) + 1 above
+            const bool careful = (i + 1) * kTile > all;
+            wait(sh, bar(sh.rawv_full), parity, g.err);
+            wait(sh, bar(sh.value_empty[buf]), reuse, g.err);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int group = warp * 2 + half;
+                const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+                const uint32_t swizzle = D == 128 ? mrow & 7 : mrow >> 1 & 3;
+                const uint32_t src = base + S::kRawV + mrow * D;
+                // rows n, token chunk of the transposed tile's panel of 64 tokens
+                const int n0 = (lane >> 3 & 1) * 8 + (lane & 7);
+                const int chunk = (group & 3) * 2 + (lane >> 4);
+                const uint32_t dst = base + S::kValues + buf * S::kValuesTile + (group >> 2) * (D * 128) +
+                                     n0 * 128 + ((chunk ^ (n0 & 7)) << 4);
+#pragma unroll
+                for (int c = 0; c < kChunks; c += 2) {
+                    uint32_t w[4], f[8];
+                    ldmatrix4_trans(w, src + (((c + (lane >> 4)) ^ swizzle) << 4));
+                    if (careful) {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            const int x0 = i * kTile + group * 16 + (m & 1) * 8 + 2 * tq;
+                            if (x0 >= it.seen) w[m] &= 0xFFFF0000u;
+                            if (x0 + 1 >= it.seen) w[m] &= 0x0000FFFFu;
+                            if (FORMAT == BACON_E4M3 && (((w[m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if ((w[m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
+                                        w[m] &= ~(0xFFu << (8 * e));
+                                        atomicMin(&sh.nan_at[k & 3][(c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
+                                                  x0 + (e >> 1));
+                                        sh.nan_any[k & 3] = 1;
+                                    }
+                            }
+                        }
+                    }
+                    pairs_half<FORMAT>(w[0], f[0], f[1]);
+                    pairs_half<FORMAT>(w[1], f[2], f[3]);
+                    pairs_half<FORMAT>(w[2], f[4], f[5]);
+                    pairs_half<FORMAT>(w[3], f[6], f[7]);
+                    stmatrix4(dst + c * 16 * 128, f);
+                    stmatrix4(dst + (c + 1) * 16 * 128, f + 4);
+                }
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(sh.value_full[buf]));
+                mbar_arrive(bar(sh.rawv_empty));
+            }
+        }
+        at += it.tiles;
+        ++k;
+        if (t < p.hi && !next_item<kRows, kTile>(g, a, unit, it)) break;
+    }
+}
+
+// ---------------------------------------------------------------- products
+
+// Row tiles of an item.
+__device__ __forceinline__ int halves_of(const CacheGeom& g, const Item& it)
+{
+    return (long long)it.asked * g.group - (long long)it.block * kRows > kHalf ? 2 : 1;
+}
+
+template <int D>
+__device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, const Place& p,
+                                      Shared<D>& sh, uint32_t base)
+{
+    using S = Smem<D>;
+    const bool leader = elect_one();
+    const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, ld_shared(smem_u32(&sh.tmem)), 0);
+    constexpr uint32_t hi = sdesc_hi(1024u);
+    const uint32_t q_lo = sdesc_lo(base), k_lo = sdesc_lo(base + S::kKeys), v_lo = sdesc_lo(base + S::kValues);
+    int unit = p.unit;
+    bool bad = false, ok = true;
+    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    long long at = p.at, t = p.lo;
+    uint32_t seq = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
+
+    auto scores = [&](int m, uint32_t s) {
+        if (leader) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t step = (kk / 4) * (S::kPanel >> 4) + (kk % 4) * 2u;
+                umma_bf16(tmem + m * 128, q_lo + m * (S::kQHalf >> 4) + step, hi,
+                          k_lo + (s & 1) * (S::kKeysTile >> 4) + step, hi, idesc_f16(kHalf, kTile), kk > 0);
+            }
+            umma_commit(bar(sh.s_full[m]));
+        }
+    };
+    while (t < p.hi && ok) {
+        const int halves = halves_of(g, it);
+        const int tiles = (int)(min((long long)it.tiles, p.hi - at) - (t - at));
+        for (int m = 0; m < halves && ok; ++m) {
+            ok = wait(sh, bar(sh.q_full[m]), q_phase[m], g.err);
+            q_phase[m] ^= 1;
+        }
+        ok = ok && wait(sh, bar(sh.key_full[seq & 1]), seq >> 1 & 1, g.err);
+        if (!ok) break;
+        fence_after_sync();
+        for (int m = 0; m < halves; ++m) scores(m, seq);
+        if (leader) umma_commit(bar(sh.key_empty[seq & 1]));
+        for (int i = 0; i < tiles && ok; ++i, ++seq) {
+            for (int m = 0; m < halves && ok; ++m) {
+                ok = wait(sh, bar(sh.p_full[m]), p_phase[m], g.err);
+                p_phase[m] ^= 1;
+                if (m == 0) ok = ok && wait(sh, bar(sh.value_full[seq & 1]), seq >> 1 & 1, g.err);
+                if (!ok) break;
+                fence_after_sync();
+                if (leader) {
+#pragma unroll
+                    for (int kk = 0; kk < kTile / 16; ++kk)
+                        umma_ts(tmem + 256 + m * 128, tmem + m * 128 + kk * 8,
+                                v_lo + (seq & 1) * (S::kValuesTile >> 4) + (kk / 4) * (D * 128 >> 4) +
+                                    (kk % 4) * 2u,
+                                hi, idesc_f16(kHalf, D), i > 0 || kk > 0);
+                    if (m == halves - 1) umma_commit(bar(sh.value_empty[seq & 1]));
+                    if (i == tiles - 1) umma_commit(bar(sh.o_full[m]));
+                }
+                if (i + 1 < tiles) {
+                    if (m == 0) ok = wait(sh, bar(sh.key_full[(seq + 1) & 1]), (seq + 1) >> 1 & 1, g.err);
+                    if (!ok) break;
+                    fence_after_sync();
+                    scores(m, seq + 1);
+                    if (leader && m == halves - 1) umma_commit(bar(sh.key_empty[(seq + 1) & 1]));
+                }
+            }
+        }
+        t += tiles;
+        at += it.tiles;
+        if (t < p.hi && ok && !next_item<kRows, kTile>(g, a, unit, it)) break;
+    }
+    // every product issued ends before tensor memory is given back
+    if (leader) {
+        umma_commit(bar(sh.drain));
+        mbar_wait(bar(sh.drain), 0, 0);
+    }
+    __syncwarp();
+}
+
+// ----------------------------------------------------------------- softmax
+
+// Largest of 16 values.
+__device__ __forceinline__ float max16(const float* v)
+{
+    const float a = max3(v[0], v[1], v[2]), b = max3(v[3], v[4], v[5]), c = max3(v[6], v[7], v[8]);
+    const float d = max3(v[9], v[10], v[11]), e = max3(v[12], v[13], v[14]);
+    return max3(max3(a, b, c), max3(d, e, v[15]), v[15]);
+}
+
+template <int FORMAT, int D>
+__device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                                        const Place& p, Shared<D>& sh, uint8_t* smem)
+{
+    using S = Smem<D>;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m = warp >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = ld_shared(smem_u32(&sh.tmem)) + ((uint32_t)(warp & 3) << 21);
+    const uint32_t logits = lanes + m * 128, out = lanes + 256 + m * 128;
+    int unit = p.unit, k = 0;
+    bool bad = false;
+    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    long long at = p.at, t = p.lo;
+    uint32_t seq = 0, s_phase = 0, o_phase = 0;
+
+    while (t < p.hi) {
+        const int begin = (int)(t - at), end = (int)min((long long)it.tiles, p.hi - at);
+        const long long c = (long long)it.block * kRows + m * kHalf + row;
+        if (m < halves_of(g, it)) {
+            const int j = (int)(c / g.group), head = it.h * g.group + (int)(c % g.group);
+            const bool mine = j < it.asked;
+            const int sees = mine ? seen_by(a, it.n, it.asked, j) : 0;
+            const int all = seen_by(a, it.n, it.asked, (it.block * kRows + m * kHalf) / g.group);
+            float factor;
+            {
+                // the row's query as fp16, scaled into its range
+                const uint16_t* const q = a.q + (long long)(it.start + j) * a.q_token_stride +
+                                          head * a.q_head_stride;
+                uint4 raw[D / 8];
+                float amax = 0.0f;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    raw[i] = make_uint4(0, 0, 0, 0);
+                    if (mine) raw[i] = *reinterpret_cast<const uint4*>(q + i * 8);
+                }
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 v = unpack16(g.dtype, w[e]);
+                        amax = max3(amax, fabsf(v.x), fabsf(v.y));
+                    }
+                }
+                const float up = query_scale(amax, factor);
+                factor *= a.scale * kLog2e;
+                uint8_t* const dst = smem + m * S::kQHalf + row * 128;
+#pragma unroll
+                for (int i = 0; i < D / 8; ++i) {
+                    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                    uint32_t h[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 v = unpack16(g.dtype, w[e]);
+                        h[e] = half2_of(v.x * up, v.y * up);
+                    }
+                    *reinterpret_cast<uint4*>(dst + (i >> 3) * S::kPanel + (((i & 7) ^ (row & 7)) << 4)) =
+                        make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            }
+            fence_proxy_async_smem();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.q_full[m]));
+
+            float top = -INFINITY, sum = 0.0f;
+            for (int i = begin; i < end; ++i) {
+                const uint32_t s = seq + (i - begin), slot = s & 3;
+                wait(sh, bar(sh.meta_full[slot]), s >> 2 & 1, g.err);
+                wait(sh, bar(sh.s_full[m]), s_phase, g.err);
+                s_phase ^= 1;
+                fence_after_sync();
+                const bool cut = (i + 1) * kTile > all;
+                const int left = sees - i * kTile;  // positions of the tile that the row sees
+                float high = -INFINITY;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float v[32];
+                    tmem_ld32(logits + q * 32, v);
+                    tmem_ld_wait_regs32(v);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (cut) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e)
+                                if (q * 32 + h * 16 + e >= left) v[h * 16 + e] = -INFINITY;
+                        }
+                        const float x = max16(v + h * 16);
+                        const float y = fmaf(x, factor * sh.k_scale[slot][q * 2 + h], sh.v_log2[slot][q * 2 + h]);
+                        if (x != -INFINITY) high = fmaxf(high, y);
+                    }
+                }
+                const bool grew = high > top + 1.0f;
+                if (__any_sync(0xFFFFFFFFu, grew)) {
+                    const float keep = grew ? fast_exp2(top - high) : 1.0f;
+                    if (grew) top = high;
+                    sum *= keep;
+                    if (i > begin) {
+#pragma unroll
+                        for (int q = 0; q < D / 32; ++q) {
+                            float v[32];
+                            tmem_ld32(out + q * 32, v);
+                            tmem_ld_wait_regs32(v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[e] *= keep;
+                            tmem_st32(out + q * 32, v);
+                        }
+                    }
+                }
+                const float ref = top == -INFINITY ? 0.0f : top - kWeightTop;
+#pragma unroll
+                for (int q = 0; q < 4; q += 2) {
+                    float w[32];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        float v[32];
+                        tmem_ld32(logits + (q + z) * 32, v);
+                        tmem_ld_wait_regs32(v);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int grp = (q + z) * 2 + h;
+                            const float f = factor * sh.k_scale[slot][grp], b = sh.v_log2[slot][grp] - ref;
+                            const unsigned long long f2 = pack2(f, f), b2 = pack2(b, b);
+                            unsigned long long part = pack2(0.0f, 0.0f);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 2) {
+                                float2 x = unpack2(fma2(pack2(v[h * 16 + e], v[h * 16 + e + 1]), f2, b2));
+                                if (cut) {
+                                    if (grp * 16 + e >= left) x.x = -INFINITY;
+                                    if (grp * 16 + e + 1 >= left) x.y = -INFINITY;
+                                }
+                                x.x = fast_exp2(x.x);
+                                x.y = fast_exp2(x.y);
+                                part = add2(part, pack2(x.x, x.y));
+                                w[z * 16 + h * 8 + e / 2] = __uint_as_float(half2_of(x.x, x.y));
+                            }
+                            const float2 y = unpack2(part);
+                            sum = fmaf(y.x + y.y, sh.v_inv[slot][grp], sum);
+                        }
+                    }
+                    // over logits that have been read: 64 tokens' weights in 32 columns
+                    tmem_st32(logits + q * 16, w);
+                }
+                tmem_st_wait();
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(sh.p_full[m]));
+            }
+
+            // ------------------------------------------------- outputs
+            wait(sh, bar(sh.o_full[m]), o_phase, g.err);
+            o_phase ^= 1;
+            fence_after_sync();
+            const bool whole = begin == 0 && end == it.tiles;
+            const bool nan = sh.nan_any[k & 3] != 0;
+            const size_t orow = (size_t)(it.start + j) * g.hq + head;
+            uint16_t* const dst = a.out + orow * D;
+            const int b = blockIdx.x;
+            const size_t slot = ((2 * (size_t)b + (begin == 0 ? 1 : 0)) * 2 + m) * kHalf;
+            const float inv = sees > 0 ? 1.0f / sum : 0.0f;
+#pragma unroll 1
+            for (int q = 0; q < D / 32; ++q) {
+                float v[32];
+                tmem_ld32(out + q * 32, v);
+                tmem_ld_wait_regs32(v);
+                if (nan) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)  // column 16 c + 8 o + n is dim 16 c + 2 n + o
+                        if (sh.nan_at[k & 3][q * 32 + (e & 16) + (e & 7) * 2 + (e >> 3 & 1)] < sees) v[e] = NAN;
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sc.many_out[slot * 128 + (q * 32 + e) * kHalf + row] = v[e];
+                } else if (mine) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int z = (e & 8) * 2 + (e & 7);
+                        w[e] = sees > 0 ? pack16(g.dtype, v[z] * inv, v[z + 8] * inv) : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<uint4*>(dst + q * 32 + e * 8) =
+                            make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                }
+            }
+            if (whole) {
+                if (mine && a.lse)
+                    a.lse[orow] = sees > 0 ? (log2f(sum) + (top - kWeightTop)) * kLn2 : -INFINITY;
+            } else {
+                sc.many_sums[slot + row] = make_float2(top, sum);
+                __threadfence();
+                const int first = owner_of(p.total, at, p.blocks);
+                const int parts = owner_of(p.total, at + it.tiles - 1, p.blocks) - first + 1;
+                named_barrier_sync(1 + m, kHalf);
+                if (row == 0) {
+                    int* const arrived = &sc.many_arrived[first * 2 + m];
+                    sh.last[m] = atomicAdd(arrived, 1) == parts - 1;
+                    if (sh.last[m]) *arrived = 0;
+                }
+                named_barrier_sync(1 + m, kHalf);
+                if (sh.last[m]) {
+                    __threadfence();
+                    auto part = [&](int q) { return ((2 * (size_t)(first + q) + (q == 0 ? 1 : 0)) * 2 + m) * kHalf; };
+                    float high = -INFINITY, total = 0.0f;
+                    for (int q = 0; q < parts; ++q) high = fmaxf(high, __ldcg(&sc.many_sums[part(q) + row]).x);
+                    for (int q = 0; q < parts; ++q) {
+                        const float2 z = __ldcg(&sc.many_sums[part(q) + row]);
+                        total += z.y * (z.x == -INFINITY ? 0.0f : fast_exp2(z.x - high));
+                    }
+                    const float scale = sees > 0 ? 1.0f / total : 0.0f;
+#pragma unroll 1
+                    for (int d = 0; d < D / 16; ++d) {
+                        float v[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+                        for (int q = 0; q < parts; ++q) {
+                            const float z = __ldcg(&sc.many_sums[part(q) + row]).x;
+                            const float f = z == -INFINITY ? 0.0f : fast_exp2(z - high);
+                            const float* const o = sc.many_out + part(q) * 128 + d * 16 * kHalf + row;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) v[e] = fmaf(__ldcg(&o[e * kHalf]), f, v[e]);
+                        }
+                        if (mine) {
+                            uint32_t w[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                w[e] = sees > 0 ? pack16(g.dtype, v[e] * scale, v[e + 8] * scale) : 0u;
+                            *reinterpret_cast<uint4*>(dst + d * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+                            *reinterpret_cast<uint4*>(dst + d * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                        }
+                    }
+                    if (mine && a.lse)
+                        a.lse[orow] = sees > 0 ? (log2f(total) + (high - kWeightTop)) * kLn2 : -INFINITY;
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.item_done[k & 3]));
+        seq += end - begin;
+        ++k;
+        t = at + end;
+        at += it.tiles;
+        if (t < p.hi && !next_item<kRows, kTile>(g, a, unit, it)) break;
+    }
+}
+
+template <int FORMAT, int D>
+__global__ void __launch_bounds__(kThreads, 1)
+many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+            CacheGeom g, AttendArgs a, SplitScratch sc)
+{
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Shared<D>& sh = *reinterpret_cast<Shared<D>*>(smem + Smem<D>::kShared);
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (uint64_t* b : {&sh.rawk_full, &sh.rawv_full, &sh.drain}) mbar_init(smem_u32(b), 1);
+        for (uint64_t* b : {&sh.rawk_empty, &sh.rawv_empty}) mbar_init(smem_u32(b), 4);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(bar(sh.key_full[i]), 4);
+            mbar_init(bar(sh.value_full[i]), 4);
+            mbar_init(bar(sh.key_empty[i]), 1);
+            mbar_init(bar(sh.value_empty[i]), 1);
+            mbar_init(bar(sh.s_full[i]), 1);
+            mbar_init(bar(sh.o_full[i]), 1);
+            mbar_init(bar(sh.p_full[i]), 4);
+            mbar_init(bar(sh.q_full[i]), 4);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(bar(sh.meta_full[i]), 1);
+            mbar_init(bar(sh.item_done[i]), 8);
+        }
+        fence_barrier_init();
+        sh.abort = 0;
+    }
+    Place p;
+    if (!find_place<kRows, kTile, kThreads>(g, a, sh.scan, sh.found, p)) return;
+    if (warp == kIssue) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        tmem_relinquish();
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t base = smem_u32(smem);
+    if (warp < kConvert) {
+        softmax<FORMAT, D>(g, a, sc, p, sh, smem);
+    } else if (warp < kIssue) {
+        convert<FORMAT, D>(g, a, p, sh, smem, base);
+    } else if (warp == kIssue) {
+        issue<D>(g, a, p, sh, base);
+    } else {
+        load<D>(&kmap, &vmap, g, a, p, sh, base);
+    }
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    if (warp == kIssue) tmem_dealloc(ld_shared(smem_u32(&sh.tmem)), 512);
+}
+
+template <int FORMAT, int D>
+cudaError_t go(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
+{
+    constexpr int bytes = Smem<D>::kBytes;
+    static const cudaError_t ready = cudaFuncSetAttribute(
+        many_kernel<FORMAT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (ready != cudaSuccess) return ready;
+    return launch_first(many_kernel<FORMAT, D>, sc.sms, kThreads, bytes, st, sc.kmap, sc.vmap, g, a, sc);
+}
+
+}  // namespace
+
+cudaError_t launch_cache_many(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                              cudaStream_t st)
+{
+    if (g.format == BACON_E4M3)
+        return g.d == 128 ? go<BACON_E4M3, 128>(g, a, sc, st) : go<BACON_E4M3, 64>(g, a, sc, st);
+    return g.d == 128 ? go<BACON_INT8, 128>(g, a, sc, st) : go<BACON_INT8, 64>(g, a, sc, st);
+}
+
+}  // namespace bacon

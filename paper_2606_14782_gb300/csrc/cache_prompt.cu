@@ -34,8 +34,15 @@ constexpr int kRows = 256;   // of an item
 constexpr int kHalf = 128;   // rows of a row tile
 constexpr int kTile = 128;   // tokens
 constexpr int kGroups = kTile / 16;
-constexpr int kConvert = 8, kIssue = 12;  // first warps of the roles; the loads are last
-constexpr int kThreads = 14 * 32;
+constexpr int kValueWarp = 8, kKeyWarp = 12, kIssueWarp = 14;  // first of each role; the loads are last
+constexpr int kThreads = 16 * 32;
+// Registers of the softmax's threads and of the others, out of 128 a thread at
+// launch: 256 x 184 + 256 x 72 = 512 x 128.
+constexpr int kSoftmaxRegs = 184, kOtherRegs = 72;
+static_assert(256 * (kSoftmaxRegs + kOtherRegs) <= kThreads * 128, "register split");
+// A row's reference follows its maximum when that has grown by 2^kSlack, with
+// the largest weight at 2^kTop then: below fp16's 2^16 in between.
+constexpr float kSlack = 8.0f, kTop = 7.0f;
 
 template <int D>
 struct Smem {
@@ -56,7 +63,7 @@ struct Shared {
     float k_scale[4][kGroups], v_log2[4][kGroups], v_inv[4][kGroups];
     uint64_t rawk_full, rawk_empty, rawv_full, rawv_empty;
     uint64_t key_full[2], key_empty[2], value_full[2], value_empty[2];
-    uint64_t s_full[2], p_full[2], o_full[2], q_full[2];
+    uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2];
     uint64_t meta_full[4], item_done[4], drain;
     long long scan[kThreads / 32];
     Found found;
@@ -187,14 +194,115 @@ __device__ __forceinline__ void load(const CUtensorMap* kmap, const CUtensorMap*
 
 // -------------------------------------------------------------- conversion
 
+// K: a row of the tile a lane, 16 codes at a time.
 template <int FORMAT, int D>
-__device__ __forceinline__ void convert(const CacheGeom& g, const AttendArgs& a, const Place& p,
-                                        Shared<D>& sh, uint8_t* smem, uint32_t base)
+__device__ __forceinline__ void convert_keys(const CacheGeom& g, const Place& p, Shared<D>& sh,
+                                             uint8_t* smem)
 {
     using S = Smem<D>;
     constexpr int kChunks = D / 16;
-    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kConvert;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kKeyWarp;
+    const uint32_t tiles = (uint32_t)(p.hi - p.lo);
+    for (uint32_t seq = 0; seq < tiles; ++seq) {
+        const int buf = seq & 1;
+        wait(sh, bar(sh.rawk_full), seq & 1, g.err);
+        wait(sh, bar(sh.key_empty[buf]), (seq >> 1 & 1) ^ 1, g.err);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int row = warp * 64 + half * 32 + lane;
+            const uint32_t swizzle = D == 128 ? row & 7 : row >> 1 & 3;
+            const uint8_t* const src = smem + S::kRawK + row * D;
+            uint8_t* const dst = smem + S::kKeys + buf * S::kKeysTile + row * 128;
+#pragma unroll
+            for (int c0 = 0; c0 < kChunks; c0 += 4) {
+                uint4 w[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    w[c] = *reinterpret_cast<const uint4*>(src + (((c0 + c) ^ swizzle) << 4));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint4 x, y;
+                    codes_half<FORMAT>(w[c].x, x.x, x.y);
+                    codes_half<FORMAT>(w[c].y, x.z, x.w);
+                    codes_half<FORMAT>(w[c].z, y.x, y.y);
+                    codes_half<FORMAT>(w[c].w, y.z, y.w);
+                    uint8_t* const panel = dst + (c0 >> 2) * S::kPanel;
+                    *reinterpret_cast<uint4*>(panel + (((2 * c) ^ (row & 7)) << 4)) = x;
+                    *reinterpret_cast<uint4*>(panel + (((2 * c + 1) ^ (row & 7)) << 4)) = y;
+                }
+            }
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(bar(sh.key_full[buf]));
+            mbar_arrive(bar(sh.rawk_empty));
+        }
+    }
+}
+
+// V: 16 tokens x 32 dims at a time; row n of a chunk's 16 in the transposed
+// tile is dim 2 n for n < 8, 2 (n - 8) + 1 above.  CUT: some row of the item
+// does not see some token of the tile, so rows that no one sees are cleared (a
+// page holds anything there) and so is a NaN, which is put back at the item's
+// end in the rows that see it.
+template <int FORMAT, int D, bool CUT>
+__device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base, int buf, int pos,
+                                                   int seen, int item)
+{
+    using S = Smem<D>;
+    const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kValueWarp;
     const int gr = lane >> 2, tq = lane & 3;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const int group = warp * 2 + half;
+        const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+        const uint32_t swizzle = D == 128 ? mrow & 7 : mrow >> 1 & 3;
+        const uint32_t src = base + S::kRawV + mrow * D;
+        // row n0 and chunk of tokens of the transposed tile's panel of 64 tokens
+        const int n0 = (lane >> 3 & 1) * 8 + (lane & 7);
+        const int chunk = (group & 3) * 2 + (lane >> 4);
+        const uint32_t dst = base + S::kValues + buf * S::kValuesTile + (group >> 2) * (D * 128) +
+                             n0 * 128 + ((chunk ^ (n0 & 7)) << 4);
+        uint32_t w[D / 32][4];
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) ldmatrix4_trans(w[c], src + (((2 * c + (lane >> 4)) ^ swizzle) << 4));
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+            uint32_t f[8];
+            if (CUT) {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const int x0 = pos + group * 16 + (m & 1) * 8 + 2 * tq;
+                    if (x0 >= seen) w[c][m] &= 0xFFFF0000u;
+                    if (x0 + 1 >= seen) w[c][m] &= 0x0000FFFFu;
+                    if (FORMAT == BACON_E4M3 && (((w[c][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if ((w[c][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
+                                w[c][m] &= ~(0xFFu << (8 * e));
+                                atomicMin(&sh.nan_at[item & 3][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
+                                          x0 + (e >> 1));
+                                sh.nan_any[item & 3] = 1;
+                            }
+                    }
+                }
+            }
+            pairs_half<FORMAT>(w[c][0], f[0], f[1]);
+            pairs_half<FORMAT>(w[c][1], f[2], f[3]);
+            pairs_half<FORMAT>(w[c][2], f[4], f[5]);
+            pairs_half<FORMAT>(w[c][3], f[6], f[7]);
+            stmatrix4(dst + c * 32 * 128, f);
+            stmatrix4(dst + (c * 32 + 16) * 128, f + 4);
+        }
+    }
+}
+
+template <int FORMAT, int D>
+__device__ __forceinline__ void convert_values(const CacheGeom& g, const AttendArgs& a, const Place& p,
+                                               Shared<D>& sh, uint32_t base)
+{
+    const int lane = threadIdx.x & 31;
     int unit = p.unit, k = 0;
     bool bad = false;
     Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
@@ -205,81 +313,12 @@ __device__ __forceinline__ void convert(const CacheGeom& g, const AttendArgs& a,
         const int end = (int)min((long long)it.tiles, p.hi - at);
         for (int i = (int)(t - at); i < end; ++i, ++t, ++seq) {
             const int buf = seq & 1;
-            const uint32_t parity = seq & 1, reuse = (seq >> 1 & 1) ^ 1;
-            // K: a row of the tile a lane, 16 codes at a time
-            wait(sh, bar(sh.rawk_full), parity, g.err);
-            wait(sh, bar(sh.key_empty[buf]), reuse, g.err);
-            {
-                const int row = warp * 32 + lane;
-                const uint32_t swizzle = D == 128 ? row & 7 : row >> 1 & 3;
-                const uint8_t* const src = smem + S::kRawK + row * D;
-                uint8_t* const dst = smem + S::kKeys + buf * S::kKeysTile + row * 128;
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(src + ((c ^ swizzle) << 4));
-                    uint4 x, y;
-                    codes_half<FORMAT>(w.x, x.x, x.y);
-                    codes_half<FORMAT>(w.y, x.z, x.w);
-                    codes_half<FORMAT>(w.z, y.x, y.y);
-                    codes_half<FORMAT>(w.w, y.z, y.w);
-                    const int q = 2 * c & 7;
-                    uint8_t* const panel = dst + (c >> 2) * S::kPanel;
-                    *reinterpret_cast<uint4*>(panel + ((q ^ (row & 7)) << 4)) = x;
-                    *reinterpret_cast<uint4*>(panel + (((q + 1) ^ (row & 7)) << 4)) = y;
-                }
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(bar(sh.key_full[buf]));
-                mbar_arrive(bar(sh.rawk_empty));
-            }
-            // V: 16 tokens x 32 dims at a time; row n of a chunk's 16 is dim
-            // 2 n for n < 8, 2 (n - 8) + 1 above
-            const bool careful = (i + 1) * kTile > all;
-            wait(sh, bar(sh.rawv_full), parity, g.err);
-            wait(sh, bar(sh.value_empty[buf]), reuse, g.err);
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int group = warp * 2 + half;
-                const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
-                const uint32_t swizzle = D == 128 ? mrow & 7 : mrow >> 1 & 3;
-                const uint32_t src = base + S::kRawV + mrow * D;
-                // rows n, token chunk of the transposed tile's panel of 64 tokens
-                const int n0 = (lane >> 3 & 1) * 8 + (lane & 7);
-                const int chunk = (group & 3) * 2 + (lane >> 4);
-                const uint32_t dst = base + S::kValues + buf * S::kValuesTile + (group >> 2) * (D * 128) +
-                                     n0 * 128 + ((chunk ^ (n0 & 7)) << 4);
-#pragma unroll
-                for (int c = 0; c < kChunks; c += 2) {
-                    uint32_t w[4], f[8];
-                    ldmatrix4_trans(w, src + (((c + (lane >> 4)) ^ swizzle) << 4));
-                    if (careful) {
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) {
-                            const int x0 = i * kTile + group * 16 + (m & 1) * 8 + 2 * tq;
-                            if (x0 >= it.seen) w[m] &= 0xFFFF0000u;
-                            if (x0 + 1 >= it.seen) w[m] &= 0x0000FFFFu;
-                            if (FORMAT == BACON_E4M3 && (((w[m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
-#pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if ((w[m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
-                                        w[m] &= ~(0xFFu << (8 * e));
-                                        atomicMin(&sh.nan_at[k & 3][(c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
-                                                  x0 + (e >> 1));
-                                        sh.nan_any[k & 3] = 1;
-                                    }
-                            }
-                        }
-                    }
-                    pairs_half<FORMAT>(w[0], f[0], f[1]);
-                    pairs_half<FORMAT>(w[1], f[2], f[3]);
-                    pairs_half<FORMAT>(w[2], f[4], f[5]);
-                    pairs_half<FORMAT>(w[3], f[6], f[7]);
-                    stmatrix4(dst + c * 16 * 128, f);
-                    stmatrix4(dst + (c + 1) * 16 * 128, f + 4);
-                }
-            }
+            wait(sh, bar(sh.rawv_full), seq & 1, g.err);
+            wait(sh, bar(sh.value_empty[buf]), (seq >> 1 & 1) ^ 1, g.err);
+            if ((i + 1) * kTile > all)
+                convert_value_tile<FORMAT, D, true>(sh, base, buf, i * kTile, it.seen, k);
+            else
+                convert_value_tile<FORMAT, D, false>(sh, base, buf, i * kTile, it.seen, k);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -341,18 +380,23 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
         if (leader) umma_commit(bar(sh.key_empty[seq & 1]));
         for (int i = 0; i < tiles && ok; ++i, ++seq) {
             for (int m = 0; m < halves && ok; ++m) {
-                ok = wait(sh, bar(sh.p_full[m]), p_phase[m], g.err);
-                p_phase[m] ^= 1;
-                if (m == 0) ok = ok && wait(sh, bar(sh.value_full[seq & 1]), seq >> 1 & 1, g.err);
-                if (!ok) break;
-                fence_after_sync();
-                if (leader) {
+                if (m == 0) ok = wait(sh, bar(sh.value_full[seq & 1]), seq >> 1 & 1, g.err);
+                // the weights of the first and of the second 64 tokens
+                for (int h = 0; h < 2 && ok; ++h) {
+                    ok = wait(sh, bar(sh.p_full[m][h]), p_phase[m], g.err);
+                    if (!ok) break;
+                    fence_after_sync();
+                    if (leader) {
 #pragma unroll
-                    for (int kk = 0; kk < kTile / 16; ++kk)
-                        umma_ts(tmem + 256 + m * 128, tmem + m * 128 + kk * 8,
-                                v_lo + (seq & 1) * (S::kValuesTile >> 4) + (kk / 4) * (D * 128 >> 4) +
-                                    (kk % 4) * 2u,
-                                hi, idesc_f16(kHalf, D), i > 0 || kk > 0);
+                        for (int kk = 0; kk < 4; ++kk)
+                            umma_ts(tmem + 256 + m * 128, tmem + m * 128 + h * 32 + kk * 8,
+                                    v_lo + (seq & 1) * (S::kValuesTile >> 4) + h * (D * 128 >> 4) + kk * 2u,
+                                    hi, idesc_f16(kHalf, D), i > 0 || h > 0 || kk > 0);
+                    }
+                }
+                p_phase[m] ^= 1;
+                if (!ok) break;
+                if (leader) {
                     if (m == halves - 1) umma_commit(bar(sh.value_empty[seq & 1]));
                     if (i == tiles - 1) umma_commit(bar(sh.o_full[m]));
                 }
@@ -387,6 +431,103 @@ __device__ __forceinline__ float max16(const float* v)
     return max3(max3(a, b, c), max3(d, e, v[15]), v[15]);
 }
 
+// One tile of a row's logits into weights.  CUT: the row sees only the first
+// `left` of the tile's tokens, or all for left >= 128.  `scaled`: O holds
+// sums that follow the reference.
+template <int D, bool CUT>
+__device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot, uint32_t logits,
+                                             uint32_t out, bool scaled, int left, float factor,
+                                             float& top, float& sum)
+{
+    const int lane = threadIdx.x & 31;
+    float v[128], high = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) tmem_ld32(logits + q * 32, v + q * 32);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        tmem_ld_wait_regs32(v + q * 32);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int grp = q * 2 + h;
+            if (CUT) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (grp * 16 + e >= left) v[grp * 16 + e] = -INFINITY;
+            }
+            const float x = max16(v + grp * 16);
+            const float y = fmaf(x, factor * sh.k_scale[slot][grp], sh.v_log2[slot][grp]);
+            if (x != -INFINITY) high = fmaxf(high, y);
+        }
+    }
+    const bool grew = high > top + kSlack;
+    if (__any_sync(0xFFFFFFFFu, grew)) {
+        const float keep = grew ? fast_exp2(top - high) : 1.0f;
+        if (grew) top = high;
+        sum *= keep;
+        if (scaled) {
+#pragma unroll
+            for (int q = 0; q < D / 16; ++q) {
+                float o[16];
+                tmem_ld16(out + q * 16, o);
+                tmem_ld_wait_regs16(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] *= keep;
+                tmem_st8(out + q * 16, o);
+                tmem_st8(out + q * 16 + 8, o + 8);
+            }
+        }
+    }
+    const float ref = top == -INFINITY ? 0.0f : top - kTop;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const int grp = half * 4 + h;
+            float w[8];
+            const float f = factor * sh.k_scale[slot][grp], b = sh.v_log2[slot][grp] - ref;
+            const unsigned long long f2 = pack2(f, f), b2 = pack2(b, b);
+            unsigned long long part = pack2(0.0f, 0.0f);
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const float* const x = v + grp * 16 + e;
+                float2 y = unpack2(fma2(pack2(x[0], x[1]), f2, b2));
+                if (CUT) {  // (a factor that underflows makes -inf a NaN)
+                    if (grp * 16 + e >= left) y.x = -INFINITY;
+                    if (grp * 16 + e + 1 >= left) y.y = -INFINITY;
+                }
+                y.x = fast_exp2(y.x);
+                y.y = fast_exp2(y.y);
+                part = add2(part, pack2(y.x, y.y));
+                w[e / 2] = __uint_as_float(half2_of(y.x, y.y));
+            }
+            const float2 y = unpack2(part);
+            sum = fmaf(y.x + y.y, sh.v_inv[slot][grp], sum);
+            // over the logits: 16 tokens' weights in 8 columns
+            tmem_st8(logits + grp * 8, w);
+        }
+        tmem_st_wait();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.p_full[m][half]));
+    }
+}
+
+// 32 columns of a row of O, column 16 c + 8 o + n being dim 16 c + 2 n + o, as
+// the output's values.
+__device__ __forceinline__ void store_row(uint16_t* dst, const float* v, float scale, bool some, int dtype)
+{
+    uint32_t w[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const int z = (e & 8) * 2 + (e & 7);
+        w[e] = some ? pack16(dtype, v[z] * scale, v[z + 8] * scale) : 0u;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint4*>(dst + e * 8) =
+            make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+}
+
 template <int FORMAT, int D>
 __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
                                         const Place& p, Shared<D>& sh, uint8_t* smem)
@@ -410,42 +551,50 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             const bool mine = j < it.asked;
             const int sees = mine ? seen_by(a, it.n, it.asked, j) : 0;
             const int all = seen_by(a, it.n, it.asked, (it.block * kRows + m * kHalf) / g.group);
-            float factor;
+            // the rows' queries as fp16, each scaled into its range: D / 8
+            // lanes a row
+            float factor = 1.0f;
             {
-                // the row's query as fp16, scaled into its range
-                const uint16_t* const q = a.q + (long long)(it.start + j) * a.q_token_stride +
-                                          head * a.q_head_stride;
-                uint4 raw[D / 8];
-                float amax = 0.0f;
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+                const long long offset = mine ? (long long)(it.start + j) * a.q_token_stride +
+                                                    head * a.q_head_stride
+                                              : -1;
+                const int piece = lane % kLanes;
+                uint4 raw[kLanes];
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
+                for (int i = 0; i < kLanes; ++i) {
+                    const long long from = __shfl_sync(0xFFFFFFFFu, offset, i * kAtOnce + lane / kLanes);
                     raw[i] = make_uint4(0, 0, 0, 0);
-                    if (mine) raw[i] = *reinterpret_cast<const uint4*>(q + i * 8);
+                    if (from >= 0) raw[i] = *reinterpret_cast<const uint4*>(a.q + from + piece * 8);
                 }
 #pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
+                for (int i = 0; i < kLanes; ++i) {
                     const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                    float2 v[4];
+                    float amax = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float2 v = unpack16(g.dtype, w[e]);
-                        amax = max3(amax, fabsf(v.x), fabsf(v.y));
+                        v[e] = unpack16(g.dtype, w[e]);
+                        amax = max3(amax, fabsf(v[e].x), fabsf(v[e].y));
                     }
+#pragma unroll
+                    for (int o = 1; o < kLanes; o <<= 1)
+                        amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+                    float back;
+                    const float up = query_scale(amax, back);
+                    const int r = i * kAtOnce + lane / kLanes;
+#pragma unroll
+                    for (int z = 0; z < kAtOnce; ++z) {
+                        const float f = __shfl_sync(0xFFFFFFFFu, back, z * kLanes);
+                        if (lane == i * kAtOnce + z) factor = f;
+                    }
+                    const int to = (warp & 3) * 32 + r;
+                    *reinterpret_cast<uint4*>(smem + m * S::kQHalf + (piece >> 3) * S::kPanel + to * 128 +
+                                              (((piece & 7) ^ (to & 7)) << 4)) =
+                        make_uint4(half2_of(v[0].x * up, v[0].y * up), half2_of(v[1].x * up, v[1].y * up),
+                                   half2_of(v[2].x * up, v[2].y * up), half2_of(v[3].x * up, v[3].y * up));
                 }
-                const float up = query_scale(amax, factor);
                 factor *= a.scale * kLog2e;
-                uint8_t* const dst = smem + m * S::kQHalf + row * 128;
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) {
-                    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                    uint32_t h[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 v = unpack16(g.dtype, w[e]);
-                        h[e] = half2_of(v.x * up, v.y * up);
-                    }
-                    *reinterpret_cast<uint4*>(dst + (i >> 3) * S::kPanel + (((i & 7) ^ (row & 7)) << 4)) =
-                        make_uint4(h[0], h[1], h[2], h[3]);
-                }
             }
             fence_proxy_async_smem();
             fence_before_sync();
@@ -461,79 +610,10 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 fence_after_sync();
                 const bool cut = (i + 1) * kTile > all;
                 const int left = sees - i * kTile;  // positions of the tile that the row sees
-                float high = -INFINITY;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float v[32];
-                    tmem_ld32(logits + q * 32, v);
-                    tmem_ld_wait_regs32(v);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (cut) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (q * 32 + h * 16 + e >= left) v[h * 16 + e] = -INFINITY;
-                        }
-                        const float x = max16(v + h * 16);
-                        const float y = fmaf(x, factor * sh.k_scale[slot][q * 2 + h], sh.v_log2[slot][q * 2 + h]);
-                        if (x != -INFINITY) high = fmaxf(high, y);
-                    }
-                }
-                const bool grew = high > top + 1.0f;
-                if (__any_sync(0xFFFFFFFFu, grew)) {
-                    const float keep = grew ? fast_exp2(top - high) : 1.0f;
-                    if (grew) top = high;
-                    sum *= keep;
-                    if (i > begin) {
-#pragma unroll
-                        for (int q = 0; q < D / 32; ++q) {
-                            float v[32];
-                            tmem_ld32(out + q * 32, v);
-                            tmem_ld_wait_regs32(v);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] *= keep;
-                            tmem_st32(out + q * 32, v);
-                        }
-                    }
-                }
-                const float ref = top == -INFINITY ? 0.0f : top - kWeightTop;
-#pragma unroll
-                for (int q = 0; q < 4; q += 2) {
-                    float w[32];
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        float v[32];
-                        tmem_ld32(logits + (q + z) * 32, v);
-                        tmem_ld_wait_regs32(v);
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int grp = (q + z) * 2 + h;
-                            const float f = factor * sh.k_scale[slot][grp], b = sh.v_log2[slot][grp] - ref;
-                            const unsigned long long f2 = pack2(f, f), b2 = pack2(b, b);
-                            unsigned long long part = pack2(0.0f, 0.0f);
-#pragma unroll
-                            for (int e = 0; e < 16; e += 2) {
-                                float2 x = unpack2(fma2(pack2(v[h * 16 + e], v[h * 16 + e + 1]), f2, b2));
-                                if (cut) {
-                                    if (grp * 16 + e >= left) x.x = -INFINITY;
-                                    if (grp * 16 + e + 1 >= left) x.y = -INFINITY;
-                                }
-                                x.x = fast_exp2(x.x);
-                                x.y = fast_exp2(x.y);
-                                part = add2(part, pack2(x.x, x.y));
-                                w[z * 16 + h * 8 + e / 2] = __uint_as_float(half2_of(x.x, x.y));
-                            }
-                            const float2 y = unpack2(part);
-                            sum = fmaf(y.x + y.y, sh.v_inv[slot][grp], sum);
-                        }
-                    }
-                    // over logits that have been read: 64 tokens' weights in 32 columns
-                    tmem_st32(logits + q * 16, w);
-                }
-                tmem_st_wait();
-                fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(sh.p_full[m]));
+                if (cut)
+                    softmax_tile<D, true>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
+                else
+                    softmax_tile<D, false>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
             }
 
             // ------------------------------------------------- outputs
@@ -561,21 +641,12 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
 #pragma unroll
                     for (int e = 0; e < 32; ++e) sc.many_out[slot * 128 + (q * 32 + e) * kHalf + row] = v[e];
                 } else if (mine) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int z = (e & 8) * 2 + (e & 7);
-                        w[e] = sees > 0 ? pack16(g.dtype, v[z] * inv, v[z + 8] * inv) : 0u;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<uint4*>(dst + q * 32 + e * 8) =
-                            make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                    store_row(dst + q * 32, v, inv, sees > 0, g.dtype);
                 }
             }
             if (whole) {
                 if (mine && a.lse)
-                    a.lse[orow] = sees > 0 ? (log2f(sum) + (top - kWeightTop)) * kLn2 : -INFINITY;
+                    a.lse[orow] = sees > 0 ? (log2f(sum) + (top - kTop)) * kLn2 : -INFINITY;
             } else {
                 sc.many_sums[slot + row] = make_float2(top, sum);
                 __threadfence();
@@ -599,28 +670,25 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                     }
                     const float scale = sees > 0 ? 1.0f / total : 0.0f;
 #pragma unroll 1
-                    for (int d = 0; d < D / 16; ++d) {
-                        float v[16];
+                    for (int d = 0; d < D / 32; ++d) {
+                        float v[32];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+                        for (int e = 0; e < 32; ++e) v[e] = 0.0f;
+#pragma unroll 2
                         for (int q = 0; q < parts; ++q) {
                             const float z = __ldcg(&sc.many_sums[part(q) + row]).x;
                             const float f = z == -INFINITY ? 0.0f : fast_exp2(z - high);
-                            const float* const o = sc.many_out + part(q) * 128 + d * 16 * kHalf + row;
+                            const float* const o = sc.many_out + part(q) * 128 + d * 32 * kHalf + row;
+                            float x[32];
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) v[e] = fmaf(__ldcg(&o[e * kHalf]), f, v[e]);
-                        }
-                        if (mine) {
-                            uint32_t w[8];
+                            for (int e = 0; e < 32; ++e) x[e] = __ldcg(&o[e * kHalf]);
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                w[e] = sees > 0 ? pack16(g.dtype, v[e] * scale, v[e + 8] * scale) : 0u;
-                            *reinterpret_cast<uint4*>(dst + d * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-                            *reinterpret_cast<uint4*>(dst + d * 16 + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                            for (int e = 0; e < 32; ++e) v[e] = fmaf(x[e], f, v[e]);
                         }
+                        if (mine) store_row(dst + d * 32, v, scale, sees > 0, g.dtype);
                     }
                     if (mine && a.lse)
-                        a.lse[orow] = sees > 0 ? (log2f(total) + (high - kWeightTop)) * kLn2 : -INFINITY;
+                        a.lse[orow] = sees > 0 ? (log2f(total) + (high - kTop)) * kLn2 : -INFINITY;
                 }
             }
         }
@@ -644,15 +712,17 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         for (uint64_t* b : {&sh.rawk_full, &sh.rawv_full, &sh.drain}) mbar_init(smem_u32(b), 1);
-        for (uint64_t* b : {&sh.rawk_empty, &sh.rawv_empty}) mbar_init(smem_u32(b), 4);
+        mbar_init(bar(sh.rawk_empty), kIssueWarp - kKeyWarp);
+        mbar_init(bar(sh.rawv_empty), kKeyWarp - kValueWarp);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(sh.key_full[i]), 4);
-            mbar_init(bar(sh.value_full[i]), 4);
+            mbar_init(bar(sh.key_full[i]), kIssueWarp - kKeyWarp);
+            mbar_init(bar(sh.value_full[i]), kKeyWarp - kValueWarp);
             mbar_init(bar(sh.key_empty[i]), 1);
             mbar_init(bar(sh.value_empty[i]), 1);
             mbar_init(bar(sh.s_full[i]), 1);
             mbar_init(bar(sh.o_full[i]), 1);
-            mbar_init(bar(sh.p_full[i]), 4);
+            mbar_init(bar(sh.p_full[i][0]), 4);
+            mbar_init(bar(sh.p_full[i][1]), 4);
             mbar_init(bar(sh.q_full[i]), 4);
         }
         for (int i = 0; i < 4; ++i) {
@@ -664,7 +734,7 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
     }
     Place p;
     if (!find_place<kRows, kTile, kThreads>(g, a, sh.scan, sh.found, p)) return;
-    if (warp == kIssue) {
+    if (warp == kIssueWarp) {
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();
     }
@@ -672,19 +742,24 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
     __syncthreads();
     fence_after_sync();
     const uint32_t base = smem_u32(smem);
-    if (warp < kConvert) {
+    if (warp < kValueWarp) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kSoftmaxRegs));
         softmax<FORMAT, D>(g, a, sc, p, sh, smem);
-    } else if (warp < kIssue) {
-        convert<FORMAT, D>(g, a, p, sh, smem, base);
-    } else if (warp == kIssue) {
-        issue<D>(g, a, p, sh, base);
     } else {
-        load<D>(&kmap, &vmap, g, a, p, sh, base);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kOtherRegs));
+        if (warp < kKeyWarp)
+            convert_values<FORMAT, D>(g, a, p, sh, base);
+        else if (warp < kIssueWarp)
+            convert_keys<FORMAT, D>(g, p, sh, smem);
+        else if (warp == kIssueWarp)
+            issue<D>(g, a, p, sh, base);
+        else
+            load<D>(&kmap, &vmap, g, a, p, sh, base);
     }
     fence_before_sync();
     __syncthreads();
     fence_after_sync();
-    if (warp == kIssue) tmem_dealloc(ld_shared(smem_u32(&sh.tmem)), 512);
+    if (warp == kIssueWarp) tmem_dealloc(ld_shared(smem_u32(&sh.tmem)), 512);
 }
 
 template <int FORMAT, int D>

@@ -30,37 +30,57 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 64;     // tokens
-constexpr int kWarps = 4;     // that compute
-constexpr int kThreads = 32 * (kWarps + 1);
-constexpr int kStages = 4;
+constexpr int kTile = 64;  // tokens of a stage
+constexpr int kGroups = 4; // of 16 tokens
 
 struct Meta {  // of 16 tokens of a stage
     float k_scale, v_log2, v_inv;
 };
 
-template <int D, int NT>
-struct Smem {
+// Sizes for CG groups of 8 NT columns.  A warp takes 16 tokens of a stage and a
+// group's columns; with two groups the codes are converted by two warps each,
+// which costs less than 32 columns' sums in one warp's registers do: 9 warps
+// have 168 registers a thread, 128 of them would be sums.  Bytes on their way
+// per SM: 3 x 3, 2 x 4 or 6 stages of 16 KB.
+template <int D, int NT, int CG>
+struct Sizes {
+    static constexpr int kWarps = 4 * CG;  // that compute
+    static constexpr int kThreads = 32 * (kWarps + 1);
+    static constexpr int kColumns = 8 * NT * CG;
+    static constexpr int kPerSm = CG == 2 ? 1 : NT == 2 ? 2 : 3;
+    static constexpr int kStages = CG == 2 ? 6 : NT == 2 ? 4 : 3;
     static constexpr int kRows = kTile * D;        // bytes of K, or V, of a stage
     static constexpr int kStage = 2 * kRows;
-    static constexpr int kJoin = kStages * kStage; // two warps' outputs
-    static constexpr int kQ = kJoin + 2 * NT * D * 8 * 4;
-    // queries as fp16 fragments, where they do not stay in registers
-    static constexpr int kMeta = kQ + (NT > 2 ? NT * D * 8 * 2 : 0);
-    static constexpr int kBytes = kMeta + 2048;
+    static constexpr int kJoin = kStages * kStage; // half of the warps' outputs
+    static constexpr int kPitch = D * 2 + 32;      // of a query row: 8 rows on distinct banks
+    static constexpr int kQueries = kColumns * kPitch;
+    static constexpr int kRaw = kJoin + CG * 2 * NT * D * 8 * 4;  // two items' query rows
+    static constexpr int kShared = kRaw + 2 * kQueries;
+    static constexpr int kBytes = kShared + 3072;
+};
+static_assert(3 * (Sizes<128, 1, 1>::kBytes + 1024) <= 228 * 1024, "three blocks on an SM");
+static_assert(2 * (Sizes<128, 2, 1>::kBytes + 1024) <= 228 * 1024, "two blocks on an SM");
+static_assert(Sizes<128, 2, 2>::kBytes <= 227 * 1024, "one block on an SM");
+
+struct Segment {  // tiles [begin, end) of an item, whose first tile is tile `at` of the call
+    Item it;
+    int begin, end;
+    long long at;
 };
 
+template <int STAGES>
 struct Shared {
-    Meta meta[kStages][kWarps];
-    float top[kWarps][32], sum[kWarps][32];
-    uint64_t full[kStages], empty[kStages];
-    long long scan[kWarps + 1];
+    Meta meta[STAGES][kGroups];
+    float top[kGroups][32], sum[kGroups][32];
+    uint64_t full[STAGES], empty[STAGES], q_full[2], q_empty[2];
+    Segment seg[2];
+    long long scan[9];
     Found found;
-    int abort;
-    int nan_at[128];        // per dim: first position of a NaN of V that not every column sees
+    int abort, last;
+    int nan_at[128];  // per dim: first position of a NaN of V that not every column sees
     int nan_any;
 };
-static_assert(sizeof(Shared) <= 2048, "shared record");
+static_assert(sizeof(Shared<6>) <= 3072, "shared record");
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -77,15 +97,21 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <int FORMAT, int D, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : NT == 2 ? 2 : 1)
+template <int N>
+struct Count {
+    static constexpr int value = N;
+};
+
+template <int FORMAT, int D, int NT, int CG>
+__global__ void __launch_bounds__(Sizes<D, NT, CG>::kThreads, Sizes<D, NT, CG>::kPerSm)
 few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
            CacheGeom g, AttendArgs a, SplitScratch sc)
 {
-    using S = Smem<D, NT>;
-    constexpr int kChunks = D / 16;
+    using S = Sizes<D, NT, CG>;
+    constexpr int kChunks = D / 16, kWarps = S::kWarps, kStages = S::kStages;
+    constexpr int kThreads = S::kThreads, kColumns = S::kColumns;
     extern __shared__ __align__(1024) uint8_t smem[];
-    Shared& sh = *reinterpret_cast<Shared*>(smem + S::kMeta);
+    auto& sh = *reinterpret_cast<Shared<kStages>*>(smem + S::kShared);
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
@@ -94,39 +120,71 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
             mbar_init(smem_u32(&sh.full[s]), 1);
             mbar_init(smem_u32(&sh.empty[s]), kWarps);
         }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&sh.q_full[s]), 1);
+            mbar_init(smem_u32(&sh.q_empty[s]), kWarps);
+        }
         fence_barrier_init();
         sh.abort = sh.nan_any = 0;
     }
     for (int i = tid; i < 128; i += kThreads) sh.nan_at[i] = 0x7FFFFFFF;
 
     Place place;
-    if (!find_place<8 * NT, kTile, kThreads>(g, a, sh.scan, sh.found, place)) return;
+    if (!find_place<kColumns, kTile, kThreads, 1>(g, a, sh.scan, sh.found, place)) return;
     const int b = blockIdx.x, blocks = place.blocks;
     const long long total = place.total, lo = place.lo, hi = place.hi;
-    bool bad = false;
-
-    int unit = place.unit;
-    Item it = item_of<8 * NT, kTile>(g, a, unit, place.block, bad);
-    long long at = place.at;  // the item's first tile
     const uint32_t abort_flag = smem_u32(&sh.abort);
 
     if (warp == kWarps) {
         // ------------------------------------------------------ loads
-        // lanes 0-3: K's 16-row groups of a tile, lanes 4-7: V's
-        const int group = lane & 3;
-        const CUtensorMap* const map = lane < 4 ? &kmap : &vmap;
-        const float* const scales = lane < 4 ? g.k_scale : g.v_scale;
-        int stage = 0, issued = 0;
+        int unit = place.unit;
+        bool bad = false;
+        Item it = item_of<kColumns, kTile>(g, a, unit, place.block, bad);
+        long long at = place.at;  // the item's first tile
+        int stage = 0, issued = 0, items = 0;
         uint32_t phase = 0;
         bool stop = false;
         long long t = lo;
         while (t < hi && !stop) {
+            const int begin = (int)(t - at), end = (int)min((long long)it.tiles, hi - at);
+            {
+                // the item and its query rows, a lane a column
+                const int slot = items & 1;
+                const uint32_t full = smem_u32(&sh.q_full[slot]);
+                if (!mbar_wait(smem_u32(&sh.q_empty[slot]), (items >> 1 & 1) ^ 1, abort_flag)) {
+                    stop = true;
+                    break;
+                }
+                if (lane == 0) sh.seg[slot] = Segment{it, begin, end, at};
+                const int c = it.block * kColumns + lane, j = c / g.group;
+                const bool live = lane < kColumns && j < it.asked;
+                const int rows = __popc(__ballot_sync(0xFFFFFFFFu, live));
+                if (lane == 0) mbar_expect_tx(full, rows * D * 2);
+                __syncwarp();
+                const int row = S::kRaw + slot * S::kQueries + lane * S::kPitch;
+                if (live) {
+                    load_bytes(base + row,
+                               a.q + (long long)(it.start + j) * a.q_token_stride +
+                                   (it.h * g.group + c % g.group) * a.q_head_stride,
+                               D * 2, full);
+                } else if (lane < kColumns) {
+#pragma unroll 1
+                    for (int i = 0; i < D * 2; i += 16)
+                        *reinterpret_cast<uint4*>(smem + row + i) = make_uint4(0, 0, 0, 0);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full);
+                ++items;
+            }
+            // lanes 0-3: K's 16-row groups of a tile, lanes 4-7: V's
+            const int group = lane % kGroups;
+            const bool of_v = lane >= kGroups;
+            const float* const scales = of_v ? g.v_scale : g.k_scale;
             const int32_t* const table =
                 a.table + (((size_t)it.r * g.layers + a.layer) * g.hkv + it.h) * g.max_blocks;
-            const int end = (int)min((long long)it.tiles, hi - at);
-            for (int i = (int)(t - at); i < end; ++i, ++t) {
+            for (int i = begin; i < end; ++i, ++t) {
                 const int pos = i * kTile + group * 16;
-                const bool live = lane < 8 && pos < it.seen;
+                const bool live = lane < 2 * kGroups && pos < it.seen;
                 int page = 0;
                 if (live) {
                     page = table[pos >> g.page_log2];
@@ -145,13 +203,13 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 __syncwarp();
                 float s = 1.0f;
                 if (live) {
-                    load_rows(base + stage * S::kStage + (lane >> 2) * S::kRows + group * 16 * D, map,
-                              (page << g.page_log2) + (pos & (g.page - 1)), full);
+                    load_rows(base + stage * S::kStage + (of_v ? S::kRows : 0) + group * 16 * D,
+                              of_v ? &vmap : &kmap, (page << g.page_log2) + (pos & (g.page - 1)), full);
                     s = scales[page];
                 }
-                if (lane < 4) {
+                if (lane < kGroups) {
                     sh.meta[stage][group].k_scale = s;
-                } else if (lane < 8) {
+                } else if (lane < 2 * kGroups) {
                     sh.meta[stage][group].v_log2 = log2f(s);
                     sh.meta[stage][group].v_inv = 1.0f / s;
                 }
@@ -164,7 +222,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 }
             }
             at += it.tiles;
-            if (t < hi && !stop && !next_item<8 * NT, kTile>(g, a, unit, it)) break;
+            if (t < hi && !stop && !next_item<kColumns, kTile>(g, a, unit, it)) break;
         }
         if (stop) {
             // the block's copies end before it does
@@ -174,40 +232,46 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
             }
             for (int i = max(0, issued - kStages); i < issued; ++i)
                 mbar_wait(smem_u32(&sh.full[i % kStages]), i / kStages & 1, 0);
+            for (int i = max(0, items - 2); i < items; ++i)
+                mbar_wait(smem_u32(&sh.q_full[i & 1]), i >> 1 & 1, 0);
         }
         return;
     }
 
     // ---------------------------------------------------------- products
     const int gr = lane >> 2, tq = lane & 3;
+    const int group = warp % kGroups, first_col = warp / kGroups * 8 * NT;
     int stage = 0;
     uint32_t phase = 0;
     float acc[kChunks][NT][4];
     float top[NT][2], sum[NT][2], factor[NT][2];
     int sees[NT][2];
-    uint32_t qf[NT > 2 ? 1 : kChunks][NT > 2 ? 1 : NT][2];
+    uint32_t qf[kChunks][NT][2];
     // matrix loads: lane l gives row l & 7 of matrix l >> 3; matrices are rows
     // 0-7, rows 8-15, of 16-byte chunk c, then of c + 1
-    const int mrow = warp * 16 + (lane & 7) + (lane >> 3 & 1) * 8, mchunk = lane >> 4;
+    const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8, mchunk = lane >> 4;
     const uint32_t swizzle = D == 128 ? mrow & 7 : mrow >> 1 & 3;
 
-    for (long long t = lo; t < hi;) {
+    int items = 0;
+    for (long long t = lo; t < hi; ++items) {
+        const int slot = items & 1;
+        if (!mbar_wait(smem_u32(&sh.q_full[slot]), items >> 1 & 1, abort_flag) && lane == 0) {
+            st_shared_volatile(abort_flag, 1);
+            atomicCAS(g.err, 0, kCacheTimeout);
+        }
+        __syncwarp();
+        const Segment seg = sh.seg[slot];
+        const Item& it = seg.it;
         // the item's queries as fragments: column g of an n-tile, dims 16 c +
         // 4 tq ... + 3 of every chunk c
-        const uint16_t* qrow[NT];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int c = it.block * 8 * NT + nt * 8 + gr, j = c / g.group;
-            qrow[nt] = j < it.asked ? a.q + (long long)(it.start + j) * a.q_token_stride +
-                                          (it.h * g.group + c % g.group) * a.q_head_stride
-                                    : nullptr;
             float amax = 0.0f;
             uint2 raw[kChunks];
 #pragma unroll
-            for (int k = 0; k < kChunks; ++k) {
-                raw[k] = make_uint2(0, 0);
-                if (qrow[nt]) raw[k] = *reinterpret_cast<const uint2*>(qrow[nt] + k * 16 + tq * 4);
-            }
+            for (int k = 0; k < kChunks; ++k)
+                raw[k] = *reinterpret_cast<const uint2*>(smem + S::kRaw + slot * S::kQueries +
+                                                         (first_col + nt * 8 + gr) * S::kPitch + k * 32 + tq * 8);
 #pragma unroll
             for (int k = 0; k < kChunks; ++k) {
                 const float2 u = unpack16(g.dtype, raw[k].x), v = unpack16(g.dtype, raw[k].y);
@@ -223,18 +287,12 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll
             for (int k = 0; k < kChunks; ++k) {
                 const float2 u = unpack16(g.dtype, raw[k].x), v = unpack16(g.dtype, raw[k].y);
-                const uint2 f = make_uint2(half2_of(u.x * up, u.y * up), half2_of(v.x * up, v.y * up));
-                if (NT > 2) {
-                    if (warp == nt % kWarps)
-                        *reinterpret_cast<uint2*>(smem + S::kQ + ((k * NT + nt) * 32 + lane) * 8) = f;
-                } else {
-                    qf[NT > 2 ? 0 : k][NT > 2 ? 0 : nt][0] = f.x;
-                    qf[NT > 2 ? 0 : k][NT > 2 ? 0 : nt][1] = f.y;
-                }
+                qf[k][nt][0] = half2_of(u.x * up, u.y * up);
+                qf[k][nt][1] = half2_of(v.x * up, v.y * up);
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int col = it.block * 8 * NT + nt * 8 + tq * 2 + i;
+                const int col = it.block * kColumns + first_col + nt * 8 + tq * 2 + i;
                 sees[nt][i] = col / g.group < it.asked ? seen_by(a, it.n, it.asked, col / g.group) : 0;
                 top[nt][i] = -INFINITY;
                 sum[nt][i] = 0.0f;
@@ -244,21 +302,21 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[k][nt][i] = 0.0f;
         }
-        if (NT > 2) named_barrier_sync(1, 32 * kWarps);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.q_empty[slot]));
         // positions that every column sees
-        const int all = seen_by(a, it.n, it.asked, it.block * 8 * NT / g.group);
-
-        const int begin = (int)(t - at), end = (int)min((long long)it.tiles, hi - at);
+        const int all = seen_by(a, it.n, it.asked, it.block * kColumns / g.group);
+        const int begin = seg.begin, end = seg.end;
         for (int i = begin; i < end; ++i) {
             if (!mbar_wait(smem_u32(&sh.full[stage]), phase, abort_flag) && lane == 0) {
                 st_shared_volatile(abort_flag, 1);
                 atomicCAS(g.err, 0, kCacheTimeout);
             }
             __syncwarp();
-            const int pos = i * kTile + warp * 16;
+            const int pos = i * kTile + group * 16;
             if (pos < it.seen) {
                 const uint32_t krow = base + stage * S::kStage + mrow * D;
-                const Meta meta = sh.meta[stage][warp];
+                const Meta meta = sh.meta[stage][group];
                 float s[NT][2][4];  // two chains of products
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -275,18 +333,8 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     codes_half<FORMAT>(w[3], f[5], f[7]);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        uint2 q0, q1;
-                        if (NT > 2) {
-                            q0 = *reinterpret_cast<const uint2*>(smem + S::kQ + ((c * NT + nt) * 32 + lane) * 8);
-                            q1 = *reinterpret_cast<const uint2*>(smem + S::kQ +
-                                                                 (((c + 1) * NT + nt) * 32 + lane) * 8);
-                        } else {
-                            constexpr int z = NT > 2 ? 0 : 1;
-                            q0 = make_uint2(qf[c * z][nt * z][0], qf[c * z][nt * z][1]);
-                            q1 = make_uint2(qf[(c + 1) * z][nt * z][0], qf[(c + 1) * z][nt * z][1]);
-                        }
-                        mma(s[nt][0], f, q0.x, q0.y);
-                        mma(s[nt][1], f + 4, q1.x, q1.y);
+                        mma(s[nt][0], f, qf[c][nt][0], qf[c][nt][1]);
+                        mma(s[nt][1], f + 4, qf[c + 1][nt][0], qf[c + 1][nt][1]);
                     }
                 }
                 // exponents, the running maximum, weights
@@ -385,8 +433,8 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) sum[nt][k] += __shfl_xor_sync(0xFFFFFFFFu, sum[nt][k], o);
                 if (gr == 0) {
-                    sh.top[warp][nt * 8 + tq * 2 + k] = top[nt][k];
-                    sh.sum[warp][nt * 8 + tq * 2 + k] = sum[nt][k];
+                    sh.top[group][first_col + nt * 8 + tq * 2 + k] = top[nt][k];
+                    sh.sum[group][first_col + nt * 8 + tq * 2 + k] = sum[nt][k];
                 }
             }
         named_barrier_sync(1, 32 * kWarps);
@@ -395,14 +443,14 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const int col = nt * 8 + tq * 2 + k;
+                const int col = first_col + nt * 8 + tq * 2 + k;
                 float m = sh.top[0][col];
 #pragma unroll
-                for (int w = 1; w < kWarps; ++w) m = fmaxf(m, sh.top[w][col]);
+                for (int w = 1; w < kGroups; ++w) m = fmaxf(m, sh.top[w][col]);
                 const float f = top[nt][k] == -INFINITY ? 0.0f : fast_exp2(top[nt][k] - m);
                 float l = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kWarps; ++w)  // (a sum of NaN has no maximum)
+                for (int w = 0; w < kGroups; ++w)  // (a sum of NaN has no maximum)
                     l += sh.sum[w][col] * (sh.top[w][col] == -INFINITY ? 0.0f : fast_exp2(sh.top[w][col] - m));
                 top[nt][k] = m;
                 sum[nt][k] = l;
@@ -412,66 +460,84 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     acc[c][nt][k + 2] *= f;
                 }
             }
-        float4* const join = reinterpret_cast<float4*>(smem + S::kJoin);
-        if (warp >= 2) {
+        // by halves: the upper groups' outputs are added to the lower ones'
+        float4* const join =
+            reinterpret_cast<float4*>(smem + S::kJoin) + warp / kGroups * 2 * kChunks * NT * 32;
+#pragma unroll
+        for (int half = kGroups / 2; half; half >>= 1) {
+            if (group >= half && group < 2 * half) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        join[((group - half) * kChunks * NT + c * NT + nt) * 32 + lane] =
+                            *reinterpret_cast<float4*>(acc[c][nt]);
+            }
+            named_barrier_sync(1, 32 * kWarps);
+            if (group < half) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float4 o = join[(group * kChunks * NT + c * NT + nt) * 32 + lane];
+                        acc[c][nt][0] += o.x;
+                        acc[c][nt][1] += o.y;
+                        acc[c][nt][2] += o.z;
+                        acc[c][nt][3] += o.w;
+                    }
+            }
+            if (half > 1) named_barrier_sync(1, 32 * kWarps);
+        }
+
+        const bool whole = begin == 0 && end == it.tiles;
+        if (group == 0 && nan) {
 #pragma unroll
             for (int c = 0; c < kChunks; ++c)
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    join[((warp - 2) * kChunks * NT + c * NT + nt) * 32 + lane] =
-                        *reinterpret_cast<float4*>(acc[c][nt]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (sh.nan_at[c * 16 + 2 * gr + (e >> 1)] < sees[nt][e & 1]) acc[c][nt][e] = NAN;
         }
-        named_barrier_sync(1, 32 * kWarps);
-        if (warp < 2) {
+        // chunks [c0, c0 + COUNT) of the columns' outputs, out of `from`
+        auto write = [&](auto count, const auto& from, int c0) {
+            constexpr int COUNT = decltype(count)::value;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c)
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    float4* const z = &join[(warp * kChunks * NT + c * NT + nt) * 32 + lane];
-                    const float4 o = *z;
-                    acc[c][nt][0] += o.x;
-                    acc[c][nt][1] += o.y;
-                    acc[c][nt][2] += o.z;
-                    acc[c][nt][3] += o.w;
-                    if (warp == 1) *z = *reinterpret_cast<float4*>(acc[c][nt]);
+                for (int k = 0; k < 2; ++k) {
+                    const int col = it.block * kColumns + first_col + nt * 8 + tq * 2 + k, j = col / g.group;
+                    if (j >= it.asked) continue;
+                    const size_t row = (size_t)(it.start + j) * g.hq + it.h * g.group + col % g.group;
+                    const bool none = sees[nt][k] == 0;
+                    const float inv = none ? 0.0f : 1.0f / sum[nt][k];
+                    uint32_t* const o = reinterpret_cast<uint32_t*>(a.out + row * D) + c0 * 8 + gr;
+#pragma unroll
+                    for (int c = 0; c < COUNT; ++c)
+                        o[c * 8] = none ? 0u : pack16(g.dtype, from[c][nt][k] * inv, from[c][nt][k + 2] * inv);
+                    if (a.lse && gr == 0 && c0 == 0)
+                        a.lse[row] = none ? -INFINITY
+                                          : (log2f(sum[nt][k]) + (top[nt][k] - kWeightTop)) * kLn2;
                 }
-        }
-        named_barrier_sync(1, 32 * kWarps);
-
-        const bool whole = begin == 0 && end == it.tiles;
-        const long long item_at = at;
-        bool write = warp == 0;
-        if (warp == 0) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const float4 o = join[(kChunks * NT + c * NT + nt) * 32 + lane];
-                    acc[c][nt][0] += o.x;
-                    acc[c][nt][1] += o.y;
-                    acc[c][nt][2] += o.z;
-                    acc[c][nt][3] += o.w;
-                }
-            if (nan) {
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (sh.nan_at[c * 16 + 2 * gr + (e >> 1)] < sees[nt][e & 1])
-                                acc[c][nt][e] = NAN;
-            }
-            if (!whole) {
+        };
+        if (whole) {
+            if (group == 0) write(Count<kChunks>{}, acc, 0);
+        } else {
+            const int first = owner_of(total, seg.at, blocks);
+            const int parts = owner_of(total, seg.at + it.tiles - 1, blocks) - first + 1;
+            // of a part: a column group's outputs as its warp holds them, then
+            // the columns' maxima and sums
+            const int mine = warp / kGroups * kChunks * NT * 32 + lane;
+            if (group == 0) {
                 // slot 2 b + 1: the item's first part, 2 b: a later one
-                const size_t slot = 2 * (size_t)b + (begin == 0 ? 1 : 0);
-                float4* const po = reinterpret_cast<float4*>(sc.out + slot * 32 * 128);
-                float2* const pm = reinterpret_cast<float2*>(sc.sums + slot * 64);
+                const size_t part = 2 * (size_t)b + (begin == 0 ? 1 : 0);
+                float4* const po = reinterpret_cast<float4*>(sc.out + part * 32 * 128) + mine;
+                float2* const pm = reinterpret_cast<float2*>(sc.sums + part * 64) + first_col;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        po[(c * NT + nt) * 32 + lane] = *reinterpret_cast<float4*>(acc[c][nt]);
+                        po[(c * NT + nt) * 32] = *reinterpret_cast<float4*>(acc[c][nt]);
                 if (gr == 0)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
@@ -479,82 +545,87 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                         for (int k = 0; k < 2; ++k)
                             pm[nt * 8 + tq * 2 + k] = make_float2(top[nt][k], sum[nt][k]);
                 __threadfence();
-                __syncwarp();
-                const int first = owner_of(total, item_at, blocks);
-                const int parts = owner_of(total, item_at + it.tiles - 1, blocks) - first + 1;
-                int last = 0;
-                if (lane == 0) {
-                    last = atomicAdd(&sc.arrived[first], 1) == parts - 1;
-                    if (last) sc.arrived[first] = 0;
-                }
-                write = __shfl_sync(0xFFFFFFFFu, last, 0) != 0;
-                if (write) {
+            }
+            named_barrier_sync(1, 32 * kWarps);
+            if (tid == 0) {
+                __threadfence();
+                const int last = atomicAdd(&sc.arrived[first], 1) == parts - 1;
+                if (last) sc.arrived[first] = 0;
+                sh.last = last;
+            }
+            named_barrier_sync(1, 32 * kWarps);
+            if (sh.last) {
+                // the parts in the blocks' order, some at a time, each warp
+                // its chunks of the outputs
+                constexpr int kOwn = kChunks / kGroups;
+                constexpr int kBatch = NT == 1 ? 8 : 4;
+                const int c0 = group * kOwn;
+                {
                     __threadfence();
-                    float m[NT][2];
+                    float o[kOwn][NT][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        top[nt][0] = top[nt][1] = -INFINITY;
+                        sum[nt][0] = sum[nt][1] = 0.0f;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            m[nt][k] = -INFINITY;
-                            for (int q = 0; q < parts; ++q) {
-                                const float2* const pq = reinterpret_cast<const float2*>(
-                                    sc.sums + (2 * (size_t)(first + q) + (q == 0)) * 64);
-                                m[nt][k] = fmaxf(m[nt][k], __ldcg(&pq[nt * 8 + tq * 2 + k]).x);
+                        for (int c = 0; c < kOwn; ++c)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[c][nt][e] = 0.0f;
+                    }
+#pragma unroll 1
+                    for (int q0 = 0; q0 < parts; q0 += kBatch) {
+                        float2 z[kBatch][NT][2];
+                        float4 x[kBatch][kOwn][NT];
+#pragma unroll
+                        for (int q = 0; q < kBatch; ++q) {
+                            const bool there = q0 + q < parts;
+                            const size_t part = 2 * (size_t)(first + q0 + q) + (q0 + q == 0 ? 1 : 0);
+                            const float2* const pm = reinterpret_cast<const float2*>(sc.sums + part * 64) + first_col;
+                            const float4* const po = reinterpret_cast<const float4*>(sc.out + part * 32 * 128) + mine;
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                                for (int k = 0; k < 2; ++k)
+                                    z[q][nt][k] = there ? __ldcg(&pm[nt * 8 + tq * 2 + k])
+                                                        : make_float2(-INFINITY, 0.0f);
+#pragma unroll
+                                for (int c = 0; c < kOwn; ++c)
+                                    x[q][c][nt] = there ? __ldcg(&po[((c0 + c) * NT + nt) * 32])
+                                                        : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                             }
-                            top[nt][k] = m[nt][k];
-                            sum[nt][k] = 0.0f;
                         }
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) acc[c][nt][e] = 0.0f;
-                    for (int q = 0; q < parts; ++q) {
-                        const size_t part = 2 * (size_t)(first + q) + (q == 0);
-                        const float2* const pq = reinterpret_cast<const float2*>(sc.sums + part * 64);
-                        const float4* const oq = reinterpret_cast<const float4*>(sc.out + part * 32 * 128);
-                        float f[NT][2];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                const float2 z = __ldcg(&pq[nt * 8 + tq * 2 + k]);
-                                f[nt][k] = z.x == -INFINITY ? 0.0f : fast_exp2(z.x - m[nt][k]);
-                                sum[nt][k] += z.y * f[nt][k];
-                            }
+                                float m = top[nt][k];
 #pragma unroll
-                        for (int c = 0; c < kChunks; ++c)
+                                for (int q = 0; q < kBatch; ++q) m = fmaxf(m, z[q][nt][k].x);
+                                const float keep = top[nt][k] == -INFINITY ? 0.0f : fast_exp2(top[nt][k] - m);
+                                top[nt][k] = m;
+                                sum[nt][k] *= keep;
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                const float4 o = __ldcg(&oq[(c * NT + nt) * 32 + lane]);
-                                acc[c][nt][0] = fmaf(o.x, f[nt][0], acc[c][nt][0]);
-                                acc[c][nt][1] = fmaf(o.y, f[nt][1], acc[c][nt][1]);
-                                acc[c][nt][2] = fmaf(o.z, f[nt][0], acc[c][nt][2]);
-                                acc[c][nt][3] = fmaf(o.w, f[nt][1], acc[c][nt][3]);
+                                for (int c = 0; c < kOwn; ++c) {
+                                    o[c][nt][k] *= keep;
+                                    o[c][nt][k + 2] *= keep;
+                                }
+#pragma unroll
+                                for (int q = 0; q < kBatch; ++q) {
+                                    const float2 y = z[q][nt][k];
+                                    const float f = y.x == -INFINITY ? 0.0f : fast_exp2(y.x - m);
+                                    sum[nt][k] = fmaf(y.y, f, sum[nt][k]);
+#pragma unroll
+                                    for (int c = 0; c < kOwn; ++c) {
+                                        const float4 w = x[q][c][nt];
+                                        o[c][nt][k] = fmaf(k ? w.y : w.x, f, o[c][nt][k]);
+                                        o[c][nt][k + 2] = fmaf(k ? w.w : w.z, f, o[c][nt][k + 2]);
+                                    }
+                                }
                             }
                     }
+                    write(Count<kOwn>{}, o, c0);
                 }
             }
-        }
-        if (write) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int col = it.block * 8 * NT + nt * 8 + tq * 2 + k, j = col / g.group;
-                    if (j >= it.asked) continue;
-                    const size_t row = (size_t)(it.start + j) * g.hq + it.h * g.group + col % g.group;
-                    const bool none = sees[nt][k] == 0;
-                    const float inv = none ? 0.0f : 1.0f / sum[nt][k];
-                    uint32_t* const o = reinterpret_cast<uint32_t*>(a.out + row * D);
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c)
-                        o[c * 8 + gr] = none ? 0u : pack16(g.dtype, acc[c][nt][k] * inv, acc[c][nt][k + 2] * inv);
-                    if (a.lse && gr == 0)
-                        a.lse[row] = none ? -INFINITY
-                                          : (log2f(sum[nt][k]) + (top[nt][k] - kWeightTop)) * kLn2;
-                }
         }
         named_barrier_sync(1, 32 * kWarps);
         if (nan) {  // the item's, not the next one's
@@ -562,31 +633,29 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
             if (tid == 0) sh.nan_any = 0;
             named_barrier_sync(1, 32 * kWarps);
         }
-        t = at + end;
-        at += it.tiles;
-        if (t < hi && !next_item<8 * NT, kTile>(g, a, unit, it)) break;
+        t = seg.at + end;
     }
 }
 
-template <int FORMAT, int D, int NT>
+template <int FORMAT, int D, int NT, int CG>
 cudaError_t go(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
 {
-    constexpr int bytes = Smem<D, NT>::kBytes;
+    using S = Sizes<D, NT, CG>;
     static const cudaError_t ready = cudaFuncSetAttribute(
-        few_kernel<FORMAT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        few_kernel<FORMAT, D, NT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
     if (ready != cudaSuccess) return ready;
-    constexpr int per_sm = NT == 1 ? 3 : NT == 2 ? 2 : 1;
-    static_assert(per_sm <= kBlocksPerSm, "room for partial sums");
-    return launch_first(few_kernel<FORMAT, D, NT>, sc.sms * per_sm, kThreads, bytes, st, sc.kmap, sc.vmap, g, a, sc);
+    static_assert(S::kPerSm <= kBlocksPerSm, "room for partial sums");
+    return launch_first(few_kernel<FORMAT, D, NT, CG>, sc.sms * S::kPerSm, S::kThreads, S::kBytes, st,
+                        sc.kmap, sc.vmap, g, a, sc);
 }
 
 template <int FORMAT, int D>
 cudaError_t by_columns(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
 {
     const long long columns = (long long)g.group * ((a.tokens + a.requests - 1) / a.requests);
-    if (columns <= 8) return go<FORMAT, D, 1>(g, a, sc, st);
-    if (columns <= 16) return go<FORMAT, D, 2>(g, a, sc, st);
-    return go<FORMAT, D, 4>(g, a, sc, st);
+    if (columns <= 8) return go<FORMAT, D, 1, 1>(g, a, sc, st);
+    if (columns <= 16) return go<FORMAT, D, 2, 1>(g, a, sc, st);
+    return go<FORMAT, D, 2, 2>(g, a, sc, st);
 }
 
 }  // namespace

@@ -83,6 +83,15 @@ __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, 
         : "memory");
 }
 
+// Untiled copy of `bytes` bytes (a multiple of 16, both ends 16-byte aligned).
+__device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar)
+        : "memory");
+}
+
 __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;\n" ::"r"(bar), "r"(bytes)
@@ -224,8 +233,9 @@ struct Found {
     int unit, block;
 };
 
-// Scan of the units' tiles by the whole block; false when it has none.
-template <int ROWS, int TILE, int THREADS>
+// Scan of the units' tiles by the whole block; false when it has none.  A block
+// gets about LEAST tiles at least: fewer parts to join.
+template <int ROWS, int TILE, int THREADS, int LEAST>
 __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs& a, long long* scan,
                                            Found& found, Place& p)
 {
@@ -256,7 +266,8 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
         if (w == warp) x += p.total;
         p.total += scan[w];
     }
-    p.blocks = p.total < (long long)gridDim.x ? (int)p.total : (int)gridDim.x;
+    const long long most = (p.total + LEAST - 1) / LEAST;
+    p.blocks = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
     if ((int)blockIdx.x >= p.blocks) return false;
     p.lo = first_tile(p.total, blockIdx.x, p.blocks);
     p.hi = first_tile(p.total, blockIdx.x + 1, p.blocks);

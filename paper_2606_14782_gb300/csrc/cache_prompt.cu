@@ -380,7 +380,10 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
         if (leader) umma_commit(bar(sh.key_empty[seq & 1]));
         for (int i = 0; i < tiles && ok; ++i, ++seq) {
             for (int m = 0; m < halves && ok; ++m) {
+                // what is there long before the weights is waited for first
                 if (m == 0) ok = wait(sh, bar(sh.value_full[seq & 1]), seq >> 1 & 1, g.err);
+                if (m == 0 && i + 1 < tiles)
+                    ok = ok && wait(sh, bar(sh.key_full[(seq + 1) & 1]), (seq + 1) >> 1 & 1, g.err);
                 // the weights of the first and of the second 64 tokens
                 for (int h = 0; h < 2 && ok; ++h) {
                     ok = wait(sh, bar(sh.p_full[m][h]), p_phase[m], g.err);
@@ -401,9 +404,6 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
                     if (i == tiles - 1) umma_commit(bar(sh.o_full[m]));
                 }
                 if (i + 1 < tiles) {
-                    if (m == 0) ok = wait(sh, bar(sh.key_full[(seq + 1) & 1]), (seq + 1) >> 1 & 1, g.err);
-                    if (!ok) break;
-                    fence_after_sync();
                     scores(m, seq + 1);
                     if (leader && m == halves - 1) umma_commit(bar(sh.key_empty[(seq + 1) & 1]));
                 }
@@ -560,39 +560,47 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                                                     head * a.q_head_stride
                                               : -1;
                 const int piece = lane % kLanes;
-                uint4 raw[kLanes];
+                // (a rolled loop: straight-line code that runs once an item
+                // costs more in instruction fetches than it does)
+#pragma unroll 1
+                for (int i0 = 0; i0 < kLanes; i0 += 4) {
+                    uint4 raw[4];
 #pragma unroll
-                for (int i = 0; i < kLanes; ++i) {
-                    const long long from = __shfl_sync(0xFFFFFFFFu, offset, i * kAtOnce + lane / kLanes);
-                    raw[i] = make_uint4(0, 0, 0, 0);
-                    if (from >= 0) raw[i] = *reinterpret_cast<const uint4*>(a.q + from + piece * 8);
-                }
-#pragma unroll
-                for (int i = 0; i < kLanes; ++i) {
-                    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-                    float2 v[4];
-                    float amax = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = unpack16(g.dtype, w[e]);
-                        amax = max3(amax, fabsf(v[e].x), fabsf(v[e].y));
+                    for (int i = 0; i < 4; ++i) {
+                        const long long from =
+                            __shfl_sync(0xFFFFFFFFu, offset, (i0 + i) * kAtOnce + lane / kLanes);
+                        raw[i] = make_uint4(0, 0, 0, 0);
+                        if (from >= 0) raw[i] = *reinterpret_cast<const uint4*>(a.q + from + piece * 8);
                     }
 #pragma unroll
-                    for (int o = 1; o < kLanes; o <<= 1)
-                        amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-                    float back;
-                    const float up = query_scale(amax, back);
-                    const int r = i * kAtOnce + lane / kLanes;
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+                        float2 v[4];
+                        float amax = 0.0f;
 #pragma unroll
-                    for (int z = 0; z < kAtOnce; ++z) {
-                        const float f = __shfl_sync(0xFFFFFFFFu, back, z * kLanes);
-                        if (lane == i * kAtOnce + z) factor = f;
+                        for (int e = 0; e < 4; ++e) {
+                            v[e] = unpack16(g.dtype, w[e]);
+                            amax = max3(amax, fabsf(v[e].x), fabsf(v[e].y));
+                        }
+#pragma unroll
+                        for (int o = 1; o < kLanes; o <<= 1)
+                            amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
+                        float back;
+                        const float up = query_scale(amax, back);
+                        const int r = (i0 + i) * kAtOnce;
+#pragma unroll
+                        for (int z = 0; z < kAtOnce; ++z) {
+                            const float f = __shfl_sync(0xFFFFFFFFu, back, z * kLanes);
+                            if (lane == r + z) factor = f;
+                        }
+                        const int to = (warp & 3) * 32 + r + lane / kLanes;
+                        *reinterpret_cast<uint4*>(smem + m * S::kQHalf + (piece >> 3) * S::kPanel +
+                                                  to * 128 + (((piece & 7) ^ (to & 7)) << 4)) =
+                            make_uint4(half2_of(v[0].x * up, v[0].y * up),
+                                       half2_of(v[1].x * up, v[1].y * up),
+                                       half2_of(v[2].x * up, v[2].y * up),
+                                       half2_of(v[3].x * up, v[3].y * up));
                     }
-                    const int to = (warp & 3) * 32 + r;
-                    *reinterpret_cast<uint4*>(smem + m * S::kQHalf + (piece >> 3) * S::kPanel + to * 128 +
-                                              (((piece & 7) ^ (to & 7)) << 4)) =
-                        make_uint4(half2_of(v[0].x * up, v[0].y * up), half2_of(v[1].x * up, v[1].y * up),
-                                   half2_of(v[2].x * up, v[2].y * up), half2_of(v[3].x * up, v[3].y * up));
                 }
                 factor *= a.scale * kLog2e;
             }
@@ -733,7 +741,7 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
         sh.abort = 0;
     }
     Place p;
-    if (!find_place<kRows, kTile, kThreads>(g, a, sh.scan, sh.found, p)) return;
+    if (!find_place<kRows, kTile, kThreads, 2>(g, a, sh.scan, sh.found, p)) return;
     if (warp == kIssueWarp) {
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();

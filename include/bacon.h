@@ -388,7 +388,7 @@ typedef struct {
     int page;         /* tokens per page: 16, 32, 64 or 128                  */
     int pages;        /* pages of the pool; pages * page < 2^31              */
     int max_requests; /* largest request count of one call                   */
-    int max_blocks;   /* columns of a table                                  */
+    int max_blocks;   /* columns of a table; max_blocks * page < 2^31 - 1024  */
     int format;       /* bacon_cache_format                                  */
     int dtype;        /* bacon_dtype of rows, queries and outputs            */
     void* k;          /* device arrays as above, kept by the caller for the  */

@@ -485,7 +485,8 @@ class Cache:
         self.head_dim, self.pages, self.page = head_dim, pages, page
         self.format, self.dtype = format, dtype
         self.max_requests = max_requests
-        self.max_blocks = pages if max_blocks is None else max_blocks
+        self.max_blocks = (min(pages, ((1 << 31) - 1025) // page) if max_blocks is None
+                           else max_blocks)
         codes, scales = (pages, page, head_dim), (pages,)
         self.k, self.v = (torch.empty(codes, dtype=torch.uint8, device="cuda") if t is None else t
                           for t in (k, v))

@@ -56,8 +56,8 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
         return fail(BACON_EINVAL, "page must be 16, 32, 64 or 128, got %d", d.page);
     if ((long long)d.pages * d.page >= 1ll << 31)
         return fail(BACON_EINVAL, "pages * page must be below 2^31");
-    if ((long long)d.max_blocks * d.page >= 1ll << 31)
-        return fail(BACON_EINVAL, "max_blocks * page must be below 2^31");
+    if ((long long)d.max_blocks * d.page >= (1ll << 31) - 1024)
+        return fail(BACON_EINVAL, "max_blocks * page must be below 2^31 - 1024");
     if ((long long)d.max_requests * d.layers * d.kv_heads >= 1ll << 31)
         return fail(BACON_EINVAL, "max_requests * layers * kv_heads must be below 2^31");
     if (d.format != BACON_E4M3 && d.format != BACON_INT8)

@@ -130,16 +130,15 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     for (int i = tid; i < 128; i += kThreads) sh.nan_at[i] = 0x7FFFFFFF;
 
     Place place;
-    if (!find_place<kColumns, kTile, kThreads, 1>(g, a, sh.scan, sh.found, place)) return;
-    const int b = blockIdx.x, blocks = place.blocks;
-    const long long total = place.total, lo = place.lo, hi = place.hi;
+    if (!find_place<kColumns, kTile, kThreads, 2>(g, a, sh.scan, sh.found, place)) return;
+    const int b = blockIdx.x;
+    const long long lo = place.lo, hi = place.hi;
     const uint32_t abort_flag = smem_u32(&sh.abort);
 
     if (warp == kWarps) {
         // ------------------------------------------------------ loads
         int unit = place.unit;
-        bool bad = false;
-        Item it = item_of<kColumns, kTile>(g, a, unit, place.block, bad);
+        Item it = sh.found.it;
         long long at = place.at;  // the item's first tile
         int stage = 0, issued = 0, items = 0;
         uint32_t phase = 0;
@@ -176,23 +175,35 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 if (lane == 0) mbar_arrive(full);
                 ++items;
             }
+            // on their way ahead of their use: the next unit's length, pages
+            // by two tiles, scales by one
+            const bool last_of_unit = it.block + 1 >= blocks_of<kColumns>(g, it.asked);
+            const int ahead = last_of_unit ? length_ahead(g, a, unit) : 0;
             // lanes 0-3: K's 16-row groups of a tile, lanes 4-7: V's
             const int group = lane % kGroups;
             const bool of_v = lane >= kGroups;
             const float* const scales = of_v ? g.v_scale : g.k_scale;
             const int32_t* const table =
                 a.table + (((size_t)it.r * g.layers + a.layer) * g.hkv + it.h) * g.max_blocks;
+            const int upto = lane < 2 * kGroups ? (int)min((long long)it.seen, (long long)end * kTile) : 0;
+            auto page_of = [&](int i) {
+                const int pos = i * kTile + group * 16;
+                return pos < upto ? table[pos >> g.page_log2] : 0;
+            };
+            auto checked = [&](int page) {
+                if (page >= 0 && page < g.pages) return page;
+                atomicCAS(g.err, 0, kCacheBadIndex);
+                return 0;
+            };
+            int page = page_of(begin), page1 = page_of(begin + 1);
+            page = checked(page);
+            float s = scales[page];
             for (int i = begin; i < end; ++i, ++t) {
                 const int pos = i * kTile + group * 16;
-                const bool live = lane < 2 * kGroups && pos < it.seen;
-                int page = 0;
-                if (live) {
-                    page = table[pos >> g.page_log2];
-                    if (page < 0 || page >= g.pages) {
-                        atomicCAS(g.err, 0, kCacheBadIndex);
-                        page = 0;
-                    }
-                }
+                const bool live = pos < upto;
+                const int page2 = page_of(i + 2);
+                page1 = checked(page1);
+                const float s1 = scales[page1];
                 const uint32_t full = smem_u32(&sh.full[stage]);
                 if (!mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1, abort_flag)) {
                     stop = true;
@@ -201,12 +212,10 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, live));
                 if (lane == 0 && boxes) mbar_expect_tx(full, boxes * kBoxRows * D);
                 __syncwarp();
-                float s = 1.0f;
-                if (live) {
+                if (live)
                     load_rows(base + stage * S::kStage + (of_v ? S::kRows : 0) + group * 16 * D,
                               of_v ? &vmap : &kmap, (page << g.page_log2) + (pos & (g.page - 1)), full);
-                    s = scales[page];
-                }
+                if (!live) s = 1.0f;
                 if (lane < kGroups) {
                     sh.meta[stage][group].k_scale = s;
                 } else if (lane < 2 * kGroups) {
@@ -220,9 +229,25 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     stage = 0;
                     phase ^= 1;
                 }
+                page = page1;
+                page1 = page2;
+                s = s1;
             }
             at += it.tiles;
-            if (t < hi && !stop && !next_item<kColumns, kTile>(g, a, unit, it)) break;
+            if (at >= hi || stop) break;
+            if (last_of_unit) {
+                ++unit;
+                it.n = ahead >= 0 && ahead <= (long long)g.max_blocks << g.page_log2 ? ahead : 0;
+                it.r = unit / g.hkv;
+                it.h = unit - it.r * g.hkv;
+                const Asked q = asked_of(g, a, it.r);
+                it.start = q.start;
+                it.asked = q.asked;
+                set_block<kColumns, kTile>(g, a, it, 0);
+                if (it.asked == 0 && !next_item<kColumns, kTile>(g, a, unit, it)) break;
+            } else {
+                set_block<kColumns, kTile>(g, a, it, it.block + 1);
+            }
         }
         if (stop) {
             // the block's copies end before it does
@@ -523,8 +548,8 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
         if (whole) {
             if (group == 0) write(Count<kChunks>{}, acc, 0);
         } else {
-            const int first = owner_of(total, seg.at, blocks);
-            const int parts = owner_of(total, seg.at + it.tiles - 1, blocks) - first + 1;
+            const int first = place.owner_of(seg.at);
+            const int parts = place.owner_of(seg.at + it.tiles - 1) - first + 1;
             // of a part: a column group's outputs as its warp holds them, then
             // the columns' maxima and sums
             const int mine = warp / kGroups * kChunks * NT * 32 + lane;
@@ -548,7 +573,6 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
             }
             named_barrier_sync(1, 32 * kWarps);
             if (tid == 0) {
-                __threadfence();
                 const int last = atomicAdd(&sc.arrived[first], 1) == parts - 1;
                 if (last) sc.arrived[first] = 0;
                 sh.last = last;

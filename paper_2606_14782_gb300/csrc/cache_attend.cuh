@@ -195,6 +195,14 @@ __device__ __forceinline__ Item item_of(const CacheGeom& g, const AttendArgs& a,
     return it;
 }
 
+// The length of the unit after `unit`, as it stands there (nothing waits for it).
+__device__ __forceinline__ int length_ahead(const CacheGeom& g, const AttendArgs& a, int unit)
+{
+    if (++unit >= a.requests * g.hkv) return 0;
+    const int r = unit / g.hkv;
+    return a.lengths[((size_t)r * g.layers + a.layer) * g.hkv + (unit - r * g.hkv)];
+}
+
 // The item after `it` that has rows; false at the end of the call's.
 template <int ROWS, int TILE>
 __device__ __forceinline__ bool next_item(const CacheGeom& g, const AttendArgs& a, int& unit, Item& it)
@@ -211,82 +219,197 @@ __device__ __forceinline__ bool next_item(const CacheGeom& g, const AttendArgs& 
     return false;
 }
 
-// First tile of block b of `blocks`, and the block that has tile t.
-__device__ __forceinline__ long long first_tile(long long total, int b, int blocks)
+// x / y; in 32 bits where that is enough.
+__device__ __forceinline__ long long quotient(long long x, long long y)
 {
-    return total * b / blocks;
-}
-__device__ __forceinline__ int owner_of(long long total, long long t, int blocks)
-{
-    return (int)(((t + 1) * blocks - 1) / total);
+    return (x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y);
 }
 
 // Tiles [lo, hi) of the call's `total`, all items' one after the other, are
-// this block's, one of `blocks`; the first of them is in item (unit, block),
-// whose first tile is `at`.
+// this block's, one of `blocks`; the first of them is in the item that `Found`
+// has, one of unit `unit` whose first tile is `at`.
 struct Place {
     long long total, lo, hi, at;
-    int blocks, unit, block;
+    long long share;  // tiles of a block; the first `more` blocks have one more
+    int blocks, more, unit;
+
+    __device__ __forceinline__ void deal(int least, int grid)
+    {
+        const long long most = quotient(total + least - 1, least);
+        blocks = most < grid ? (int)most : grid;
+        share = blocks ? quotient(total, blocks) : 0;
+        more = (int)(total - share * blocks);
+    }
+    __device__ __forceinline__ long long first_tile(int b) const { return share * b + min(b, more); }
+    __device__ __forceinline__ int owner_of(long long tile) const
+    {
+        const long long long_ones = (share + 1) * more;
+        return tile < long_ones ? (int)quotient(tile, share + 1)
+                                : more + (int)quotient(tile - long_ones, share);
+    }
 };
 struct Found {
+    Item it;
     long long at;
-    int unit, block;
+    int unit;
 };
 
-// Scan of the units' tiles by the whole block; false when it has none.  A block
+// Scan of the items' tiles by the whole block; false when it has none.  A block
 // gets about LEAST tiles at least: fewer parts to join.
+//
+// An entry is an item when all requests have the same number of queries, else
+// a unit with all its items.  Each warp takes a run of entries, a lane an
+// entry at a time: their sums give the total and the warps' places, and the
+// warp that has the block's first tile walks its entries again to find it.
 template <int ROWS, int TILE, int THREADS, int LEAST>
 __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs& a, long long* scan,
                                            Found& found, Place& p)
 {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int units = a.requests * g.hkv;
-    const int per = (units + THREADS - 1) / THREADS, u0 = tid * per, u1 = min(units, u0 + per);
+    constexpr int kWarps = THREADS / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const bool same = a.starts == nullptr;
+    Asked q = {0, 0};
+    if (same) q = asked_of(g, a, 0);
+    const unsigned each = same ? blocks_of<ROWS>(g, q.asked) : 1;
+    const unsigned entries = (unsigned)a.requests * g.hkv * each;
+    const unsigned run = (entries + THREADS - 1) / THREADS * 32;
+    const unsigned e0 = warp * run + lane, e1 = min(entries, (warp + 1) * run);
+    bool bad = blockIdx.x == 0 && starts_are_bad(a, threadIdx.x, THREADS);
+
+    // entry e as its first item, the number of its items in `items`
+    auto entry = [&](unsigned e, int& unit, int& items) {
+        Item it;
+        int block = 0;
+        unit = (int)e;
+        if (each > 1) {
+            unit = (int)(e / each);
+            block = (int)(e - unit * each);
+        }
+        it.r = (unsigned)unit / (unsigned)g.hkv;
+        it.h = unit - it.r * g.hkv;
+        it.n = length_of(g, a, it.r, it.h, bad);
+        if (!same) q = asked_of(g, a, it.r);
+        it.asked = q.asked;
+        it.start = same ? it.r * q.asked : q.start;
+        items = same ? 1 : blocks_of<ROWS>(g, q.asked);
+        set_block<ROWS, TILE>(g, a, it, block);
+        return it;
+    };
+    // tiles of all of an entry's items
+    auto tiles_of = [&](Item it, int items) {
+        long long sum = items ? it.tiles : 0;
+        for (int i = 1; i < items; ++i) {
+            set_block<ROWS, TILE>(g, a, it, i);
+            sum += it.tiles;
+        }
+        return sum;
+    };
     long long mine = 0;
-    bool bad = blockIdx.x == 0 && starts_are_bad(a, tid, THREADS);
-    for (int u = u0; u < u1; ++u) {
-        Item it = item_of<ROWS, TILE>(g, a, u, 0, bad);
-        const int blocks = blocks_of<ROWS>(g, it.asked);
-        for (int c = 0; c < blocks; ++c) {
-            set_block<ROWS, TILE>(g, a, it, c);
-            mine += it.tiles;
+    // one item a unit, which sees all its tokens: only lengths are needed, on
+    // their way together and kept
+    const bool short_run = same && each == 1 && run <= 256;
+    int n[8];
+    auto tiles_of_unit = [](int x) { return max(1, (int)(((unsigned)x + TILE - 1) / TILE)); };
+    if (short_run) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned e = e0 + i * 32, r = e / (unsigned)g.hkv;
+            n[i] = -1;
+            if (e < e1) n[i] = a.lengths[((size_t)r * g.layers + a.layer) * g.hkv + (e - r * g.hkv)];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e0 + i * 32 < e1) {
+                if (n[i] < 0 || n[i] > (long long)g.max_blocks << g.page_log2) {
+                    bad = true;
+                    n[i] = 0;
+                }
+                mine += tiles_of_unit(n[i]);
+            }
+    } else {
+        for (unsigned e = e0; e < e1; e += 32) {
+            int unit, items;
+            const Item it = entry(e, unit, items);
+            mine += tiles_of(it, items);
         }
     }
     if (bad) atomicCAS(g.err, 0, kCacheBadIndex);
-    long long x = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 31) scan[warp] = x;
+    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+    if (lane == 0) scan[warp] = mine;
     __syncthreads();
+    long long before = 0;
     p.total = 0;
-    for (int w = 0; w < THREADS / 32; ++w) {
-        if (w == warp) x += p.total;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w == warp) before = p.total;
         p.total += scan[w];
     }
-    const long long most = (p.total + LEAST - 1) / LEAST;
-    p.blocks = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
+    p.deal(LEAST, gridDim.x);
     if ((int)blockIdx.x >= p.blocks) return false;
-    p.lo = first_tile(p.total, blockIdx.x, p.blocks);
-    p.hi = first_tile(p.total, blockIdx.x + 1, p.blocks);
-    if (p.lo >= x - mine && p.lo < x) {
-        long long at = x - mine;
-        for (int u = u0; u < u1; ++u) {
-            Item it = item_of<ROWS, TILE>(g, a, u, 0, bad);
-            const int blocks = blocks_of<ROWS>(g, it.asked);
-            for (int c = 0; c < blocks; ++c) {
-                set_block<ROWS, TILE>(g, a, it, c);
-                if (at <= p.lo && p.lo < at + it.tiles) found = Found{at, u, c};
-                at += it.tiles;
+    p.lo = p.first_tile(blockIdx.x);
+    p.hi = p.first_tile(blockIdx.x + 1);
+    const bool has = p.lo >= before && p.lo < before + mine;
+    if (has && short_run) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int own = n[i] < 0 ? 0 : tiles_of_unit(n[i]);
+            int x = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
             }
+            const int all = __shfl_sync(0xFFFFFFFFu, x, 31);
+            if (p.lo < before + all) {
+                if (before + x - own <= p.lo && p.lo < before + x) {
+                    Item it;
+                    const int unit = (int)(e0 + i * 32);
+                    it.r = (unsigned)unit / (unsigned)g.hkv;
+                    it.h = unit - it.r * g.hkv;
+                    it.block = 0;
+                    it.n = it.seen = n[i];
+                    it.asked = q.asked;
+                    it.start = it.r * q.asked;
+                    it.tiles = own;
+                    found = Found{it, before + x - own, unit};
+                }
+                break;
+            }
+            before += all;
+        }
+    } else if (has) {
+        for (unsigned e = e0;; e += 32) {
+            int unit = 0, items = 0;
+            Item it;
+            long long own = 0;
+            if (e < e1) {
+                it = entry(e, unit, items);
+                own = tiles_of(it, items);
+            }
+            long long x = own;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
+            }
+            const long long all = __shfl_sync(0xFFFFFFFFu, x, 31);
+            if (p.lo < before + all) {
+                long long at = before + x - own;
+                if (at <= p.lo && p.lo < at + own) {
+                    for (int i = 1; p.lo >= at + it.tiles; ++i) {
+                        at += it.tiles;
+                        set_block<ROWS, TILE>(g, a, it, i);
+                    }
+                    found = Found{it, at, unit};
+                }
+                break;
+            }
+            before += all;
         }
     }
     __syncthreads();
     p.at = found.at;
     p.unit = found.unit;
-    p.block = found.block;
     return true;
 }
 

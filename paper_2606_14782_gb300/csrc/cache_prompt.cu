@@ -128,8 +128,8 @@ __device__ __forceinline__ void load(const CUtensorMap* kmap, const CUtensorMap*
     const int lane = threadIdx.x & 31, group = lane & 7;
     const bool of_v = lane >= 8;
     int unit = p.unit, k = 0;
-    bool bad = false, ok = true;
-    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    bool ok = true;
+    Item it = sh.found.it;
     long long at = p.at, t = p.lo;
     uint32_t seq = 0;
     while (t < p.hi && ok) {
@@ -304,8 +304,7 @@ __device__ __forceinline__ void convert_values(const CacheGeom& g, const AttendA
 {
     const int lane = threadIdx.x & 31;
     int unit = p.unit, k = 0;
-    bool bad = false;
-    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    Item it = sh.found.it;
     long long at = p.at, t = p.lo;
     uint32_t seq = 0;
     while (t < p.hi) {
@@ -350,8 +349,8 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
     constexpr uint32_t hi = sdesc_hi(1024u);
     const uint32_t q_lo = sdesc_lo(base), k_lo = sdesc_lo(base + S::kKeys), v_lo = sdesc_lo(base + S::kValues);
     int unit = p.unit;
-    bool bad = false, ok = true;
-    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    bool ok = true;
+    Item it = sh.found.it;
     long long at = p.at, t = p.lo;
     uint32_t seq = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
 
@@ -538,8 +537,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
     const uint32_t lanes = ld_shared(smem_u32(&sh.tmem)) + ((uint32_t)(warp & 3) << 21);
     const uint32_t logits = lanes + m * 128, out = lanes + 256 + m * 128;
     int unit = p.unit, k = 0;
-    bool bad = false;
-    Item it = item_of<kRows, kTile>(g, a, unit, p.block, bad);
+    Item it = sh.found.it;
     long long at = p.at, t = p.lo;
     uint32_t seq = 0, s_phase = 0, o_phase = 0;
 
@@ -658,8 +656,8 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             } else {
                 sc.many_sums[slot + row] = make_float2(top, sum);
                 __threadfence();
-                const int first = owner_of(p.total, at, p.blocks);
-                const int parts = owner_of(p.total, at + it.tiles - 1, p.blocks) - first + 1;
+                const int first = p.owner_of(at);
+                const int parts = p.owner_of(at + it.tiles - 1) - first + 1;
                 named_barrier_sync(1 + m, kHalf);
                 if (row == 0) {
                     int* const arrived = &sc.many_arrived[first * 2 + m];

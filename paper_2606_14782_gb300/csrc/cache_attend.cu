@@ -130,7 +130,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     for (int i = tid; i < 128; i += kThreads) sh.nan_at[i] = 0x7FFFFFFF;
 
     Place place;
-    if (!find_place<kColumns, kTile, kThreads, 2>(g, a, sh.scan, sh.found, place)) return;
+    if (!find_place<kColumns, kTile, kThreads, 1>(g, a, sh.scan, sh.found, place)) return;
     const int b = blockIdx.x;
     const long long lo = place.lo, hi = place.hi;
     const uint32_t abort_flag = smem_u32(&sh.abort);
@@ -569,14 +569,9 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
                             pm[nt * 8 + tq * 2 + k] = make_float2(top[nt][k], sum[nt][k]);
-                __threadfence();
             }
             named_barrier_sync(1, 32 * kWarps);
-            if (tid == 0) {
-                const int last = atomicAdd(&sc.arrived[first], 1) == parts - 1;
-                if (last) sc.arrived[first] = 0;
-                sh.last = last;
-            }
+            if (tid == 0) sh.last = arrive_last(&sc.arrived[first], parts);
             named_barrier_sync(1, 32 * kWarps);
             if (sh.last) {
                 // the parts in the blocks' order, some at a time, each warp
@@ -585,7 +580,6 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 constexpr int kBatch = NT == 1 ? 8 : 4;
                 const int c0 = group * kOwn;
                 {
-                    __threadfence();
                     float o[kOwn][NT][4];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {

@@ -111,6 +111,19 @@ __device__ __forceinline__ float query_scale(float amax, float& back)
     return __uint_as_float((uint32_t)(127 - e) << 23);
 }
 
+// Counts a part that the block's threads have written (a block barrier lies
+// between their writes and this) and tells whether it is the last of `parts`.
+// Release and acquire at once: what the other blocks wrote before their counts
+// can be read by the block's threads after the next barrier.
+__device__ __forceinline__ bool arrive_last(int* count, int parts)
+{
+    int before;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;\n" : "=r"(before) : "l"(count) : "memory");
+    if (before != parts - 1) return false;
+    *count = 0;
+    return true;
+}
+
 __device__ __forceinline__ uint32_t half2_of(float x, float y)
 {
     uint32_t w;

@@ -655,18 +655,12 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                     a.lse[orow] = sees > 0 ? (log2f(sum) + (top - kTop)) * kLn2 : -INFINITY;
             } else {
                 sc.many_sums[slot + row] = make_float2(top, sum);
-                __threadfence();
                 const int first = p.owner_of(at);
                 const int parts = p.owner_of(at + it.tiles - 1) - first + 1;
                 named_barrier_sync(1 + m, kHalf);
-                if (row == 0) {
-                    int* const arrived = &sc.many_arrived[first * 2 + m];
-                    sh.last[m] = atomicAdd(arrived, 1) == parts - 1;
-                    if (sh.last[m]) *arrived = 0;
-                }
+                if (row == 0) sh.last[m] = arrive_last(&sc.many_arrived[first * 2 + m], parts);
                 named_barrier_sync(1 + m, kHalf);
                 if (sh.last[m]) {
-                    __threadfence();
                     auto part = [&](int q) { return ((2 * (size_t)(first + q) + (q == 0 ? 1 : 0)) * 2 + m) * kHalf; };
                     float high = -INFINITY, total = 0.0f;
                     for (int q = 0; q < parts; ++q) high = fmaxf(high, __ldcg(&sc.many_sums[part(q) + row]).x);

@@ -30,9 +30,16 @@ struct PlanGeom {
     int layers, hkv, page_log2, pages, max_blocks;
 };
 
+// (a unit has fewer than 2^31 - 1024 tokens)
 __device__ __forceinline__ int blocks_of(int tokens, int page_log2)
 {
-    return (int)(((long long)tokens + (1 << page_log2) - 1) >> page_log2);
+    return (tokens + (1 << page_log2) - 1) >> page_log2;
+}
+
+// x mod pages for x < 2 pages
+__device__ __forceinline__ int wrapped(unsigned x, int pages)
+{
+    return (int)(x < (unsigned)pages ? x : x - pages);
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
@@ -46,7 +53,7 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lh = g.layers * g.hkv;
     const int u0 = blockIdx.x * own, u1 = min(a.units, u0 + own), r0 = u0 / lh;
-    const long long most = (long long)g.max_blocks << g.page_log2;
+    const int most = g.max_blocks << g.page_log2;
     const bool alloc = a.ring != nullptr;
     if (tid == 0) s_bad = 0;
     __syncthreads();
@@ -55,10 +62,11 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
     // in total and before
     long long sum[4] = {0, 0, 0, 0};
     bool bad = false;
+#pragma unroll 4
     for (int u = tid; u < a.units; u += kPlanThreads) {
         const int n = a.lengths ? a.lengths[u] : 0;
         const int m = a.per_unit ? a.added[u] : a.added ? a.added[u / lh] : 1;
-        if (n < 0 || m < 0 || (long long)n + m > most) {
+        if (n < 0 || n > most || m < 0 || m > most - n) {
             bad = true;
             continue;
         }
@@ -119,7 +127,7 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
     if (tid < own && u0 + tid < u1) {
         s_n[tid] = n;
         s_a[tid] = m;
-        s_page[tid] = (int)((head + sum[1] + (long long)(x >> 32)) % g.pages);
+        s_page[tid] = wrapped(wrapped((unsigned)head + (unsigned)sum[1], g.pages) + (unsigned)(x >> 32), g.pages);
         int row = (int)sum[3];
         if (a.per_unit) {
             row += (int)(uint32_t)x;
@@ -129,7 +137,7 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
         s_row[tid] = row;
     }
     if (alloc && blockIdx.x == 0 && tid == 0) {
-        a.state_out[0] = given ? (int)((head + sum[0]) % g.pages) : head;
+        a.state_out[0] = given ? wrapped((unsigned)head + (unsigned)sum[0], g.pages) : head;
         a.state_out[1] = given ? (int)(count - sum[0]) : count;
     }
     __syncthreads();
@@ -142,22 +150,20 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
             const int have = blocks_of(n0, g.page_log2);
             const int gets = alloc ? blocks_of(n0 + add, g.page_log2) - have : 0;
             int32_t* const entry = a.table + (size_t)u * g.max_blocks;
-            for (int b = lane; b < gets; b += 32)
-                entry[have + b] = a.ring[((long long)first + b) % g.pages];
-            const int l = u / g.hkv % g.layers, h = u % g.hkv;
+            for (int b = lane; b < gets; b += 32) entry[have + b] = a.ring[wrapped((unsigned)first + b, g.pages)];
+            int32_t* const to = a.per_unit
+                                    ? a.slots + row
+                                    : a.slots + ((size_t)(u / g.hkv % g.layers) * a.rows + row) * g.hkv + u % g.hkv;
+            const int step = a.per_unit ? 1 : g.hkv;
+#pragma unroll 4
             for (int j = lane; j < add; j += 32) {
                 const int pos = n0 + j, b = pos >> g.page_log2;
-                const int page = alloc && b >= have
-                                     ? a.ring[((long long)first + (b - have)) % g.pages]
-                                     : entry[b];
-                int slot = -1;
-                if (page >= 0 && page < g.pages)
-                    slot = (page << g.page_log2) + (pos & ((1 << g.page_log2) - 1));
-                else
-                    wrong = true;
-                const size_t at = a.per_unit ? (size_t)row + j
-                                             : ((size_t)l * a.rows + row + j) * g.hkv + h;
-                a.slots[at] = slot;
+                const int page = alloc && b >= have ? a.ring[wrapped((unsigned)first + (b - have), g.pages)]
+                                                    : entry[b];
+                const bool fine = page >= 0 && page < g.pages;
+                wrong |= !fine;
+                to[(size_t)j * step] =
+                    fine ? (page << g.page_log2) + (pos & ((1 << g.page_log2) - 1)) : -1;
             }
         }
         if (wrong) atomicCAS(err, 0, kCacheBadIndex);

@@ -1,14 +1,17 @@
-// Rows into the pages of the 8-bit cache and back.
+// Rows into the pages of the 8-bit cache and back: bound by their bytes, three
+// of every element of a row one way or the other.
 //
 // A run is the rows of one call that lie in one page one after the other.  A
-// block takes a run: its rows are read once into registers (4 x 16 bytes a
-// thread at most), their largest finite magnitude gives the page's scale, and
-// the codes leave as 8 bytes a thread.  A page that is appended to (the run
-// starts above row 0) keeps its scale unless the new rows need a larger one;
-// then its older rows are quantised again.  Blocks find their runs themselves:
-// a run belongs to the block whose window of tokens it starts in.
-#include <cfloat>
-
+// block takes a run of K or of V: its rows are read once, into registers (4 x
+// 16 bytes a thread at most), their largest finite magnitude gives the page's
+// scale, and the codes leave as 8 bytes a thread.  A page that is appended to
+// (the run starts above row 0) keeps its scale unless the new rows need a
+// larger one; then its older rows are quantised again.  Blocks find their runs
+// themselves: a run belongs to the block whose window of tokens it starts in,
+// and one pass over the window's slots and a page's beyond marks where runs
+// break.  The magnitudes are compared as 16-bit integers, two at a time; only
+// when the largest is an infinity or NaN are they gone through again without
+// such values.
 #include "cache.h"
 #include "cache_values.cuh"
 #include "common.cuh"
@@ -18,14 +21,35 @@ namespace {
 
 constexpr int kChunks = 4;  // 16-byte pieces of rows per thread
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    uint32_t m;
+    asm("max.u16x2 %0, %1, %2;\n" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+}
+
+// The larger of both halves, over the block.
+__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* s_max)
+{
+    m = max(m & 0xFFFFu, m >> 16);
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    const int warps = blockDim.x / 32;
+    if (warps == 1) return m;
+    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    return __reduce_max_sync(0xFFFFFFFFu, lane < warps ? s_max[lane] : 0);
+}
+
 template <int DTYPE, int FORMAT, int D>
 __global__ void __launch_bounds__(512)
 store_kernel(CacheGeom g, StoreArgs a, int window)
 {
-    __shared__ uint32_t s_start[4];  // bit i: a run starts at the window's token i
-    __shared__ int s_len;
-    __shared__ float s_max[16];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x;
+    constexpr uint32_t kInfinite = DTYPE == BACON_BF16 ? 0x7F80 : 0x7C00;
+    __shared__ uint32_t s_start[4];   // bit i: a run starts at the window's token i
+    __shared__ uint32_t s_break[9];   // bit i: no run goes on from token i - 1 to i
+    __shared__ uint32_t s_max[2][16];
+    const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
     const int h = blockIdx.y, which = blockIdx.z;
     const int p = g.page;
     const long long t0 = (long long)blockIdx.x * window;
@@ -34,88 +58,108 @@ store_kernel(CacheGeom g, StoreArgs a, int window)
     const long long stride = a.token_stride[which];
     uint8_t* const pool = which ? g.v : g.k;
     float* const scales = which ? g.v_scale : g.k_scale;
+    const int32_t* const slots = a.slots + h;
 
-    for (int base = 0; base < window; base += threads) {
+    for (int base = 0; base < window + p; base += threads) {
         const int i = base + tid;
         const long long t = t0 + i;
-        bool start = false;
-        if (i < window && t < a.tokens) {
-            const int s = a.slots[t * a.heads + h];
-            if (s < -1 || s >= limit) {
+        bool start = false, stop = true;
+        if (i < window + p && t < a.tokens) {
+            const int s = slots[t * a.heads], prev = t ? slots[(t - 1) * a.heads] : -1;
+            const bool on = (s & (p - 1)) != 0 && prev == s - 1;
+            if (s >= 0 && s < limit) {
+                stop = !on;
+                start = !on && i < window;
+            } else if (s != -1 && i < window) {
                 atomicCAS(g.err, 0, kCacheBadIndex);
-            } else if (s >= 0) {
-                const int prev = t ? a.slots[(t - 1) * a.heads + h] : -1;
-                start = (s & (p - 1)) == 0 || prev != s - 1;
             }
         }
-        const uint32_t bits = __ballot_sync(0xFFFFFFFFu, start);
-        if (lane == 0 && base + warp * 32 < window) s_start[(base >> 5) + warp] = bits;
+        const uint32_t starts = __ballot_sync(0xFFFFFFFFu, start);
+        const uint32_t stops = __ballot_sync(0xFFFFFFFFu, stop);
+        if (lane == 0) {
+            const int w = i >> 5;
+            if (w < 4) s_start[w] = starts;
+            if (w < 9) s_break[w] = stops;
+        }
     }
     __syncthreads();
 
-    for (int i = 0; i < window; ++i) {
-        if (!(s_start[i >> 5] >> (i & 31) & 1)) continue;
-        const long long t = t0 + i;
-        const int slot = a.slots[t * a.heads + h];
-        const int page = slot >> g.page_log2, off = slot & (p - 1);
-        __syncthreads();
-        if (tid == 0) s_len = p - off;
-        __syncthreads();
-        for (int j = tid; j < p - off; j += threads)
-            if (t + j >= a.tokens || a.slots[(t + j) * a.heads + h] != slot + j) atomicMin(&s_len, j);
-        __syncthreads();
-        const int len = s_len;
-        const float old = off ? scales[page] : 0.0f;
+    int parity = 0;
+    for (int word = 0; word * 32 < window; ++word) {
+        for (uint32_t left = s_start[word]; left; left &= left - 1) {
+            const int i = word * 32 + __ffs(left) - 1;
+            const long long t = t0 + i;
+            const int slot = slots[t * a.heads];
+            const int page = slot >> g.page_log2, off = slot & (p - 1);
+            // to the next break: within a page's tokens there is one, or the page ends
+            int len = p - off;
+            for (int w = i >> 5; w * 32 < i + len; ++w) {
+                uint32_t x = s_break[w];
+                if (w == i >> 5) x &= ~(2u << (i & 31)) + 1u;  // bits above i
+                if (x) {
+                    len = min(len, w * 32 + __ffs(x) - 1 - i);
+                    break;
+                }
+            }
+            const float old = off ? scales[page] : 0.0f;
 
-        uint4 raw[kChunks];
-        float amax = 0.0f;
+            uint4 raw[kChunks];
+            uint32_t most = 0;
 #pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
-            raw[c] = make_uint4(0, 0, 0, 0);
-            if (r < len) raw[c] = *reinterpret_cast<const uint4*>(rows + (t + r) * stride + q * 8);
-        }
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 v = unpack16<DTYPE>(w[j]);
-                const float x = fabsf(v.x), y = fabsf(v.y);
-                if (x <= FLT_MAX) amax = fmaxf(amax, x);
-                if (y <= FLT_MAX) amax = fmaxf(amax, y);
+            for (int c = 0; c < kChunks; ++c) {
+                const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
+                raw[c] = make_uint4(0, 0, 0, 0);
+                if (r < len) raw[c] = *reinterpret_cast<const uint4*>(rows + (t + r) * stride + q * 8);
             }
-        }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-        if (lane == 0) s_max[warp] = amax;
-        __syncthreads();
-        for (int w = 0; w < threads / 32; ++w) amax = fmaxf(amax, s_max[w]);
-        const float scale = fmaxf(old, scale_of<FORMAT>(amax));
-        const float inv = __fdiv_rn(1.0f, scale);
-        uint8_t* const dst = pool + ((size_t)page << g.page_log2) * D;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) {
-            const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
-            if (r >= len) continue;
-            const float2 v0 = unpack16<DTYPE>(raw[c].x), v1 = unpack16<DTYPE>(raw[c].y);
-            const float2 v2 = unpack16<DTYPE>(raw[c].z), v3 = unpack16<DTYPE>(raw[c].w);
-            uint2 code;
-            code.x = encode4<FORMAT>(make_float4(v0.x, v0.y, v1.x, v1.y), scale, inv);
-            code.y = encode4<FORMAT>(make_float4(v2.x, v2.y, v3.x, v3.y), scale, inv);
-            *reinterpret_cast<uint2*>(dst + (size_t)(off + r) * D + q * 8) = code;
-        }
-        if (off && scale > old)  // older rows of the page
-            for (int e = tid; e < off * D / 4; e += threads) {
-                uint32_t* const w = reinterpret_cast<uint32_t*>(dst) + e;
-                float4 x = codes_float<FORMAT>(*w);
-                x.x *= old;
-                x.y *= old;
-                x.z *= old;
-                x.w *= old;
-                *w = encode4<FORMAT>(x, scale, inv);
+            for (int c = 0; c < kChunks; ++c) {
+                const uint32_t x = max_u16x2(raw[c].x & 0x7FFF7FFFu, raw[c].y & 0x7FFF7FFFu);
+                const uint32_t y = max_u16x2(raw[c].z & 0x7FFF7FFFu, raw[c].w & 0x7FFF7FFFu);
+                most = max_u16x2(most, max_u16x2(x, y));
             }
-        if (tid == 0) scales[page] = scale;
+            most = block_max(most, s_max[parity]);
+            parity ^= 1;
+            if (most >= kInfinite) {
+                most = 0;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t lo = w[j] & 0x7FFFu, hi = w[j] >> 16 & 0x7FFFu;
+                        if (lo < kInfinite) most = max(most, lo);
+                        if (hi < kInfinite) most = max(most, hi);
+                    }
+                }
+                most = block_max(most, s_max[parity]);
+                parity ^= 1;
+            }
+            const float scale = fmaxf(old, scale_of<FORMAT>(unpack16<DTYPE>(most).x));
+            const float inv = __fdiv_rn(1.0f, scale);
+            uint8_t* const dst = pool + ((size_t)page << g.page_log2) * D;
+#pragma unroll
+            for (int c = 0; c < kChunks; ++c) {
+                const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
+                if (r >= len) continue;
+                const float2 v0 = unpack16<DTYPE>(raw[c].x), v1 = unpack16<DTYPE>(raw[c].y);
+                const float2 v2 = unpack16<DTYPE>(raw[c].z), v3 = unpack16<DTYPE>(raw[c].w);
+                uint2 code;
+                code.x = encode4<FORMAT>(make_float4(v0.x, v0.y, v1.x, v1.y), scale, inv);
+                code.y = encode4<FORMAT>(make_float4(v2.x, v2.y, v3.x, v3.y), scale, inv);
+                *reinterpret_cast<uint2*>(dst + (size_t)(off + r) * D + q * 8) = code;
+            }
+            if (off && scale > old)  // older rows of the page
+                for (int e = tid; e < off * D / 4; e += threads) {
+                    uint32_t* const w = reinterpret_cast<uint32_t*>(dst) + e;
+                    float4 x = codes_float<FORMAT>(*w);
+                    x.x *= old;
+                    x.y *= old;
+                    x.z *= old;
+                    x.w *= old;
+                    *w = encode4<FORMAT>(x, scale, inv);
+                }
+            if (tid == 0) scales[page] = scale;
+        }
     }
 }
 

@@ -62,21 +62,18 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
     // in total and before
     long long sum[4] = {0, 0, 0, 0};
     bool bad = false;
-#pragma unroll 4
+#pragma unroll 8
     for (int u = tid; u < a.units; u += kPlanThreads) {
         const int n = a.lengths ? a.lengths[u] : 0;
         const int m = a.per_unit ? a.added[u] : a.added ? a.added[u / lh] : 1;
-        if (n < 0 || n > most || m < 0 || m > most - n) {
-            bad = true;
-            continue;
-        }
-        const int need = blocks_of(n + m, g.page_log2) - blocks_of(n, g.page_log2);
+        const bool fine = n >= 0 && n <= most && m >= 0 && m <= most - n;
+        const int need = fine ? blocks_of(n + m, g.page_log2) - blocks_of(n, g.page_log2) : 0;
+        const int tokens = fine && a.per_unit ? m : 0;
+        bad |= !fine;
         sum[0] += need;
-        if (u < u0) sum[1] += need;
-        if (a.per_unit) {
-            sum[2] += m;
-            if (u < u0) sum[3] += m;
-        }
+        sum[1] += u < u0 ? need : 0;
+        sum[2] += tokens;
+        sum[3] += u < u0 ? tokens : 0;
     }
     if (!a.per_unit)
         for (int r = tid; r < a.requests; r += kPlanThreads) {

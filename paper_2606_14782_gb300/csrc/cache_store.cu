@@ -2,7 +2,7 @@
 // of every element of a row one way or the other.
 //
 // A run is the rows of one call that lie in one page one after the other.  A
-// block takes a run of K or of V: its rows are read once, into registers (4 x
+// block takes a run of K and V: its rows are read once, into registers (2 x 4 x
 // 16 bytes a thread at most), their largest finite magnitude gives the page's
 // scale, and the codes leave as 8 bytes a thread.  A page that is appended to
 // (the run starts above row 0) keeps its scale unless the new rows need a
@@ -28,17 +28,20 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
     return m;
 }
 
-// The larger of both halves, over the block.
-__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t* s_max)
+// The larger of both halves, over the block, for K's and for V's.
+__device__ __forceinline__ void block_max(uint32_t (&m)[2], uint32_t (*s_max)[2])
 {
-    m = max(m & 0xFFFFu, m >> 16);
-    m = __reduce_max_sync(0xFFFFFFFFu, m);
-    const int warps = blockDim.x / 32;
-    if (warps == 1) return m;
-    if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+    const int lane = threadIdx.x & 31, warps = blockDim.x / 32;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        m[z] = max(m[z] & 0xFFFFu, m[z] >> 16);
+        m[z] = __reduce_max_sync(0xFFFFFFFFu, m[z]);
+        if (warps > 1 && lane == 0) s_max[threadIdx.x >> 5][z] = m[z];
+    }
+    if (warps == 1) return;
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return __reduce_max_sync(0xFFFFFFFFu, lane < warps ? s_max[lane] : 0);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) m[z] = __reduce_max_sync(0xFFFFFFFFu, lane < warps ? s_max[lane][z] : 0);
 }
 
 template <int DTYPE, int FORMAT, int D>
@@ -48,16 +51,13 @@ store_kernel(CacheGeom g, StoreArgs a, int window)
     constexpr uint32_t kInfinite = DTYPE == BACON_BF16 ? 0x7F80 : 0x7C00;
     __shared__ uint32_t s_start[4];   // bit i: a run starts at the window's token i
     __shared__ uint32_t s_break[9];   // bit i: no run goes on from token i - 1 to i
-    __shared__ uint32_t s_max[2][16];
+    __shared__ uint32_t s_max[2][16][2];
     const int tid = threadIdx.x, lane = tid & 31, threads = blockDim.x;
-    const int h = blockIdx.y, which = blockIdx.z;
+    const int h = blockIdx.y;
     const int p = g.page;
     const long long t0 = (long long)blockIdx.x * window;
     const long long limit = (long long)g.pages << g.page_log2;
-    const uint16_t* const rows = a.rows[which] + h * a.head_stride[which];
-    const long long stride = a.token_stride[which];
-    uint8_t* const pool = which ? g.v : g.k;
-    float* const scales = which ? g.v_scale : g.k_scale;
+    const uint16_t* const rows[2] = {a.rows[0] + h * a.head_stride[0], a.rows[1] + h * a.head_stride[1]};
     const int32_t* const slots = a.slots + h;
 
     for (int base = 0; base < window + p; base += threads) {
@@ -101,95 +101,123 @@ store_kernel(CacheGeom g, StoreArgs a, int window)
                     break;
                 }
             }
-            const float old = off ? scales[page] : 0.0f;
+            const float old[2] = {off ? g.k_scale[page] : 0.0f, off ? g.v_scale[page] : 0.0f};
 
-            uint4 raw[kChunks];
-            uint32_t most = 0;
+            uint4 raw[2][kChunks];
+            uint32_t most[2] = {0, 0};
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
-                raw[c] = make_uint4(0, 0, 0, 0);
-                if (r < len) raw[c] = *reinterpret_cast<const uint4*>(rows + (t + r) * stride + q * 8);
-            }
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const uint32_t x = max_u16x2(raw[c].x & 0x7FFF7FFFu, raw[c].y & 0x7FFF7FFFu);
-                const uint32_t y = max_u16x2(raw[c].z & 0x7FFF7FFFu, raw[c].w & 0x7FFF7FFFu);
-                most = max_u16x2(most, max_u16x2(x, y));
-            }
-            most = block_max(most, s_max[parity]);
-            parity ^= 1;
-            if (most >= kInfinite) {
-                most = 0;
+            for (int z = 0; z < 2; ++z)
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
-                    const uint32_t w[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t lo = w[j] & 0x7FFFu, hi = w[j] >> 16 & 0x7FFFu;
-                        if (lo < kInfinite) most = max(most, lo);
-                        if (hi < kInfinite) most = max(most, hi);
-                    }
+                    const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
+                    raw[z][c] = make_uint4(0, 0, 0, 0);
+                    if (r < len)
+                        raw[z][c] = *reinterpret_cast<const uint4*>(rows[z] + (t + r) * a.token_stride[z] + q * 8);
                 }
-                most = block_max(most, s_max[parity]);
+#pragma unroll
+            for (int z = 0; z < 2; ++z)
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const uint4 w = raw[z][c];
+                    const uint32_t x = max_u16x2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu);
+                    const uint32_t y = max_u16x2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu);
+                    most[z] = max_u16x2(most[z], max_u16x2(x, y));
+                }
+            block_max(most, s_max[parity]);
+            parity ^= 1;
+            if (most[0] >= kInfinite || most[1] >= kInfinite) {
+                most[0] = most[1] = 0;
+#pragma unroll
+                for (int z = 0; z < 2; ++z)
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) {
+                        const uint32_t w[4] = {raw[z][c].x, raw[z][c].y, raw[z][c].z, raw[z][c].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t lo = w[j] & 0x7FFFu, hi = w[j] >> 16 & 0x7FFFu;
+                            if (lo < kInfinite) most[z] = max(most[z], lo);
+                            if (hi < kInfinite) most[z] = max(most[z], hi);
+                        }
+                    }
+                block_max(most, s_max[parity]);
                 parity ^= 1;
             }
-            const float scale = fmaxf(old, scale_of<FORMAT>(unpack16<DTYPE>(most).x));
-            const float inv = __fdiv_rn(1.0f, scale);
-            uint8_t* const dst = pool + ((size_t)page << g.page_log2) * D;
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
-                const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
-                if (r >= len) continue;
-                const float2 v0 = unpack16<DTYPE>(raw[c].x), v1 = unpack16<DTYPE>(raw[c].y);
-                const float2 v2 = unpack16<DTYPE>(raw[c].z), v3 = unpack16<DTYPE>(raw[c].w);
-                uint2 code;
-                code.x = encode4<FORMAT>(make_float4(v0.x, v0.y, v1.x, v1.y), scale, inv);
-                code.y = encode4<FORMAT>(make_float4(v2.x, v2.y, v3.x, v3.y), scale, inv);
-                *reinterpret_cast<uint2*>(dst + (size_t)(off + r) * D + q * 8) = code;
-            }
-            if (off && scale > old)  // older rows of the page
-                for (int e = tid; e < off * D / 4; e += threads) {
-                    uint32_t* const w = reinterpret_cast<uint32_t*>(dst) + e;
-                    float4 x = codes_float<FORMAT>(*w);
-                    x.x *= old;
-                    x.y *= old;
-                    x.z *= old;
-                    x.w *= old;
-                    *w = encode4<FORMAT>(x, scale, inv);
+            for (int z = 0; z < 2; ++z) {
+                const float scale = fmaxf(old[z], scale_of<FORMAT>(unpack16<DTYPE>(most[z]).x));
+                const float inv = __fdiv_rn(1.0f, scale);
+                uint8_t* const dst = (z ? g.v : g.k) + ((size_t)page << g.page_log2) * D;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
+                    if (r >= len) continue;
+                    const uint4 w = raw[z][c];
+                    const float2 v0 = unpack16<DTYPE>(w.x), v1 = unpack16<DTYPE>(w.y);
+                    const float2 v2 = unpack16<DTYPE>(w.z), v3 = unpack16<DTYPE>(w.w);
+                    uint2 code;
+                    code.x = encode4<FORMAT>(make_float4(v0.x, v0.y, v1.x, v1.y), scale, inv);
+                    code.y = encode4<FORMAT>(make_float4(v2.x, v2.y, v3.x, v3.y), scale, inv);
+                    *reinterpret_cast<uint2*>(dst + (size_t)(off + r) * D + q * 8) = code;
                 }
-            if (tid == 0) scales[page] = scale;
+                if (off && scale > old[z])  // older rows of the page
+                    for (int e = tid; e < off * D / 4; e += threads) {
+                        uint32_t* const w = reinterpret_cast<uint32_t*>(dst) + e;
+                        float4 x = codes_float<FORMAT>(*w);
+                        x.x *= old[z];
+                        x.y *= old[z];
+                        x.z *= old[z];
+                        x.w *= old[z];
+                        *w = encode4<FORMAT>(x, scale, inv);
+                    }
+                if (tid == 0) (z ? g.v_scale : g.k_scale)[page] = scale;
+            }
         }
     }
 }
 
+// Eight codes as values.
+template <int DTYPE, int FORMAT>
+__device__ __forceinline__ uint4 values_of(uint2 c, float s)
+{
+    const float4 x = codes_float<FORMAT>(c.x), y = codes_float<FORMAT>(c.y);
+    return make_uint4(pack16<DTYPE>(x.x * s, x.y * s), pack16<DTYPE>(x.z * s, x.w * s),
+                      pack16<DTYPE>(y.x * s, y.y * s), pack16<DTYPE>(y.z * s, y.w * s));
+}
+
+// A thread takes 8 values of K and the same of V (one slot's latency for both)
+// of two rows, so that a warp's stores are whole lines.
 template <int DTYPE, int FORMAT, int D>
 __global__ void __launch_bounds__(256)
 load_kernel(CacheGeom g, int rows, const int32_t* slots, uint16_t* k_out, uint16_t* v_out)
 {
-    const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
-    const long long i = e / (D / 16);
-    const int q = (int)(e % (D / 16));
-    if (i >= rows) return;
-    const int slot = slots[i];
-    uint4* const out = reinterpret_cast<uint4*>((blockIdx.y ? v_out : k_out) + i * D + q * 16);
-    if (slot < 0 || slot >= (long long)g.pages << g.page_log2) {
-        if (slot != -1) atomicCAS(g.err, 0, kCacheBadIndex);
-        out[0] = out[1] = make_uint4(0, 0, 0, 0);
-        return;
-    }
-    const float s = (blockIdx.y ? g.v_scale : g.k_scale)[slot >> g.page_log2];
-    const uint4 c = *reinterpret_cast<const uint4*>((blockIdx.y ? g.v : g.k) + (size_t)slot * D + q * 16);
-    const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    uint32_t o[8];
+    constexpr int kLanes = D / 8, kRows = 256 / kLanes;
+    const int q = threadIdx.x % kLanes;
+    const long long i0 = (long long)blockIdx.x * (2 * kRows) + threadIdx.x / kLanes;
+    int slot[2];
+    uint2 k[2], v[2];
+    float ks[2], vs[2];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const float4 x = codes_float<FORMAT>(w[j]);
-        o[2 * j] = pack16<DTYPE>(x.x * s, x.y * s);
-        o[2 * j + 1] = pack16<DTYPE>(x.z * s, x.w * s);
+    for (int z = 0; z < 2; ++z) slot[z] = i0 + z * kRows < rows ? slots[i0 + z * kRows] : -1;
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        k[z] = v[z] = make_uint2(0, 0);
+        ks[z] = vs[z] = 0.0f;
+        if (slot[z] >= 0 && slot[z] < (long long)g.pages << g.page_log2) {
+            k[z] = *reinterpret_cast<const uint2*>(g.k + (size_t)slot[z] * D + q * 8);
+            v[z] = *reinterpret_cast<const uint2*>(g.v + (size_t)slot[z] * D + q * 8);
+            ks[z] = g.k_scale[slot[z] >> g.page_log2];
+            vs[z] = g.v_scale[slot[z] >> g.page_log2];
+        } else if (slot[z] != -1) {
+            atomicCAS(g.err, 0, kCacheBadIndex);
+        }
     }
-    out[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    out[1] = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+        const long long i = i0 + z * kRows;
+        if (i >= rows) break;
+        *reinterpret_cast<uint4*>(k_out + i * D + q * 8) = values_of<DTYPE, FORMAT>(k[z], ks[z]);
+        *reinterpret_cast<uint4*>(v_out + i * D + q * 8) = values_of<DTYPE, FORMAT>(v[z], vs[z]);
+    }
 }
 
 // f(dtype, format, head_dim) with all three as constants
@@ -223,8 +251,8 @@ struct Load {
     static cudaError_t go(const CacheGeom& g, int rows, const int32_t* slots, void* k_out,
                           void* v_out, cudaStream_t st)
     {
-        const long long pieces = (long long)rows * (D / 16);
-        return launch_first(load_kernel<DTYPE, FORMAT, D>, dim3((unsigned)((pieces + 255) / 256), 2),
+        const int own = 2 * 256 / (D / 8);  // rows of a block
+        return launch_first(load_kernel<DTYPE, FORMAT, D>, (unsigned)((rows + own - 1LL) / own),
                             256, 0, st, g, rows, slots, static_cast<uint16_t*>(k_out),
                             static_cast<uint16_t*>(v_out));
     }
@@ -238,7 +266,7 @@ cudaError_t launch_cache_store(const CacheGeom& g, const StoreArgs& a, cudaStrea
     // ones when there are few, so that short runs do not queue in one block
     const long long per_block = (long long)a.tokens * a.heads / (152 * 8);
     int window = per_block < 1 ? 1 : per_block > g.page ? g.page : (int)per_block;
-    const dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads, 2);
+    const dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
     return by_type<Store>(g, a, grid, window, st);
 }
 

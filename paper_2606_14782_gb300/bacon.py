@@ -458,11 +458,14 @@ class State:
         return idx_out
 
 
+_i32 = torch.int32
+
+
 def _int32(t, shape, what):
     """The address of a contiguous int32 tensor of this shape on the GPU."""
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 cuda tensor of shape {tuple(shape)}")
-    return t.data_ptr()
+    if t.dtype is _i32 and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{what} must be a contiguous int32 cuda tensor of shape {tuple(shape)}")
 
 
 class Cache:
@@ -504,6 +507,13 @@ class Cache:
         h = _vp()
         _check(lib.bacon_cache_create(ctypes.byref(h), ctypes.byref(desc)))
         self.handle, self._lib = h, lib
+        # what every call needs, looked up once
+        self.device, self._index = self.k.device, self.k.device.index
+        self._unit, self._row = (layers, kv_heads), (layers, kv_heads, self.max_blocks)
+
+    def _stream(self, stream):
+        return (torch._C._cuda_getCurrentRawStream(self._index) if stream is None
+                else stream.cuda_stream)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -523,7 +533,7 @@ class Cache:
         self.close()
 
     def sync(self, stream=None):
-        _check(self._lib.bacon_cache_sync(self.handle, _stream_ptr(stream)))
+        _check(self._lib.bacon_cache_sync(self.handle, self._stream(stream)))
 
     def tables(self, requests):
         """(lengths, table, ring, state) of `requests` empty requests: every
@@ -544,56 +554,56 @@ class Cache:
         tokens in all.  The table gets the new pages; returns (slots,
         lengths_out, state_out)."""
         R = lengths.shape[0]
-        units = (R, self.layers, self.kv_heads)
+        units = (R,) + self._unit
         per_unit = added is not None and added.dim() == 3
+        shape = (rows,) if per_unit else (self.layers, rows, self.kv_heads)
+        p_lengths, p_state = _int32(lengths, units, "lengths"), _int32(state, (2,), "state")
         if slots is None:
-            slots = torch.empty((rows,) if per_unit else (self.layers, rows, self.kv_heads),
-                                dtype=torch.int32, device=lengths.device)
+            slots = torch.empty(shape, dtype=_i32, device=self.device)
         if lengths_out is None:
-            lengths_out = torch.empty_like(lengths)
+            lengths_out = torch.empty(units, dtype=_i32, device=self.device)
         if state_out is None:
-            state_out = torch.empty_like(state)
-        p_slots = _int32(slots, (rows,) if per_unit else (self.layers, rows, self.kv_heads),
-                         "slots")
+            state_out = torch.empty((2,), dtype=_i32, device=self.device)
         _check(self._lib.bacon_cache_plan(
-            self.handle, R, _int32(lengths, units, "lengths"),
+            self.handle, R, p_lengths,
             None if added is None else _int32(added, units if per_unit else (R,), "added"),
-            int(per_unit), _int32(table, units + (self.max_blocks,), "table"),
-            _int32(ring, (self.pages,), "ring"), _int32(state, (2,), "state"), rows,
-            p_slots, _int32(lengths_out, units, "lengths_out"),
-            _int32(state_out, (2,), "state_out"), _stream_ptr(stream)))
+            per_unit, _int32(table, (R,) + self._row, "table"),
+            _int32(ring, (self.pages,), "ring"), p_state, rows, _int32(slots, shape, "slots"),
+            _int32(lengths_out, units, "lengths_out"), _int32(state_out, (2,), "state_out"),
+            self._stream(stream)))
         return slots, lengths_out, state_out
 
     def locate(self, count, table, rows, first=None, slots=None, stream=None):
         """Slots [rows] of the positions [first, first + count) of each unit
         (first None: 0), the units one after the other; -1 beyond them."""
         R = count.shape[0]
-        units = (R, self.layers, self.kv_heads)
+        units = (R,) + self._unit
         if slots is None:
             slots = torch.empty((rows,), dtype=torch.int32, device=count.device)
         _check(self._lib.bacon_cache_locate(
             self.handle, R, None if first is None else _int32(first, units, "first"),
-            _int32(count, units, "count"), _int32(table, units + (self.max_blocks,), "table"),
-            rows, _int32(slots, (rows,), "slots"), _stream_ptr(stream)))
+            _int32(count, units, "count"), _int32(table, (R,) + self._row, "table"),
+            rows, _int32(slots, (rows,), "slots"), self._stream(stream)))
         return slots
 
     def release(self, done, lengths, table, ring, state, stream=None):
         """Gives the pages of the requests with done [R] != 0 back, in place."""
         R = lengths.shape[0]
-        units = (R, self.layers, self.kv_heads)
+        units = (R,) + self._unit
         _check(self._lib.bacon_cache_release(
             self.handle, R, _int32(done, (R,), "done"), _int32(lengths, units, "lengths"),
-            _int32(table, units + (self.max_blocks,), "table"),
+            _int32(table, (R,) + self._row, "table"),
             _int32(ring, (self.pages,), "ring"), _int32(state, (2,), "state"),
-            _stream_ptr(stream)))
+            self._stream(stream)))
 
     def _rows(self, t, what):
         """(address, token stride, head stride) of rows [T, H, d] or [T, d]."""
+        stride = t.stride()
         if (t.dtype is not self.dtype or not t.is_cuda or t.shape[-1] != self.head_dim
-                or t.dim() not in (2, 3) or t.stride(-1) != 1):
+                or len(stride) not in (2, 3) or stride[-1] != 1):
             raise ValueError(f"{what} must be {self.dtype} cuda rows of {self.head_dim} values, "
                              "[tokens, heads, d] or [tokens, d], the last dimension contiguous")
-        return t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0
+        return t.data_ptr(), stride[0], stride[1] if len(stride) == 3 else 0
 
     def store(self, k, v, slots, stream=None):
         """Rows k, v [T, H, d] (slots [T, H]) or [T, d] (slots [T]) into their
@@ -603,21 +613,21 @@ class Cache:
         kp, vp = self._rows(k, "k"), self._rows(v, "v")
         _check(self._lib.bacon_cache_store(
             self.handle, k.shape[0], k.shape[1] if k.dim() == 3 else 1, *kp, *vp,
-            _int32(slots, k.shape[:-1], "slots"), _stream_ptr(stream)))
+            _int32(slots, k.shape[:-1], "slots"), self._stream(stream)))
 
     def load(self, slots, k_out=None, v_out=None, stream=None):
         """The values of the slots' rows, shape [*slots.shape, d] each."""
         shape = slots.shape + (self.head_dim,)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=self.dtype, device=slots.device)
+            k_out = torch.empty(shape, dtype=self.dtype, device=self.device)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=self.dtype, device=slots.device)
+            v_out = torch.empty(shape, dtype=self.dtype, device=self.device)
         for t in (k_out, v_out):
             if t.shape != shape or t.dtype is not self.dtype or not t.is_contiguous():
                 raise ValueError(f"outputs must be contiguous {self.dtype} of shape {tuple(shape)}")
         _check(self._lib.bacon_cache_load(self.handle, slots.numel(),
                                           _int32(slots, slots.shape, "slots"), k_out.data_ptr(),
-                                          v_out.data_ptr(), _stream_ptr(stream)))
+                                          v_out.data_ptr(), self._stream(stream)))
         return k_out, v_out
 
     def attend(self, layer, q, lengths, table, starts=None, causal=True, scale=None, out=None,
@@ -626,24 +636,23 @@ class Cache:
         (already stored) over their units.  starts [R + 1] int32: where each
         request's queries begin; None: T / R each.  Returns out [T, q_heads,
         d], with lse=True (or a tensor) also the log-sum-exp [T, q_heads]."""
-        R, T = lengths.shape[0], q.shape[0]
-        units = (R, self.layers, self.kv_heads)
-        if q.dim() != 3 or q.shape[1] != self.q_heads:
+        R, shape = lengths.shape[0], q.shape
+        if len(shape) != 3 or shape[1] != self.q_heads:
             raise ValueError(f"q must be [tokens, {self.q_heads}, {self.head_dim}]")
         qp = self._rows(q, "q")
         if out is None:
-            out = torch.empty((T, self.q_heads, self.head_dim), dtype=self.dtype, device=q.device)
-        elif out.shape != q.shape or out.dtype is not self.dtype or not out.is_contiguous():
+            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+        elif out.shape != shape or out.dtype is not self.dtype or not out.is_contiguous():
             raise ValueError("out must be contiguous and of q's shape and type")
         if lse is True:
-            lse = torch.empty((T, self.q_heads), dtype=torch.float32, device=q.device)
-        elif lse is not None and (lse.shape != q.shape[:2] or lse.dtype is not torch.float32
+            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+        elif lse is not None and (lse.shape != shape[:2] or lse.dtype is not torch.float32
                                   or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [tokens, q_heads]")
         _check(self._lib.bacon_cache_attend(
-            self.handle, R, layer, T, *qp,
+            self.handle, R, layer, shape[0], *qp,
             None if starts is None else _int32(starts, (R + 1,), "starts"),
-            _int32(lengths, units, "lengths"),
-            _int32(table, units + (self.max_blocks,), "table"), int(causal),
-            0.0 if scale is None else scale, out.data_ptr(), _ptr(lse), _stream_ptr(stream)))
+            _int32(lengths, (R,) + self._unit, "lengths"),
+            _int32(table, (R,) + self._row, "table"), bool(causal),
+            0.0 if scale is None else scale, out.data_ptr(), _ptr(lse), self._stream(stream)))
         return out if lse is None else (out, lse)

@@ -76,7 +76,7 @@ struct SplitScratch {
     float* out;    // [2 sms kBlocksPerSm][32 columns][128]
     float* sums;   // [2 sms kBlocksPerSm][32 columns][maximum, sum]
     int* arrived;  // [sms kBlocksPerSm] parts that are there, 0 between calls
-    float* many_out;    // [2 sms][2 row tiles][128 dims][128 rows]
+    float* many_out;    // [2 sms][2 row tiles][32 quads of dims][128 rows][4]
     float2* many_sums;  // [2 sms][2][128] maximum, sum
     int* many_arrived;  // [sms][2]
 };

@@ -511,6 +511,12 @@ __device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot
     }
 }
 
+// Four dims of a row of a part, rows side by side.
+__device__ __forceinline__ float4& part_of(const SplitScratch& sc, size_t slot, int quad, int row)
+{
+    return reinterpret_cast<float4*>(sc.many_out)[slot * 32 + quad * kHalf + row];
+}
+
 // 32 columns of a row of O, column 16 c + 8 o + n being dim 16 c + 2 n + o, as
 // the output's values.
 __device__ __forceinline__ void store_row(uint16_t* dst, const float* v, float scale, bool some, int dtype)
@@ -548,6 +554,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             const int j = (int)(c / g.group), head = it.h * g.group + (int)(c % g.group);
             const bool mine = j < it.asked;
             const int sees = mine ? seen_by(a, it.n, it.asked, j) : 0;
+            const bool live = __any_sync(0xFFFFFFFFu, mine);  // else the warp only keeps time
             const int all = seen_by(a, it.n, it.asked, (it.block * kRows + m * kHalf) / g.group);
             // the rows' queries as fp16, each scaled into its range: D / 8
             // lanes a row
@@ -561,17 +568,17 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 // (a rolled loop: straight-line code that runs once an item
                 // costs more in instruction fetches than it does)
 #pragma unroll 1
-                for (int i0 = 0; i0 < kLanes; i0 += 4) {
-                    uint4 raw[4];
+                for (int i0 = 0; i0 < kLanes; i0 += 8) {
+                    uint4 raw[8];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         const long long from =
                             __shfl_sync(0xFFFFFFFFu, offset, (i0 + i) * kAtOnce + lane / kLanes);
                         raw[i] = make_uint4(0, 0, 0, 0);
                         if (from >= 0) raw[i] = *reinterpret_cast<const uint4*>(a.q + from + piece * 8);
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 8; ++i) {
                         const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
                         float2 v[4];
                         float amax = 0.0f;
@@ -616,7 +623,9 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 fence_after_sync();
                 const bool cut = (i + 1) * kTile > all;
                 const int left = sees - i * kTile;  // positions of the tile that the row sees
-                if (cut)
+                if (!live) {
+                    if (lane < 2) mbar_arrive(bar(sh.p_full[m][lane]));
+                } else if (cut)
                     softmax_tile<D, true>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
                 else
                     softmax_tile<D, false>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
@@ -634,7 +643,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             const size_t slot = ((2 * (size_t)b + (begin == 0 ? 1 : 0)) * 2 + m) * kHalf;
             const float inv = sees > 0 ? 1.0f / sum : 0.0f;
 #pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
+            for (int q = 0; live && q < D / 32; ++q) {
                 float v[32];
                 tmem_ld32(out + q * 32, v);
                 tmem_ld_wait_regs32(v);
@@ -645,7 +654,8 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 }
                 if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) sc.many_out[slot * 128 + (q * 32 + e) * kHalf + row] = v[e];
+                    for (int e = 0; e < 32; e += 4)
+                        part_of(sc, slot, q * 8 + e / 4, row) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                 } else if (mine) {
                     store_row(dst + q * 32, v, inv, sees > 0, g.dtype);
                 }
@@ -663,27 +673,44 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 if (sh.last[m]) {
                     auto part = [&](int q) { return ((2 * (size_t)(first + q) + (q == 0 ? 1 : 0)) * 2 + m) * kHalf; };
                     float high = -INFINITY, total = 0.0f;
+#pragma unroll 8
                     for (int q = 0; q < parts; ++q) high = fmaxf(high, __ldcg(&sc.many_sums[part(q) + row]).x);
+#pragma unroll 8
                     for (int q = 0; q < parts; ++q) {
                         const float2 z = __ldcg(&sc.many_sums[part(q) + row]);
                         total += z.y * (z.x == -INFINITY ? 0.0f : fast_exp2(z.x - high));
                     }
                     const float scale = sees > 0 ? 1.0f / total : 0.0f;
+                    // 32 dims at a time, out of four parts at a time
 #pragma unroll 1
-                    for (int d = 0; d < D / 32; ++d) {
+                    for (int d = 0; live && d < D / 32; ++d) {
                         float v[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.0f;
-#pragma unroll 2
-                        for (int q = 0; q < parts; ++q) {
-                            const float z = __ldcg(&sc.many_sums[part(q) + row]).x;
-                            const float f = z == -INFINITY ? 0.0f : fast_exp2(z - high);
-                            const float* const o = sc.many_out + part(q) * 128 + d * 32 * kHalf + row;
-                            float x[32];
+#pragma unroll 1
+                        for (int q0 = 0; q0 < parts; q0 += 4) {
+                            float f[4];
+                            float4 x[4][8];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) x[e] = __ldcg(&o[e * kHalf]);
+                            for (int z = 0; z < 4; ++z) {
+                                const bool there = q0 + z < parts;
+                                f[z] = there ? __ldcg(&sc.many_sums[part(q0 + z) + row]).x : -INFINITY;
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = fmaf(x[e], f, v[e]);
+                                for (int e = 0; e < 8; ++e)
+                                    x[z][e] = there ? __ldcg(&part_of(sc, part(q0 + z), d * 8 + e, row))
+                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            }
+#pragma unroll
+                            for (int z = 0; z < 4; ++z) {
+                                const float w = f[z] == -INFINITY ? 0.0f : fast_exp2(f[z] - high);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    v[4 * e] = fmaf(x[z][e].x, w, v[4 * e]);
+                                    v[4 * e + 1] = fmaf(x[z][e].y, w, v[4 * e + 1]);
+                                    v[4 * e + 2] = fmaf(x[z][e].z, w, v[4 * e + 2]);
+                                    v[4 * e + 3] = fmaf(x[z][e].w, w, v[4 * e + 3]);
+                                }
+                            }
                         }
                         if (mine) store_row(dst + d * 32, v, scale, sees > 0, g.dtype);
                     }

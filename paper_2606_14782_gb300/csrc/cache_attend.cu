@@ -76,7 +76,7 @@ struct Shared {
     Segment seg[2];
     long long scan[9];
     Found found;
-    int abort, last;
+    int abort, last, quit;
     int nan_at[128];  // per dim: first position of a NaN of V that not every column sees
     int nan_any;
 };
@@ -280,11 +280,14 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     int items = 0;
     for (long long t = lo; t < hi; ++items) {
         const int slot = items & 1;
-        if (!mbar_wait(smem_u32(&sh.q_full[slot]), items >> 1 & 1, abort_flag) && lane == 0) {
+        const bool there = mbar_wait(smem_u32(&sh.q_full[slot]), items >> 1 & 1, abort_flag);
+        if (!there && lane == 0) {
             st_shared_volatile(abort_flag, 1);
             atomicCAS(g.err, 0, kCacheTimeout);
         }
-        __syncwarp();
+        if (tid == 0) sh.quit = !there;
+        named_barrier_sync(1, 32 * kWarps);
+        if (sh.quit) return;  // the same for all that compute
         const Segment seg = sh.seg[slot];
         const Item& it = seg.it;
         // the item's queries as fragments: column g of an n-tile, dims 16 c +
@@ -548,8 +551,8 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
         if (whole) {
             if (group == 0) write(Count<kChunks>{}, acc, 0);
         } else {
-            const int first = place.owner_of(seg.at);
-            const int parts = place.owner_of(seg.at + it.tiles - 1) - first + 1;
+            int first, parts;
+            place.parts_of(seg.at, it.tiles, first, parts);
             // of a part: a column group's outputs as its warp holds them, then
             // the columns' maxima and sums
             const int mine = warp / kGroups * kChunks * NT * 32 + lane;

@@ -238,27 +238,32 @@ __device__ __forceinline__ long long quotient(long long x, long long y)
     return (x | y) >> 32 ? x / y : (long long)((unsigned)x / (unsigned)y);
 }
 
-// Tiles [lo, hi) of the call's `total`, all items' one after the other, are
-// this block's, one of `blocks`; the first of them is in the item that `Found`
-// has, one of unit `unit` whose first tile is `at`.
+// What a block does: tiles [lo, hi), counted so that the first of them lies in
+// the item that `Found` has, one of unit `unit` whose first tile is `at`.
+//
+// Dealt evenly, the tiles of all items stand one after the other and block b
+// has the b-th share, wherever items end.  A block whose tiles lie in two items
+// forms and joins sums twice, which a few tiles do not pay for: a call with
+// few items and few tiles gives each item blocks of its own, `run` tiles each.
 struct Place {
     long long total, lo, hi, at;
     long long share;  // tiles of a block; the first `more` blocks have one more
     int blocks, more, unit;
+    int run;          // > 0: blocks of their own
+    int first, parts; // and then the first of them and their number
 
-    __device__ __forceinline__ void deal(int least, int grid)
-    {
-        const long long most = quotient(total + least - 1, least);
-        blocks = most < grid ? (int)most : grid;
-        share = blocks ? quotient(total, blocks) : 0;
-        more = (int)(total - share * blocks);
-    }
     __device__ __forceinline__ long long first_tile(int b) const { return share * b + min(b, more); }
     __device__ __forceinline__ int owner_of(long long tile) const
     {
         const long long long_ones = (share + 1) * more;
         return tile < long_ones ? (int)quotient(tile, share + 1)
                                 : more + (int)quotient(tile - long_ones, share);
+    }
+    // the blocks of a cut item whose first tile is `item_at`
+    __device__ __forceinline__ void parts_of(long long item_at, int tiles, int& from, int& count) const
+    {
+        from = run ? first : owner_of(item_at);
+        count = run ? parts : owner_of(item_at + tiles - 1) - from + 1;
     }
 };
 struct Found {
@@ -267,8 +272,7 @@ struct Found {
     int unit;
 };
 
-// Scan of the items' tiles by the whole block; false when it has none.  A block
-// gets about LEAST tiles at least: fewer parts to join.
+// Finds the block's place by a scan of all items; false when it has none.
 //
 // An entry is an item when all requests have the same number of queries, else
 // a unit with all its items.  Each warp takes a run of entries, a lane an
@@ -289,6 +293,26 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
     const unsigned e0 = warp * run + lane, e1 = min(entries, (warp + 1) * run);
     bool bad = blockIdx.x == 0 && starts_are_bad(a, threadIdx.x, THREADS);
 
+    // one item a unit, which sees all its tokens: only lengths are needed, on
+    // their way together and kept
+    const bool short_run = same && each == 1 && run <= 256;
+    int n[8];
+    if (short_run) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const unsigned e = e0 + i * 32, r = e / (unsigned)g.hkv;
+            n[i] = -1;
+            if (e < e1) n[i] = a.lengths[((size_t)r * g.layers + a.layer) * g.hkv + (e - r * g.hkv)];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (e0 + i * 32 < e1 && (n[i] < 0 || n[i] > (long long)g.max_blocks << g.page_log2)) {
+                bad = true;
+                n[i] = 0;
+            }
+    }
+    auto tiles_of_unit = [](int x) { return max(1, (int)(((unsigned)x + TILE - 1) / TILE)); };
+
     // entry e as its first item, the number of its items in `items`
     auto entry = [&](unsigned e, int& unit, int& items) {
         Item it;
@@ -308,64 +332,77 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
         set_block<ROWS, TILE>(g, a, it, block);
         return it;
     };
-    // tiles of all of an entry's items
-    auto tiles_of = [&](Item it, int items) {
-        long long sum = items ? it.tiles : 0;
-        for (int i = 1; i < items; ++i) {
-            set_block<ROWS, TILE>(g, a, it, i);
-            sum += it.tiles;
+    // runs of `by` tiles of all of an entry's items
+    auto runs_of = [&](Item it, int items, int by) {
+        long long sum = 0;
+        for (int i = 0; i < items; ++i) {
+            if (i) set_block<ROWS, TILE>(g, a, it, i);
+            sum += by == 1 ? it.tiles : (unsigned)(it.tiles + by - 1) / (unsigned)by;
         }
         return sum;
     };
-    long long mine = 0;
-    // one item a unit, which sees all its tokens: only lengths are needed, on
-    // their way together and kept
-    const bool short_run = same && each == 1 && run <= 256;
-    int n[8];
-    auto tiles_of_unit = [](int x) { return max(1, (int)(((unsigned)x + TILE - 1) / TILE)); };
-    if (short_run) {
+    // the sum of them over all entries, that of the warps before in `before`
+    long long mine, before = 0;
+    auto sum_of = [&](int by) {
+        mine = 0;
+        if (short_run) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const unsigned e = e0 + i * 32, r = e / (unsigned)g.hkv;
-            n[i] = -1;
-            if (e < e1) n[i] = a.lengths[((size_t)r * g.layers + a.layer) * g.hkv + (e - r * g.hkv)];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (e0 + i * 32 < e1) {
-                if (n[i] < 0 || n[i] > (long long)g.max_blocks << g.page_log2) {
-                    bad = true;
-                    n[i] = 0;
+            for (int i = 0; i < 8; ++i)
+                if (n[i] >= 0) {
+                    const int tiles = tiles_of_unit(n[i]);
+                    mine += by == 1 ? tiles : (unsigned)(tiles + by - 1) / (unsigned)by;
                 }
-                mine += tiles_of_unit(n[i]);
+        } else {
+            for (unsigned e = e0; e < e1; e += 32) {
+                int unit, items;
+                const Item it = entry(e, unit, items);
+                mine += runs_of(it, items, by);
             }
-    } else {
-        for (unsigned e = e0; e < e1; e += 32) {
-            int unit, items;
-            const Item it = entry(e, unit, items);
-            mine += tiles_of(it, items);
         }
-    }
-    if (bad) atomicCAS(g.err, 0, kCacheBadIndex);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
-    if (lane == 0) scan[warp] = mine;
-    __syncthreads();
-    long long before = 0;
-    p.total = 0;
-    for (int w = 0; w < kWarps; ++w) {
-        if (w == warp) before = p.total;
-        p.total += scan[w];
+        for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, o);
+        if (lane == 0) scan[warp] = mine;
+        __syncthreads();
+        long long all = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w == warp) before = all;
+            all += scan[w];
+        }
+        return all;
+    };
+    p.total = sum_of(1);
+    if (bad) atomicCAS(g.err, 0, kCacheBadIndex);
+    // requests with other numbers of queries: no more items than this
+    const long long items = same ? (long long)entries
+                                 : ((long long)a.tokens * g.group / ROWS + a.requests) * g.hkv;
+    const int grid = gridDim.x, b = blockIdx.x;
+    p.run = 0;
+    if (items * 4 <= grid && p.total <= 16LL * grid) {
+        // at most total / run + items blocks
+        p.run = max(LEAST, (int)((unsigned)(p.total + grid - items - 1) / (unsigned)(grid - items)));
+        p.blocks = (int)p.total;
+        if (p.run > 1) {
+            __syncthreads();
+            p.blocks = (int)sum_of(p.run);
+        }
+    } else {
+        p.blocks = p.total < grid ? (int)p.total : grid;
+        p.share = p.blocks ? quotient(p.total, p.blocks) : 0;
+        p.more = (int)(p.total - p.share * p.blocks);
     }
-    p.deal(LEAST, gridDim.x);
-    if ((int)blockIdx.x >= p.blocks) return false;
-    p.lo = p.first_tile(blockIdx.x);
-    p.hi = p.first_tile(blockIdx.x + 1);
-    const bool has = p.lo >= before && p.lo < before + mine;
+    if (b >= p.blocks) return false;
+    if (!p.run) {
+        p.lo = p.first_tile(b);
+        p.hi = p.first_tile(b + 1);
+    }
+    const int by = max(p.run, 1);
+    const long long target = p.run ? b : p.lo;
+    const bool has = target >= before && target < before + mine;
     if (has && short_run) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int own = n[i] < 0 ? 0 : tiles_of_unit(n[i]);
+            const int tiles = n[i] < 0 ? 0 : tiles_of_unit(n[i]);
+            const int own = by == 1 ? tiles : (unsigned)(tiles + by - 1) / (unsigned)by;
             int x = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -373,8 +410,8 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
                 if (lane >= o) x += y;
             }
             const int all = __shfl_sync(0xFFFFFFFFu, x, 31);
-            if (p.lo < before + all) {
-                if (before + x - own <= p.lo && p.lo < before + x) {
+            if (target < before + all) {
+                if (before + x - own <= target && target < before + x) {
                     Item it;
                     const int unit = (int)(e0 + i * 32);
                     it.r = (unsigned)unit / (unsigned)g.hkv;
@@ -383,7 +420,7 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
                     it.n = it.seen = n[i];
                     it.asked = q.asked;
                     it.start = it.r * q.asked;
-                    it.tiles = own;
+                    it.tiles = tiles;
                     found = Found{it, before + x - own, unit};
                 }
                 break;
@@ -392,12 +429,12 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
         }
     } else if (has) {
         for (unsigned e = e0;; e += 32) {
-            int unit = 0, items = 0;
+            int unit = 0, count_of = 0;
             Item it;
             long long own = 0;
             if (e < e1) {
-                it = entry(e, unit, items);
-                own = tiles_of(it, items);
+                it = entry(e, unit, count_of);
+                own = runs_of(it, count_of, by);
             }
             long long x = own;
 #pragma unroll
@@ -406,11 +443,11 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
                 if (lane >= o) x += y;
             }
             const long long all = __shfl_sync(0xFFFFFFFFu, x, 31);
-            if (p.lo < before + all) {
+            if (target < before + all) {
                 long long at = before + x - own;
-                if (at <= p.lo && p.lo < at + own) {
-                    for (int i = 1; p.lo >= at + it.tiles; ++i) {
-                        at += it.tiles;
+                if (at <= target && target < at + own) {
+                    for (int i = 1; target >= at + (it.tiles + by - 1) / by; ++i) {
+                        at += (it.tiles + by - 1) / by;
                         set_block<ROWS, TILE>(g, a, it, i);
                     }
                     found = Found{it, at, unit};
@@ -423,6 +460,14 @@ __device__ __forceinline__ bool find_place(const CacheGeom& g, const AttendArgs&
     __syncthreads();
     p.at = found.at;
     p.unit = found.unit;
+    if (p.run) {
+        const int k = b - (int)found.at, tiles = found.it.tiles;
+        p.first = (int)found.at;
+        p.parts = (tiles + by - 1) / by;
+        p.at = 0;
+        p.lo = (long long)k * by;
+        p.hi = min((long long)tiles, p.lo + by);
+    }
     return true;
 }
 

@@ -58,19 +58,30 @@ struct Smem {
     static constexpr int kBytes = kShared + 3072;
 };
 
+// Tiles [begin, end) of an item, whose first tile is tile `at` of the call.
+struct Segment {
+    Item it;
+    int begin, end;
+    long long at;
+};
+// The loads are at most this many items ahead of the outputs.
+constexpr int kItems = 2;
+
 template <int D>
 struct Shared {
     float k_scale[4][kGroups], v_log2[4][kGroups], v_inv[4][kGroups];
     uint64_t rawk_full, rawk_empty, rawv_full, rawv_empty;
     uint64_t key_full[2], key_empty[2], value_full[2], value_empty[2];
     uint64_t s_full[2], p_full[2][2], o_full[2], q_full[2];
-    uint64_t meta_full[4], item_done[4], drain;
+    uint64_t meta_full[4], item_full[kItems], item_done[kItems], drain;
+    Segment seg[kItems];
     long long scan[kThreads / 32];
     Found found;
+    Place place;
     uint32_t tmem;
-    int abort, last[2];
-    int nan_any[4];
-    int nan_at[4][D];  // of an item, per dim: first position of a NaN of V that not every row sees
+    int abort, last[2], quit[2];
+    int nan_any[kItems];
+    int nan_at[kItems][D];  // of an item, per dim: first position of a NaN of V that not every row sees
 };
 static_assert(sizeof(Shared<128>) <= 3072, "shared record");
 
@@ -108,7 +119,9 @@ __device__ __forceinline__ void give_up(Shared<D>& sh, int* err)
 }
 
 // Bounded wait of a role's thread: one that runs out raises the abort flag, at
-// which every other wait ends at once and the roles run through to their ends.
+// which every other wait ends at once.  The roles then run through the item
+// that they have (a warpgroup's named barriers need all its warps) and leave
+// before the next.
 template <int D>
 __device__ __forceinline__ bool wait(Shared<D>& sh, uint32_t b, uint32_t parity, int* err)
 {
@@ -133,12 +146,18 @@ __device__ __forceinline__ void load(const CUtensorMap* kmap, const CUtensorMap*
     long long at = p.at, t = p.lo;
     uint32_t seq = 0;
     while (t < p.hi && ok) {
-        if (k >= 4) ok = wait(sh, bar(sh.item_done[k & 3]), (k >> 2 & 1) ^ 1, g.err);
-        for (int i = lane; i < D; i += 32) sh.nan_at[k & 3][i] = 0x7FFFFFFF;
-        if (lane == 0) sh.nan_any[k & 3] = 0;
+        ok = wait(sh, bar(sh.item_done[k % kItems]), (k / kItems & 1) ^ 1, g.err);
+        if (!ok) break;
+        for (int i = lane; i < D; i += 32) sh.nan_at[k % kItems][i] = 0x7FFFFFFF;
+        const int end = (int)min((long long)it.tiles, p.hi - at);
+        if (lane == 0) {
+            sh.nan_any[k % kItems] = 0;
+            sh.seg[k % kItems] = Segment{it, (int)(t - at), end, at};
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.item_full[k % kItems]));
         const int32_t* const table =
             a.table + (((size_t)it.r * g.layers + a.layer) * g.hkv + it.h) * g.max_blocks;
-        const int end = (int)min((long long)it.tiles, p.hi - at);
         for (int i = (int)(t - at); i < end && ok; ++i, ++t, ++seq) {
             const int pos = i * kTile + group * 16;
             const bool live = lane < 16 && pos < it.seen;
@@ -205,8 +224,9 @@ __device__ __forceinline__ void convert_keys(const CacheGeom& g, const Place& p,
     const uint32_t tiles = (uint32_t)(p.hi - p.lo);
     for (uint32_t seq = 0; seq < tiles; ++seq) {
         const int buf = seq & 1;
-        wait(sh, bar(sh.rawk_full), seq & 1, g.err);
-        wait(sh, bar(sh.key_empty[buf]), (seq >> 1 & 1) ^ 1, g.err);
+        if (!wait(sh, bar(sh.rawk_full), seq & 1, g.err) ||
+            !wait(sh, bar(sh.key_empty[buf]), (seq >> 1 & 1) ^ 1, g.err))
+            return;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int row = warp * 64 + half * 32 + lane;
@@ -281,9 +301,9 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
                         for (int e = 0; e < 4; ++e)
                             if ((w[c][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
                                 w[c][m] &= ~(0xFFu << (8 * e));
-                                atomicMin(&sh.nan_at[item & 3][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
+                                atomicMin(&sh.nan_at[item % kItems][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
                                           x0 + (e >> 1));
-                                sh.nan_any[item & 3] = 1;
+                                sh.nan_any[item % kItems] = 1;
                             }
                     }
                 }
@@ -303,21 +323,22 @@ __device__ __forceinline__ void convert_values(const CacheGeom& g, const AttendA
                                                Shared<D>& sh, uint32_t base)
 {
     const int lane = threadIdx.x & 31;
-    int unit = p.unit, k = 0;
-    Item it = sh.found.it;
-    long long at = p.at, t = p.lo;
+    const uint32_t tiles = (uint32_t)(p.hi - p.lo);
     uint32_t seq = 0;
-    while (t < p.hi) {
-        const int all = seen_by(a, it.n, it.asked, it.block * kRows / g.group);
-        const int end = (int)min((long long)it.tiles, p.hi - at);
-        for (int i = (int)(t - at); i < end; ++i, ++t, ++seq) {
+    for (int k = 0; seq < tiles; ++k) {
+        if (!wait(sh, bar(sh.item_full[k % kItems]), k / kItems & 1, g.err)) return;
+        const Segment& seg = sh.seg[k % kItems];
+        const int all = seen_by(a, seg.it.n, seg.it.asked, seg.it.block * kRows / g.group);
+        const int end = seg.end, seen = seg.it.seen;
+        for (int i = seg.begin; i < end; ++i, ++seq) {
             const int buf = seq & 1;
-            wait(sh, bar(sh.rawv_full), seq & 1, g.err);
-            wait(sh, bar(sh.value_empty[buf]), (seq >> 1 & 1) ^ 1, g.err);
+            if (!wait(sh, bar(sh.rawv_full), seq & 1, g.err) ||
+                !wait(sh, bar(sh.value_empty[buf]), (seq >> 1 & 1) ^ 1, g.err))
+                return;
             if ((i + 1) * kTile > all)
-                convert_value_tile<FORMAT, D, true>(sh, base, buf, i * kTile, it.seen, k);
+                convert_value_tile<FORMAT, D, true>(sh, base, buf, i * kTile, seen, k);
             else
-                convert_value_tile<FORMAT, D, false>(sh, base, buf, i * kTile, it.seen, k);
+                convert_value_tile<FORMAT, D, false>(sh, base, buf, i * kTile, seen, k);
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -325,9 +346,6 @@ __device__ __forceinline__ void convert_values(const CacheGeom& g, const AttendA
                 mbar_arrive(bar(sh.rawv_empty));
             }
         }
-        at += it.tiles;
-        ++k;
-        if (t < p.hi && !next_item<kRows, kTile>(g, a, unit, it)) break;
     }
 }
 
@@ -340,18 +358,15 @@ __device__ __forceinline__ int halves_of(const CacheGeom& g, const Item& it)
 }
 
 template <int D>
-__device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, const Place& p,
-                                      Shared<D>& sh, uint32_t base)
+__device__ __forceinline__ void issue(const CacheGeom& g, const Place& p, Shared<D>& sh, uint32_t base)
 {
     using S = Smem<D>;
     const bool leader = elect_one();
     const uint32_t tmem = __shfl_sync(0xFFFFFFFFu, ld_shared(smem_u32(&sh.tmem)), 0);
     constexpr uint32_t hi = sdesc_hi(1024u);
     const uint32_t q_lo = sdesc_lo(base), k_lo = sdesc_lo(base + S::kKeys), v_lo = sdesc_lo(base + S::kValues);
-    int unit = p.unit;
     bool ok = true;
-    Item it = sh.found.it;
-    long long at = p.at, t = p.lo;
+    const uint32_t every = (uint32_t)(p.hi - p.lo);
     uint32_t seq = 0, q_phase[2] = {0, 0}, p_phase[2] = {0, 0};
 
     auto scores = [&](int m, uint32_t s) {
@@ -365,9 +380,11 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
             umma_commit(bar(sh.s_full[m]));
         }
     };
-    while (t < p.hi && ok) {
-        const int halves = halves_of(g, it);
-        const int tiles = (int)(min((long long)it.tiles, p.hi - at) - (t - at));
+    for (int k = 0; seq < every && ok; ++k) {
+        ok = wait(sh, bar(sh.item_full[k % kItems]), k / kItems & 1, g.err);
+        if (!ok) break;
+        const Segment& seg = sh.seg[k % kItems];
+        const int halves = halves_of(g, seg.it), tiles = seg.end - seg.begin;
         for (int m = 0; m < halves && ok; ++m) {
             ok = wait(sh, bar(sh.q_full[m]), q_phase[m], g.err);
             q_phase[m] ^= 1;
@@ -408,9 +425,6 @@ __device__ __forceinline__ void issue(const CacheGeom& g, const AttendArgs& a, c
                 }
             }
         }
-        t += tiles;
-        at += it.tiles;
-        if (t < p.hi && ok && !next_item<kRows, kTile>(g, a, unit, it)) break;
     }
     // every product issued ends before tensor memory is given back
     if (leader) {
@@ -542,13 +556,17 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lanes = ld_shared(smem_u32(&sh.tmem)) + ((uint32_t)(warp & 3) << 21);
     const uint32_t logits = lanes + m * 128, out = lanes + 256 + m * 128;
-    int unit = p.unit, k = 0;
-    Item it = sh.found.it;
-    long long at = p.at, t = p.lo;
+    const uint32_t tiles = (uint32_t)(p.hi - p.lo);
     uint32_t seq = 0, s_phase = 0, o_phase = 0;
 
-    while (t < p.hi) {
-        const int begin = (int)(t - at), end = (int)min((long long)it.tiles, p.hi - at);
+    for (int k = 0; seq < tiles; ++k) {
+        const bool there = wait(sh, bar(sh.item_full[k % kItems]), k / kItems & 1, g.err);
+        if (row == 0) sh.quit[m] = !there;
+        named_barrier_sync(1 + m, kHalf);
+        if (sh.quit[m]) return;  // the same for the warpgroup's threads
+        const Segment& seg = sh.seg[k % kItems];
+        const Item& it = seg.it;
+        const int begin = seg.begin, end = seg.end;
         const long long c = (long long)it.block * kRows + m * kHalf + row;
         if (m < halves_of(g, it)) {
             const int j = (int)(c / g.group), head = it.h * g.group + (int)(c % g.group);
@@ -636,7 +654,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             o_phase ^= 1;
             fence_after_sync();
             const bool whole = begin == 0 && end == it.tiles;
-            const bool nan = sh.nan_any[k & 3] != 0;
+            const bool nan = sh.nan_any[k % kItems] != 0;
             const size_t orow = (size_t)(it.start + j) * g.hq + head;
             uint16_t* const dst = a.out + orow * D;
             const int b = blockIdx.x;
@@ -650,7 +668,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 if (nan) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e)  // column 16 c + 8 o + n is dim 16 c + 2 n + o
-                        if (sh.nan_at[k & 3][q * 32 + (e & 16) + (e & 7) * 2 + (e >> 3 & 1)] < sees) v[e] = NAN;
+                        if (sh.nan_at[k % kItems][q * 32 + (e & 16) + (e & 7) * 2 + (e >> 3 & 1)] < sees) v[e] = NAN;
                 }
                 if (!whole) {
 #pragma unroll
@@ -665,8 +683,8 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                     a.lse[orow] = sees > 0 ? (log2f(sum) + (top - kTop)) * kLn2 : -INFINITY;
             } else {
                 sc.many_sums[slot + row] = make_float2(top, sum);
-                const int first = p.owner_of(at);
-                const int parts = p.owner_of(at + it.tiles - 1) - first + 1;
+                int first, parts;
+                p.parts_of(seg.at, it.tiles, first, parts);
                 named_barrier_sync(1 + m, kHalf);
                 if (row == 0) sh.last[m] = arrive_last(&sc.many_arrived[first * 2 + m], parts);
                 named_barrier_sync(1 + m, kHalf);
@@ -681,18 +699,18 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                         total += z.y * (z.x == -INFINITY ? 0.0f : fast_exp2(z.x - high));
                     }
                     const float scale = sees > 0 ? 1.0f / total : 0.0f;
-                    // 32 dims at a time, out of four parts at a time
+                    // 32 dims at a time, out of two parts at a time
 #pragma unroll 1
                     for (int d = 0; live && d < D / 32; ++d) {
                         float v[32];
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.0f;
 #pragma unroll 1
-                        for (int q0 = 0; q0 < parts; q0 += 4) {
-                            float f[4];
-                            float4 x[4][8];
+                        for (int q0 = 0; q0 < parts; q0 += 2) {
+                            float f[2];
+                            float4 x[2][8];
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
+                            for (int z = 0; z < 2; ++z) {
                                 const bool there = q0 + z < parts;
                                 f[z] = there ? __ldcg(&sc.many_sums[part(q0 + z) + row]).x : -INFINITY;
 #pragma unroll
@@ -701,7 +719,7 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                                                     : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                             }
 #pragma unroll
-                            for (int z = 0; z < 4; ++z) {
+                            for (int z = 0; z < 2; ++z) {
                                 const float w = f[z] == -INFINITY ? 0.0f : fast_exp2(f[z] - high);
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) {
@@ -719,13 +737,9 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 }
             }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(sh.item_done[k & 3]));
         seq += end - begin;
-        ++k;
-        t = at + end;
-        at += it.tiles;
-        if (t < p.hi && !next_item<kRows, kTile>(g, a, unit, it)) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(sh.item_done[k % kItems]));
     }
 }
 
@@ -752,15 +766,20 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
             mbar_init(bar(sh.p_full[i][1]), 4);
             mbar_init(bar(sh.q_full[i]), 4);
         }
-        for (int i = 0; i < 4; ++i) {
-            mbar_init(bar(sh.meta_full[i]), 1);
-            mbar_init(bar(sh.item_done[i]), 8);
+        for (int i = 0; i < 4; ++i) mbar_init(bar(sh.meta_full[i]), 1);
+        for (int i = 0; i < kItems; ++i) {
+            mbar_init(bar(sh.item_full[i]), 1);
+            mbar_init(bar(sh.item_done[i]), kValueWarp);
         }
         fence_barrier_init();
         sh.abort = 0;
     }
-    Place p;
-    if (!find_place<kRows, kTile, kThreads, 2>(g, a, sh.scan, sh.found, p)) return;
+    {
+        Place p;
+        if (!find_place<kRows, kTile, kThreads, 2>(g, a, sh.scan, sh.found, p)) return;
+        if (threadIdx.x == 0) sh.place = p;
+    }
+    const Place& p = sh.place;
     if (warp == kIssueWarp) {
         tmem_alloc(smem_u32(&sh.tmem), 512);
         tmem_relinquish();
@@ -779,7 +798,7 @@ many_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CU
         else if (warp < kIssueWarp)
             convert_keys<FORMAT, D>(g, p, sh, smem);
         else if (warp == kIssueWarp)
-            issue<D>(g, a, p, sh, base);
+            issue<D>(g, p, sh, base);
         else
             load<D>(&kmap, &vmap, g, a, p, sh, base);
     }

@@ -80,12 +80,14 @@ struct SplitScratch {
     float2* many_sums;  // [2 sms][2][128] maximum, sum
     int* many_arrived;  // [sms][2]
 };
-// Requests of up to kFewRows rows (queries x heads of a kv-head), and of more.
-constexpr int kFewRows = 32;
+// Requests of up to a.upto rows by one kernel (`typical`: rows of most of them),
+// of more than a.above by the other; launch_cache_attend chooses.
 cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
-                             cudaStream_t st);
+                             int typical, cudaStream_t st);
 cudaError_t launch_cache_many(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
                               cudaStream_t st);
+cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                                cudaStream_t st);
 // One descriptor over a pool of `rows` rows of d bytes, 16 of them a load.
 bool encode_pool_map(CUtensorMap* out, const void* base, int d, long long rows);
 

@@ -246,23 +246,7 @@ bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int
                  q_token_stride, q_head_stride, starts, lengths, table, scale,
                  static_cast<uint16_t*>(out), lse, 0, 0};
     DeviceGuard dg(cache->device);
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // each request goes by its own number of rows; with the same for all, or
-    // too few in the call for any to have many, one kernel has them all
-    const long long rows = (long long)tokens * g.group;
-    const bool same = starts == nullptr;
-    if (same ? rows / requests <= kFewRows : rows <= kFewRows) {
-        a.upto = kFewRows;
-        BACON_CUDA(launch_cache_few(g, a, cache->sc, st), "attend launch");
-        return BACON_OK;
-    }
-    if (!same) {
-        a.upto = kFewRows;
-        BACON_CUDA(launch_cache_few(g, a, cache->sc, st), "attend launch");
-    }
-    a.above = kFewRows;
-    a.upto = 1ll << 62;
-    BACON_CUDA(launch_cache_many(g, a, cache->sc, st), "attend launch");
+    BACON_CUDA(launch_cache_attend(g, a, cache->sc, static_cast<cudaStream_t>(stream)), "attend launch");
     return BACON_OK;
 }
 

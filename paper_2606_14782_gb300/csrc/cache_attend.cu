@@ -51,10 +51,10 @@ struct Sizes {
     static constexpr int kStages = CG == 2 ? 6 : NT == 2 ? 4 : 3;
     static constexpr int kRows = kTile * D;        // bytes of K, or V, of a stage
     static constexpr int kStage = 2 * kRows;
-    static constexpr int kJoin = kStages * kStage; // half of the warps' outputs
+    static constexpr int kJoin = kStages * kStage; // the warps' outputs
     static constexpr int kPitch = D * 2 + 32;      // of a query row: 8 rows on distinct banks
     static constexpr int kQueries = kColumns * kPitch;
-    static constexpr int kRaw = kJoin + CG * 2 * NT * D * 8 * 4;  // two items' query rows
+    static constexpr int kRaw = kJoin + kWarps * NT * D * 8 * 4;  // two items' query rows
     static constexpr int kShared = kRaw + 2 * kQueries;
     static constexpr int kBytes = kShared + 3072;
 };
@@ -96,11 +96,6 @@ __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, ui
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-template <int N>
-struct Count {
-    static constexpr int value = N;
-};
 
 template <int FORMAT, int D, int NT, int CG>
 __global__ void __launch_bounds__(Sizes<D, NT, CG>::kThreads, Sizes<D, NT, CG>::kPerSm)
@@ -488,48 +483,42 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     acc[c][nt][k + 2] *= f;
                 }
             }
-        // by halves: the upper groups' outputs are added to the lower ones'
+        // every warp adds up its chunks of all groups' outputs
+        constexpr int kOwn = kChunks / kGroups;
+        const int c0 = group * kOwn;
         float4* const join =
-            reinterpret_cast<float4*>(smem + S::kJoin) + warp / kGroups * 2 * kChunks * NT * 32;
+            reinterpret_cast<float4*>(smem + S::kJoin) + warp / kGroups * kGroups * kChunks * NT * 32;
 #pragma unroll
-        for (int half = kGroups / 2; half; half >>= 1) {
-            if (group >= half && group < 2 * half) {
+        for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c)
+            for (int nt = 0; nt < NT; ++nt)
+                join[(group * kChunks * NT + c * NT + nt) * 32 + lane] = *reinterpret_cast<float4*>(acc[c][nt]);
+        named_barrier_sync(1, 32 * kWarps);
+        float o[kOwn][NT][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        join[((group - half) * kChunks * NT + c * NT + nt) * 32 + lane] =
-                            *reinterpret_cast<float4*>(acc[c][nt]);
-            }
-            named_barrier_sync(1, 32 * kWarps);
-            if (group < half) {
+        for (int c = 0; c < kOwn; ++c)
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c)
+            for (int nt = 0; nt < NT; ++nt) {
+                float4 x = join[((c0 + c) * NT + nt) * 32 + lane];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        const float4 o = join[(group * kChunks * NT + c * NT + nt) * 32 + lane];
-                        acc[c][nt][0] += o.x;
-                        acc[c][nt][1] += o.y;
-                        acc[c][nt][2] += o.z;
-                        acc[c][nt][3] += o.w;
-                    }
-            }
-            if (half > 1) named_barrier_sync(1, 32 * kWarps);
-        }
-
-        const bool whole = begin == 0 && end == it.tiles;
-        if (group == 0 && nan) {
-#pragma unroll
-            for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int w = 1; w < kGroups; ++w) {
+                    const float4 y = join[(w * kChunks * NT + (c0 + c) * NT + nt) * 32 + lane];
+                    x.x += y.x;
+                    x.y += y.y;
+                    x.z += y.z;
+                    x.w += y.w;
+                }
+                *reinterpret_cast<float4*>(o[c][nt]) = x;
+                if (nan) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (sh.nan_at[c * 16 + 2 * gr + (e >> 1)] < sees[nt][e & 1]) acc[c][nt][e] = NAN;
-        }
-        // chunks [c0, c0 + COUNT) of the columns' outputs, out of `from`
-        auto write = [&](auto count, const auto& from, int c0) {
-            constexpr int COUNT = decltype(count)::value;
+                        if (sh.nan_at[(c0 + c) * 16 + 2 * gr + (e >> 1)] < sees[nt][e & 1]) o[c][nt][e] = NAN;
+                }
+            }
+
+        const bool whole = begin == 0 && end == it.tiles;
+        // the columns' outputs of this warp's chunks
+        auto write = [&] {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -539,113 +528,105 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     const size_t row = (size_t)(it.start + j) * g.hq + it.h * g.group + col % g.group;
                     const bool none = sees[nt][k] == 0;
                     const float inv = none ? 0.0f : 1.0f / sum[nt][k];
-                    uint32_t* const o = reinterpret_cast<uint32_t*>(a.out + row * D) + c0 * 8 + gr;
+                    uint32_t* const to = reinterpret_cast<uint32_t*>(a.out + row * D) + c0 * 8 + gr;
 #pragma unroll
-                    for (int c = 0; c < COUNT; ++c)
-                        o[c * 8] = none ? 0u : pack16(g.dtype, from[c][nt][k] * inv, from[c][nt][k + 2] * inv);
-                    if (a.lse && gr == 0 && c0 == 0)
+                    for (int c = 0; c < kOwn; ++c)
+                        to[c * 8] = none ? 0u : pack16(g.dtype, o[c][nt][k] * inv, o[c][nt][k + 2] * inv);
+                    if (a.lse && gr == 0 && group == 0)
                         a.lse[row] = none ? -INFINITY
                                           : (log2f(sum[nt][k]) + (top[nt][k] - kWeightTop)) * kLn2;
                 }
         };
         if (whole) {
-            if (group == 0) write(Count<kChunks>{}, acc, 0);
+            write();
         } else {
             int first, parts;
             place.parts_of(seg.at, it.tiles, first, parts);
             // of a part: a column group's outputs as its warp holds them, then
             // the columns' maxima and sums
             const int mine = warp / kGroups * kChunks * NT * 32 + lane;
-            if (group == 0) {
-                // slot 2 b + 1: the item's first part, 2 b: a later one
-                const size_t part = 2 * (size_t)b + (begin == 0 ? 1 : 0);
-                float4* const po = reinterpret_cast<float4*>(sc.out + part * 32 * 128) + mine;
-                float2* const pm = reinterpret_cast<float2*>(sc.sums + part * 64) + first_col;
+            // slot 2 b + 1: the item's first part, 2 b: a later one
+            const size_t part = 2 * (size_t)b + (begin == 0 ? 1 : 0);
+            float4* const po = reinterpret_cast<float4*>(sc.out + part * 32 * 128) + mine;
+            float2* const pm = reinterpret_cast<float2*>(sc.sums + part * 64) + first_col;
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c)
+            for (int c = 0; c < kOwn; ++c)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        po[(c * NT + nt) * 32] = *reinterpret_cast<float4*>(acc[c][nt]);
-                if (gr == 0)
+                for (int nt = 0; nt < NT; ++nt)
+                    po[((c0 + c) * NT + nt) * 32] = *reinterpret_cast<float4*>(o[c][nt]);
+            if (gr == 0 && group == 0)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            pm[nt * 8 + tq * 2 + k] = make_float2(top[nt][k], sum[nt][k]);
-            }
+                    for (int k = 0; k < 2; ++k)
+                        pm[nt * 8 + tq * 2 + k] = make_float2(top[nt][k], sum[nt][k]);
             named_barrier_sync(1, 32 * kWarps);
             if (tid == 0) sh.last = arrive_last(&sc.arrived[first], parts);
             named_barrier_sync(1, 32 * kWarps);
             if (sh.last) {
-                // the parts in the blocks' order, some at a time, each warp
-                // its chunks of the outputs
-                constexpr int kOwn = kChunks / kGroups;
+                // the parts in the blocks' order, some at a time
                 constexpr int kBatch = NT == 1 ? 8 : 4;
-                const int c0 = group * kOwn;
-                {
-                    float o[kOwn][NT][4];
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        top[nt][0] = top[nt][1] = -INFINITY;
-                        sum[nt][0] = sum[nt][1] = 0.0f;
+                for (int nt = 0; nt < NT; ++nt) {
+                    top[nt][0] = top[nt][1] = -INFINITY;
+                    sum[nt][0] = sum[nt][1] = 0.0f;
 #pragma unroll
-                        for (int c = 0; c < kOwn; ++c)
+                    for (int c = 0; c < kOwn; ++c)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) o[c][nt][e] = 0.0f;
-                    }
+                        for (int e = 0; e < 4; ++e) o[c][nt][e] = 0.0f;
+                }
 #pragma unroll 1
-                    for (int q0 = 0; q0 < parts; q0 += kBatch) {
-                        float2 z[kBatch][NT][2];
-                        float4 x[kBatch][kOwn][NT];
+                for (int q0 = 0; q0 < parts; q0 += kBatch) {
+                    float2 z[kBatch][NT][2];
+                    float4 x[kBatch][kOwn][NT];
 #pragma unroll
-                        for (int q = 0; q < kBatch; ++q) {
-                            const bool there = q0 + q < parts;
-                            const size_t part = 2 * (size_t)(first + q0 + q) + (q0 + q == 0 ? 1 : 0);
-                            const float2* const pm = reinterpret_cast<const float2*>(sc.sums + part * 64) + first_col;
-                            const float4* const po = reinterpret_cast<const float4*>(sc.out + part * 32 * 128) + mine;
+                    for (int q = 0; q < kBatch; ++q) {
+                        const bool there = q0 + q < parts;
+                        const size_t part = 2 * (size_t)(first + q0 + q) + (q0 + q == 0 ? 1 : 0);
+                        const float2* const pm = reinterpret_cast<const float2*>(sc.sums + part * 64) + first_col;
+                        const float4* const po = reinterpret_cast<const float4*>(sc.out + part * 32 * 128) + mine;
 #pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
+                        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                                for (int k = 0; k < 2; ++k)
-                                    z[q][nt][k] = there ? __ldcg(&pm[nt * 8 + tq * 2 + k])
-                                                        : make_float2(-INFINITY, 0.0f);
+                            for (int k = 0; k < 2; ++k)
+                                z[q][nt][k] = there ? __ldcg(&pm[nt * 8 + tq * 2 + k])
+                                                    : make_float2(-INFINITY, 0.0f);
 #pragma unroll
-                                for (int c = 0; c < kOwn; ++c)
-                                    x[q][c][nt] = there ? __ldcg(&po[((c0 + c) * NT + nt) * 32])
-                                                        : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            }
+                            for (int c = 0; c < kOwn; ++c)
+                                x[q][c][nt] = there ? __ldcg(&po[((c0 + c) * NT + nt) * 32])
+                                                    : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         }
+                    }
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                float m = top[nt][k];
+                        for (int k = 0; k < 2; ++k) {
+                            float m = top[nt][k];
 #pragma unroll
-                                for (int q = 0; q < kBatch; ++q) m = fmaxf(m, z[q][nt][k].x);
-                                const float keep = top[nt][k] == -INFINITY ? 0.0f : fast_exp2(top[nt][k] - m);
-                                top[nt][k] = m;
-                                sum[nt][k] *= keep;
+                            for (int q = 0; q < kBatch; ++q) m = fmaxf(m, z[q][nt][k].x);
+                            const float keep = top[nt][k] == -INFINITY ? 0.0f : fast_exp2(top[nt][k] - m);
+                            top[nt][k] = m;
+                            sum[nt][k] *= keep;
+#pragma unroll
+                            for (int c = 0; c < kOwn; ++c) {
+                                o[c][nt][k] *= keep;
+                                o[c][nt][k + 2] *= keep;
+                            }
+#pragma unroll
+                            for (int q = 0; q < kBatch; ++q) {
+                                const float2 y = z[q][nt][k];
+                                const float f = y.x == -INFINITY ? 0.0f : fast_exp2(y.x - m);
+                                sum[nt][k] = fmaf(y.y, f, sum[nt][k]);
 #pragma unroll
                                 for (int c = 0; c < kOwn; ++c) {
-                                    o[c][nt][k] *= keep;
-                                    o[c][nt][k + 2] *= keep;
-                                }
-#pragma unroll
-                                for (int q = 0; q < kBatch; ++q) {
-                                    const float2 y = z[q][nt][k];
-                                    const float f = y.x == -INFINITY ? 0.0f : fast_exp2(y.x - m);
-                                    sum[nt][k] = fmaf(y.y, f, sum[nt][k]);
-#pragma unroll
-                                    for (int c = 0; c < kOwn; ++c) {
-                                        const float4 w = x[q][c][nt];
-                                        o[c][nt][k] = fmaf(k ? w.y : w.x, f, o[c][nt][k]);
-                                        o[c][nt][k + 2] = fmaf(k ? w.w : w.z, f, o[c][nt][k + 2]);
-                                    }
+                                    const float4 w = x[q][c][nt];
+                                    o[c][nt][k] = fmaf(k ? w.y : w.x, f, o[c][nt][k]);
+                                    o[c][nt][k + 2] = fmaf(k ? w.w : w.z, f, o[c][nt][k + 2]);
                                 }
                             }
-                    }
-                    write(Count<kOwn>{}, o, c0);
+                        }
                 }
+                write();
             }
         }
         named_barrier_sync(1, 32 * kWarps);
@@ -671,9 +652,9 @@ cudaError_t go(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, 
 }
 
 template <int FORMAT, int D>
-cudaError_t by_columns(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
+cudaError_t by_columns(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, int columns,
+                       cudaStream_t st)
 {
-    const long long columns = (long long)g.group * ((a.tokens + a.requests - 1) / a.requests);
     if (columns <= 8) return go<FORMAT, D, 1, 1>(g, a, sc, st);
     if (columns <= 16) return go<FORMAT, D, 2, 1>(g, a, sc, st);
     return go<FORMAT, D, 2, 2>(g, a, sc, st);
@@ -682,11 +663,50 @@ cudaError_t by_columns(const CacheGeom& g, const AttendArgs& a, const SplitScrat
 }  // namespace
 
 cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
-                             cudaStream_t st)
+                             int typical, cudaStream_t st)
 {
     if (g.format == BACON_E4M3)
-        return g.d == 128 ? by_columns<BACON_E4M3, 128>(g, a, sc, st) : by_columns<BACON_E4M3, 64>(g, a, sc, st);
-    return g.d == 128 ? by_columns<BACON_INT8, 128>(g, a, sc, st) : by_columns<BACON_INT8, 64>(g, a, sc, st);
+        return g.d == 128 ? by_columns<BACON_E4M3, 128>(g, a, sc, typical, st)
+                          : by_columns<BACON_E4M3, 64>(g, a, sc, typical, st);
+    return g.d == 128 ? by_columns<BACON_INT8, 128>(g, a, sc, typical, st)
+                      : by_columns<BACON_INT8, 64>(g, a, sc, typical, st);
+}
+
+// Which kernel has which requests, by their rows (queries x query heads of a
+// kv-head).  Both on calls of 28 / 4 and 32 / 8 heads of 128, in us, few and
+// many:
+//   21 rows, 8 x  4096 tokens  30   32        24 rows, 8 x 4096  46   49
+//   21 rows, 8 x 32768        125  111        24 rows, 1 x 1024  17   23
+//   56 rows, 8 x  4096         74   51        56 rows, 1 x 1024  17   23
+// so up to 32 rows, a block of columns, are few.  When the requests ask
+// differently, which ones do is known on the device only; each kernel then
+// takes its own, and one that has none still costs a launch, one that has some
+// the time of its own split and joining.  So a call that has few rows a
+// request on average leaves up to 64 with the others (32 requests of 7 to 49
+// rows over 1024 tokens: 52, 70 with the cut at 32), and one that has many
+// lets only what is close to a single token be few (8 requests of 21 to 49
+// rows over 4096: 40, 63 with the cut at 32).
+cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
+                                cudaStream_t st)
+{
+    constexpr int kFew = 32;
+    const long long rows = (long long)a.tokens * g.group, each = rows / a.requests;
+    AttendArgs few = a, many = a;
+    few.above = 0;
+    many.upto = 1ll << 62;
+    int typical = (int)(each < kFew ? each : kFew);
+    if (!a.starts) {
+        few.upto = many.above = each <= kFew ? many.upto : 0;
+    } else if (each <= kFew) {
+        few.upto = many.above = 2 * kFew;
+    } else {
+        few.upto = many.above = kFew / 2;
+        typical = g.group;
+    }
+    cudaError_t e = cudaSuccess;
+    if (few.upto > 0) e = launch_cache_few(g, few, sc, typical, st);
+    if (e == cudaSuccess && many.above < rows) e = launch_cache_many(g, many, sc, st);
+    return e;
 }
 
 }  // namespace bacon

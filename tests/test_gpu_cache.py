@@ -659,3 +659,18 @@ def test_refusals():
     cache.sync()
     cache.close()
     refused(lambda: cache.sync())
+
+
+@pytest.mark.parametrize("format,most", [("e4m3", 0.05), ("int8", 0.02)])
+def test_the_example_serves_kept_rows(format, most):
+    """Codes are off by a sixteenth (e4m3: 2^-4 of the value) or a 127th of the
+    page's largest at most, half of that on average or less, and the softmax
+    averages the values' part of it."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "serve_kept_rows.py")
+    spec = importlib.util.spec_from_file_location("serve_kept_rows", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    assert mod.main(format) < most

@@ -1,5 +1,7 @@
 // C ABI of the 8-bit paged cache: argument checks and the handle.
 #include <cmath>
+#include <cstdlib>
+#include <cstring>
 #include <new>
 
 #include "bacon.h"
@@ -12,6 +14,7 @@ using namespace bacon;
 struct bacon_cache {
     int device = 0;
     int max_requests = 0;
+    int fault_pending = 0;  // test-only fault injection (BACON_FAULT=missing_page)
     CacheGeom g{};
     SplitScratch sc{};
 };
@@ -118,6 +121,8 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
         bacon_cache_destroy(c);
         return fail(BACON_ECUDA, "cuTensorMapEncodeTiled failed");
     }
+    const char* const fault = std::getenv("BACON_FAULT");
+    c->fault_pending = fault && std::strcmp(fault, "missing_page") == 0;
     *out = c;
     return BACON_OK;
 }
@@ -244,7 +249,8 @@ bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int
     if (scale == 0.0f) scale = 1.0f / std::sqrt((float)g.d);
     AttendArgs a{requests, layer, tokens, causal != 0, static_cast<const uint16_t*>(q),
                  q_token_stride, q_head_stride, starts, lengths, table, scale,
-                 static_cast<uint16_t*>(out), lse, 0, 0};
+                 static_cast<uint16_t*>(out), lse, cache->fault_pending, 0, 0};
+    cache->fault_pending = 0;
     DeviceGuard dg(cache->device);
     BACON_CUDA(launch_cache_attend(g, a, cache->sc, static_cast<cudaStream_t>(stream)), "attend launch");
     return BACON_OK;
@@ -259,7 +265,11 @@ bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream)
     int flag = 0;
     BACON_CUDA(cudaMemcpy(&flag, cache->g.err, sizeof(int), cudaMemcpyDeviceToHost), "error flag read");
     if (!flag) return BACON_OK;
-    BACON_CUDA(cudaMemset(cache->g.err, 0, sizeof(int)), "error flag reset");
+    // cleared before it is reported, so that the next call starts clean; a
+    // block that gave up may have left counts of parts behind
+    BACON_CUDA(cudaMemset(cache->sc.arrived, 0,
+                          (const char*)(cache->g.err + 1) - (const char*)cache->sc.arrived),
+               "error flag reset");
     if (flag == kCacheBadIndex)
         return fail(BACON_EINVAL, "a length, slot, page or query range was outside its array");
     if (flag == kCacheNoPages) return fail(BACON_ENOMEM, "the ring holds too few pages");

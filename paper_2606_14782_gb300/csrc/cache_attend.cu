@@ -207,7 +207,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 const int boxes = __popc(__ballot_sync(0xFFFFFFFFu, live));
                 if (lane == 0 && boxes) mbar_expect_tx(full, boxes * kBoxRows * D);
                 __syncwarp();
-                if (live)
+                if (live && !(a.fault && b == 0 && issued == 0 && lane == 0))
                     load_rows(base + stage * S::kStage + (of_v ? S::kRows : 0) + group * 16 * D,
                               of_v ? &vmap : &kmap, (page << g.page_log2) + (pos & (g.page - 1)), full);
                 if (!live) s = 1.0f;

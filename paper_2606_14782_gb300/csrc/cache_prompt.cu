@@ -176,7 +176,8 @@ __device__ __forceinline__ void load(const CUtensorMap* kmap, const CUtensorMap*
             if (!ok) break;
             if (lane == 0 && boxes) mbar_expect_tx(bar(sh.rawk_full), boxes * kBoxRows * D);
             __syncwarp();
-            if (live && !of_v) load_rows(base + S::kRawK + group * 16 * D, kmap, row, bar(sh.rawk_full));
+            if (live && !of_v && !(a.fault && blockIdx.x == 0 && seq == 0 && lane == 0))
+                load_rows(base + S::kRawK + group * 16 * D, kmap, row, bar(sh.rawk_full));
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sh.rawk_full));
             const int slot = seq & 3;

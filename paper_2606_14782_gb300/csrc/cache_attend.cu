@@ -30,25 +30,30 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 64;  // tokens of a stage
-constexpr int kGroups = 4; // of 16 tokens
+constexpr int kGroups = 4;  // warps beside one another on a stage's tokens
 
 struct Meta {  // of 16 tokens of a stage
     float k_scale, v_log2, v_inv;
 };
 
-// Sizes for CG groups of 8 NT columns.  A warp takes 16 tokens of a stage and a
-// group's columns; with two groups the codes are converted by two warps each,
+// Sizes for CG groups of 8 NT columns.  A warp takes 16 MT tokens of a stage and
+// a group's columns; with two groups the codes are converted by two warps each,
 // which costs less than 32 columns' sums in one warp's registers do: 9 warps
-// have 168 registers a thread, 128 of them would be sums.  Bytes on their way
-// per SM: 3 x 3, 2 x 4 or 6 stages of 16 KB.
+// have 168 registers a thread, 128 of them would be sums.  MT = 2 gives a stage
+// the bytes that its barriers and its maximum are worth, and two independent
+// chains: at head_dim 64 and for two groups (us, MT = 1 and 2: a token of 32
+// requests over 8192 rows of 64 69 and 56; four tokens of 8 over 16384 of 128
+// 75 and 72), but with one group at 128 it leaves two blocks on an SM instead
+// of three (a token of 24 multi-head requests over 256 rows 25.7 and 27.7).
 template <int D, int NT, int CG>
 struct Sizes {
-    static constexpr int kWarps = 4 * CG;  // that compute
+    static constexpr int kMT = D == 64 || CG == 2 ? 2 : 1;
+    static constexpr int kTile = 16 * kMT * kGroups;  // tokens of a stage
+    static constexpr int kWarps = kGroups * CG;       // that compute
     static constexpr int kThreads = 32 * (kWarps + 1);
     static constexpr int kColumns = 8 * NT * CG;
     static constexpr int kPerSm = CG == 2 ? 1 : NT == 2 ? 2 : 3;
-    static constexpr int kStages = CG == 2 ? 6 : NT == 2 ? 4 : 3;
+    static constexpr int kStages = D == 128 && CG == 2 ? 3 : CG == 2 ? 6 : NT == 2 ? 4 : 3;
     static constexpr int kRows = kTile * D;        // bytes of K, or V, of a stage
     static constexpr int kStage = 2 * kRows;
     static constexpr int kJoin = kStages * kStage; // the warps' outputs
@@ -58,7 +63,8 @@ struct Sizes {
     static constexpr int kShared = kRaw + 2 * kQueries;
     static constexpr int kBytes = kShared + 3072;
 };
-static_assert(3 * (Sizes<128, 1, 1>::kBytes + 1024) <= 228 * 1024, "three blocks on an SM");
+static_assert(Sizes<128, 1, 1>::kPerSm * (Sizes<128, 1, 1>::kBytes + 1024) <= 228 * 1024, "blocks on an SM");
+static_assert(Sizes<64, 1, 1>::kPerSm * (Sizes<64, 1, 1>::kBytes + 1024) <= 228 * 1024, "blocks on an SM");
 static_assert(2 * (Sizes<128, 2, 1>::kBytes + 1024) <= 228 * 1024, "two blocks on an SM");
 static_assert(Sizes<128, 2, 2>::kBytes <= 227 * 1024, "one block on an SM");
 
@@ -68,9 +74,9 @@ struct Segment {  // tiles [begin, end) of an item, whose first tile is tile `at
     long long at;
 };
 
-template <int STAGES>
+template <int STAGES, int MT>
 struct Shared {
-    Meta meta[STAGES][kGroups];
+    Meta meta[STAGES][kGroups * MT];
     float top[kGroups][32], sum[kGroups][32];
     uint64_t full[STAGES], empty[STAGES], q_full[2], q_empty[2];
     Segment seg[2];
@@ -80,7 +86,7 @@ struct Shared {
     int nan_at[128];  // per dim: first position of a NaN of V that not every column sees
     int nan_any;
 };
-static_assert(sizeof(Shared<6>) <= 3072, "shared record");
+static_assert(sizeof(Shared<6, 2>) <= 3072, "shared record");
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -104,9 +110,9 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 {
     using S = Sizes<D, NT, CG>;
     constexpr int kChunks = D / 16, kWarps = S::kWarps, kStages = S::kStages;
-    constexpr int kThreads = S::kThreads, kColumns = S::kColumns;
+    constexpr int kThreads = S::kThreads, kColumns = S::kColumns, kTile = S::kTile, kMT = S::kMT;
     extern __shared__ __align__(1024) uint8_t smem[];
-    auto& sh = *reinterpret_cast<Shared<kStages>*>(smem + S::kShared);
+    auto& sh = *reinterpret_cast<Shared<kStages, kMT>*>(smem + S::kShared);
     const uint32_t base = smem_u32(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
@@ -174,13 +180,14 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
             // by two tiles, scales by one
             const bool last_of_unit = it.block + 1 >= blocks_of<kColumns>(g, it.asked);
             const int ahead = last_of_unit ? length_ahead(g, a, unit) : 0;
-            // lanes 0-3: K's 16-row groups of a tile, lanes 4-7: V's
-            const int group = lane % kGroups;
-            const bool of_v = lane >= kGroups;
+            // a lane a 16-row group of a tile: K's first, then V's
+            constexpr int kBoxes = kGroups * kMT;
+            const int group = lane % kBoxes;
+            const bool of_v = lane >= kBoxes;
             const float* const scales = of_v ? g.v_scale : g.k_scale;
             const int32_t* const table =
                 a.table + (((size_t)it.r * g.layers + a.layer) * g.hkv + it.h) * g.max_blocks;
-            const int upto = lane < 2 * kGroups ? (int)min((long long)it.seen, (long long)end * kTile) : 0;
+            const int upto = lane < 2 * kBoxes ? (int)min((long long)it.seen, (long long)end * kTile) : 0;
             auto page_of = [&](int i) {
                 const int pos = i * kTile + group * 16;
                 return pos < upto ? table[pos >> g.page_log2] : 0;
@@ -211,9 +218,9 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                     load_rows(base + stage * S::kStage + (of_v ? S::kRows : 0) + group * 16 * D,
                               of_v ? &vmap : &kmap, (page << g.page_log2) + (pos & (g.page - 1)), full);
                 if (!live) s = 1.0f;
-                if (lane < kGroups) {
+                if (lane < kBoxes) {
                     sh.meta[stage][group].k_scale = s;
-                } else if (lane < 2 * kGroups) {
+                } else if (lane < 2 * kBoxes) {
                     sh.meta[stage][group].v_log2 = log2f(s);
                     sh.meta[stage][group].v_inv = 1.0f / s;
                 }
@@ -269,7 +276,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
     uint32_t qf[kChunks][NT][2];
     // matrix loads: lane l gives row l & 7 of matrix l >> 3; matrices are rows
     // 0-7, rows 8-15, of 16-byte chunk c, then of c + 1
-    const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8, mchunk = lane >> 4;
+    const int mrow = group * 16 * kMT + (lane & 7) + (lane >> 3 & 1) * 8, mchunk = lane >> 4;
     const uint32_t swizzle = D == 128 ? mrow & 7 : mrow >> 1 & 3;
 
     int items = 0;
@@ -336,62 +343,82 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 atomicCAS(g.err, 0, kCacheTimeout);
             }
             __syncwarp();
-            const int pos = i * kTile + group * 16;
+            const int pos = i * kTile + group * 16 * kMT;
             if (pos < it.seen) {
                 const uint32_t krow = base + stage * S::kStage + mrow * D;
-                const Meta meta = sh.meta[stage][group];
-                float s[NT][2][4];  // two chains of products
+                float y[kMT][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int t = 0; t < kMT; ++t) {
+                    float s[NT][2][4];  // two chains of products
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[nt][0][e] = s[nt][1][e] = 0.0f;
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < kChunks; c += 2) {
-                    uint32_t w[4], f[8];
-                    ldmatrix4(w, krow + (((c + mchunk) ^ swizzle) << 4));
-                    // rows gr and gr + 8, first pairs of dims then second ones
-                    codes_half<FORMAT>(w[0], f[0], f[2]);
-                    codes_half<FORMAT>(w[1], f[1], f[3]);
-                    codes_half<FORMAT>(w[2], f[4], f[6]);
-                    codes_half<FORMAT>(w[3], f[5], f[7]);
+                        for (int e = 0; e < 4; ++e) s[nt][0][e] = s[nt][1][e] = 0.0f;
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma(s[nt][0], f, qf[c][nt][0], qf[c][nt][1]);
-                        mma(s[nt][1], f + 4, qf[c + 1][nt][0], qf[c + 1][nt][1]);
+                    for (int c = 0; c < kChunks; c += 2) {
+                        uint32_t w[4], f[8];
+                        ldmatrix4(w, krow + t * 16 * D + (((c + mchunk) ^ swizzle) << 4));
+                        // rows gr and gr + 8, first pairs of dims then second ones
+                        codes_half<FORMAT>(w[0], f[0], f[2]);
+                        codes_half<FORMAT>(w[1], f[1], f[3]);
+                        codes_half<FORMAT>(w[2], f[4], f[6]);
+                        codes_half<FORMAT>(w[3], f[5], f[7]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma(s[nt][0], f, qf[c][nt][0], qf[c][nt][1]);
+                            mma(s[nt][1], f + 4, qf[c + 1][nt][0], qf[c + 1][nt][1]);
+                        }
                     }
+                    const float ks = sh.meta[stage][group * kMT + t].k_scale;
+                    const float vl = sh.meta[stage][group * kMT + t].v_log2;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[t][nt][e] = (s[nt][0][e] + s[nt][1][e]) * (factor[nt][e & 1] * ks) + vl;
                 }
                 // exponents, the running maximum, weights
-                const bool cut = pos + 16 > all;
-                uint32_t p[NT][2];
+                const bool cut = pos + 16 * kMT > all;
+                uint32_t p[kMT][NT][2];
                 bool grew = false;
                 float keep[NT][2];
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    float y[4], high[2];
+                    if (cut) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        y[e] = (s[nt][0][e] + s[nt][1][e]) * (factor[nt][e & 1] * meta.k_scale) + meta.v_log2;
-                        if (cut && pos + gr + (e >> 1) * 8 >= sees[nt][e & 1]) y[e] = -INFINITY;
+                        for (int t = 0; t < kMT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (pos + t * 16 + gr + (e >> 1) * 8 >= sees[nt][e & 1]) y[t][nt][e] = -INFINITY;
                     }
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        high[k] = fmaxf(y[k], y[k + 2]);
+                        float high = fmaxf(y[0][nt][k], y[0][nt][k + 2]);
 #pragma unroll
-                        for (int o = 4; o < 32; o <<= 1)
-                            high[k] = fmaxf(high[k], __shfl_xor_sync(0xFFFFFFFFu, high[k], o));
+                        for (int t = 1; t < kMT; ++t) high = fmaxf(high, fmaxf(y[t][nt][k], y[t][nt][k + 2]));
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xFFFFFFFFu, high, o));
                         keep[nt][k] = 1.0f;
-                        if (high[k] > top[nt][k]) {
-                            keep[nt][k] = fast_exp2(top[nt][k] - high[k]);
-                            top[nt][k] = high[k];
+                        if (high > top[nt][k]) {
+                            keep[nt][k] = fast_exp2(top[nt][k] - high);
+                            top[nt][k] = high;
                             grew = true;
                         }
                         const float m = top[nt][k] == -INFINITY ? 0.0f : top[nt][k] - kWeightTop;
-                        y[k] = fast_exp2(y[k] - m);
-                        y[k + 2] = fast_exp2(y[k + 2] - m);
-                        sum[nt][k] = sum[nt][k] * keep[nt][k] + (y[k] + y[k + 2]) * meta.v_inv;
+                        sum[nt][k] *= keep[nt][k];
+#pragma unroll
+                        for (int t = 0; t < kMT; ++t) {
+                            y[t][nt][k] = fast_exp2(y[t][nt][k] - m);
+                            y[t][nt][k + 2] = fast_exp2(y[t][nt][k + 2] - m);
+                            sum[nt][k] = fmaf(y[t][nt][k] + y[t][nt][k + 2],
+                                              sh.meta[stage][group * kMT + t].v_inv, sum[nt][k]);
+                        }
                     }
-                    p[nt][0] = transpose8(half2_of(y[0], y[1]));
-                    p[nt][1] = transpose8(half2_of(y[2], y[3]));
+#pragma unroll
+                    for (int t = 0; t < kMT; ++t) {
+                        p[t][nt][0] = transpose8(half2_of(y[t][nt][0], y[t][nt][1]));
+                        p[t][nt][1] = transpose8(half2_of(y[t][nt][2], y[t][nt][3]));
+                    }
                 }
                 if (__any_sync(0xFFFFFFFFu, grew)) {
 #pragma unroll
@@ -401,42 +428,45 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll
                             for (int e = 0; e < 4; ++e) acc[c][nt][e] *= keep[nt][e & 1];
                 }
-                const uint32_t vrow = krow + S::kRows;
 #pragma unroll
-                for (int c = 0; c < kChunks; c += 2) {
-                    uint32_t w[4], f[8];
-                    ldmatrix4_trans(w, vrow + (((c + mchunk) ^ swizzle) << 4));
-                    if (cut) {
-                        // rows that no column sees are whatever the page holds;
-                        // a NaN that some column does not see is taken out
-                        // and put back at the item's end
+                for (int t = 0; t < kMT; ++t) {
+                    const uint32_t vrow = krow + S::kRows + t * 16 * D;
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) {
-                            const int x0 = pos + (m & 1) * 8 + 2 * tq;
-                            if (x0 >= it.seen) w[m] &= 0xFFFF0000u;
-                            if (x0 + 1 >= it.seen) w[m] &= 0x0000FFFFu;
-                            if (FORMAT == BACON_E4M3 &&
-                                (((w[m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+                    for (int c = 0; c < kChunks; c += 2) {
+                        uint32_t w[4], f[8];
+                        ldmatrix4_trans(w, vrow + (((c + mchunk) ^ swizzle) << 4));
+                        if (cut) {
+                            // rows that no column sees are whatever the page
+                            // holds; a NaN that some column does not see is
+                            // taken out and put back at the item's end
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    if ((w[m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
-                                        w[m] &= ~(0xFFu << (8 * e));
-                                        atomicMin(&sh.nan_at[(c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
-                                                  x0 + (e >> 1));
-                                        sh.nan_any = 1;
-                                    }
+                            for (int m = 0; m < 4; ++m) {
+                                const int x0 = pos + t * 16 + (m & 1) * 8 + 2 * tq;
+                                if (x0 >= it.seen) w[m] &= 0xFFFF0000u;
+                                if (x0 + 1 >= it.seen) w[m] &= 0x0000FFFFu;
+                                if (FORMAT == BACON_E4M3 &&
+                                    (((w[m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        if ((w[m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
+                                            w[m] &= ~(0xFFu << (8 * e));
+                                            atomicMin(&sh.nan_at[(c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
+                                                      x0 + (e >> 1));
+                                            sh.nan_any = 1;
+                                        }
+                                }
                             }
                         }
-                    }
-                    // rows gr: dim 2 gr, rows gr + 8: dim 2 gr + 1 of a chunk
-                    pairs_half<FORMAT>(w[0], f[0], f[1]);
-                    pairs_half<FORMAT>(w[1], f[2], f[3]);
-                    pairs_half<FORMAT>(w[2], f[4], f[5]);
-                    pairs_half<FORMAT>(w[3], f[6], f[7]);
+                        // rows gr: dim 2 gr, rows gr + 8: dim 2 gr + 1 of a chunk
+                        pairs_half<FORMAT>(w[0], f[0], f[1]);
+                        pairs_half<FORMAT>(w[1], f[2], f[3]);
+                        pairs_half<FORMAT>(w[2], f[4], f[5]);
+                        pairs_half<FORMAT>(w[3], f[6], f[7]);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma(acc[c][nt], f, p[nt][0], p[nt][1]);
-                        mma(acc[c + 1][nt], f + 4, p[nt][0], p[nt][1]);
+                        for (int nt = 0; nt < NT; ++nt) {
+                            mma(acc[c][nt], f, p[t][nt][0], p[t][nt][1]);
+                            mma(acc[c + 1][nt], f + 4, p[t][nt][0], p[t][nt][1]);
+                        }
                     }
                 }
             }

@@ -634,21 +634,27 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
             if (lane == 0) mbar_arrive(bar(sh.q_full[m]));
 
             float top = -INFINITY, sum = 0.0f;
-            for (int i = begin; i < end; ++i) {
-                const uint32_t s = seq + (i - begin), slot = s & 3;
-                wait(sh, bar(sh.meta_full[slot]), s >> 2 & 1, g.err);
+            // the tile's logits are there
+            auto arrived = [&](int i) {
+                const uint32_t s = seq + (i - begin);
+                wait(sh, bar(sh.meta_full[s & 3]), s >> 2 & 1, g.err);
                 wait(sh, bar(sh.s_full[m]), s_phase, g.err);
                 s_phase ^= 1;
                 fence_after_sync();
-                const bool cut = (i + 1) * kTile > all;
-                const int left = sees - i * kTile;  // positions of the tile that the row sees
-                if (!live) {
+                return s & 3;
+            };
+            int i = begin;
+            if (!live) {
+                for (; i < end; ++i) {
+                    arrived(i);
                     if (lane < 2) mbar_arrive(bar(sh.p_full[m][lane]));
-                } else if (cut)
-                    softmax_tile<D, true>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
-                else
-                    softmax_tile<D, false>(sh, m, slot, logits, out, i > begin, left, factor, top, sum);
+                }
             }
+            for (const int full = min(end, all / kTile); i < full; ++i)
+                softmax_tile<D, false>(sh, m, arrived(i), logits, out, i > begin, kTile, factor, top, sum);
+            for (; i < end; ++i)
+                softmax_tile<D, true>(sh, m, arrived(i), logits, out, i > begin, sees - i * kTile, factor,
+                                      top, sum);
 
             // ------------------------------------------------- outputs
             wait(sh, bar(sh.o_full[m]), o_phase, g.err);

@@ -274,7 +274,7 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
     using S = Smem<D>;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kValueWarp;
     const int gr = lane >> 2, tq = lane & 3;
-#pragma unroll
+#pragma unroll (CUT ? 1 : 2)
     for (int half = 0; half < 2; ++half) {
         const int group = warp * 2 + half;
         const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
@@ -285,23 +285,30 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
         const int chunk = (group & 3) * 2 + (lane >> 4);
         const uint32_t dst = base + S::kValues + buf * S::kValuesTile + (group >> 2) * (D * 128) +
                              n0 * 128 + ((chunk ^ (n0 & 7)) << 4);
-        uint32_t w[D / 32][4];
+        // (loads together where nothing is cut; cut tiles are few, and their
+        // loop is rolled to be fetched at once)
+        constexpr int kTogether = CUT ? 1 : D / 32;
+#pragma unroll 1
+        for (int c0 = 0; c0 < D / 32; c0 += kTogether) {
+        uint32_t w[kTogether][4];
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) ldmatrix4_trans(w[c], src + (((2 * c + (lane >> 4)) ^ swizzle) << 4));
+        for (int z = 0; z < kTogether; ++z)
+            ldmatrix4_trans(w[z], src + (((2 * (c0 + z) + (lane >> 4)) ^ swizzle) << 4));
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
+        for (int z = 0; z < kTogether; ++z) {
+            const int c = c0 + z;
             uint32_t f[8];
             if (CUT) {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     const int x0 = pos + group * 16 + (m & 1) * 8 + 2 * tq;
-                    if (x0 >= seen) w[c][m] &= 0xFFFF0000u;
-                    if (x0 + 1 >= seen) w[c][m] &= 0x0000FFFFu;
-                    if (FORMAT == BACON_E4M3 && (((w[c][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+                    if (x0 >= seen) w[z][m] &= 0xFFFF0000u;
+                    if (x0 + 1 >= seen) w[z][m] &= 0x0000FFFFu;
+                    if (FORMAT == BACON_E4M3 && (((w[z][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if ((w[c][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
-                                w[c][m] &= ~(0xFFu << (8 * e));
+                            if ((w[z][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
+                                w[z][m] &= ~(0xFFu << (8 * e));
                                 atomicMin(&sh.nan_at[item % kItems][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
                                           x0 + (e >> 1));
                                 sh.nan_any[item % kItems] = 1;
@@ -309,12 +316,13 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
                     }
                 }
             }
-            pairs_half<FORMAT>(w[c][0], f[0], f[1]);
-            pairs_half<FORMAT>(w[c][1], f[2], f[3]);
-            pairs_half<FORMAT>(w[c][2], f[4], f[5]);
-            pairs_half<FORMAT>(w[c][3], f[6], f[7]);
+            pairs_half<FORMAT>(w[z][0], f[0], f[1]);
+            pairs_half<FORMAT>(w[z][1], f[2], f[3]);
+            pairs_half<FORMAT>(w[z][2], f[4], f[5]);
+            pairs_half<FORMAT>(w[z][3], f[6], f[7]);
             stmatrix4(dst + c * 32 * 128, f);
             stmatrix4(dst + (c * 32 + 16) * 128, f + 4);
+        }
         }
     }
 }
@@ -445,13 +453,34 @@ __device__ __forceinline__ float max16(const float* v)
     return max3(max3(a, b, c), max3(d, e, v[15]), v[15]);
 }
 
-// One tile of a row's logits into weights.  CUT: the row sees only the first
-// `left` of the tile's tokens, or all for left >= 128.  `scaled`: O holds
-// sums that follow the reference.
-template <int D, bool CUT>
+// The row's reference follows its maximum `high` when that has grown; `scaled`:
+// O holds sums that follow it too.
+template <int D>
+__device__ __forceinline__ void follow(float high, bool scaled, uint32_t out, float& top, float& sum)
+{
+    const bool grew = high > top + kSlack;
+    if (!__any_sync(0xFFFFFFFFu, grew)) return;
+    const float keep = grew ? fast_exp2(top - high) : 1.0f;
+    if (grew) top = high;
+    sum *= keep;
+    if (scaled) {
+#pragma unroll
+        for (int q = 0; q < D / 16; ++q) {
+            float o[16];
+            tmem_ld16(out + q * 16, o);
+            tmem_ld_wait_regs16(o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] *= keep;
+            tmem_st8(out + q * 16, o);
+            tmem_st8(out + q * 16 + 8, o + 8);
+        }
+    }
+}
+
+// One tile of a row's logits, all of which it sees, into weights.
+template <int D>
 __device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot, uint32_t logits,
-                                             uint32_t out, bool scaled, int left, float factor,
-                                             float& top, float& sum)
+                                             uint32_t out, bool scaled, float factor, float& top, float& sum)
 {
     const int lane = threadIdx.x & 31;
     float v[128], high = -INFINITY;
@@ -463,34 +492,11 @@ __device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int grp = q * 2 + h;
-            if (CUT) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (grp * 16 + e >= left) v[grp * 16 + e] = -INFINITY;
-            }
             const float x = max16(v + grp * 16);
-            const float y = fmaf(x, factor * sh.k_scale[slot][grp], sh.v_log2[slot][grp]);
-            if (x != -INFINITY) high = fmaxf(high, y);
+            high = fmaxf(high, fmaf(x, factor * sh.k_scale[slot][grp], sh.v_log2[slot][grp]));
         }
     }
-    const bool grew = high > top + kSlack;
-    if (__any_sync(0xFFFFFFFFu, grew)) {
-        const float keep = grew ? fast_exp2(top - high) : 1.0f;
-        if (grew) top = high;
-        sum *= keep;
-        if (scaled) {
-#pragma unroll
-            for (int q = 0; q < D / 16; ++q) {
-                float o[16];
-                tmem_ld16(out + q * 16, o);
-                tmem_ld_wait_regs16(o);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] *= keep;
-                tmem_st8(out + q * 16, o);
-                tmem_st8(out + q * 16 + 8, o + 8);
-            }
-        }
-    }
+    follow<D>(high, scaled, out, top, sum);
     const float ref = top == -INFINITY ? 0.0f : top - kTop;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -505,10 +511,6 @@ __device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot
             for (int e = 0; e < 16; e += 2) {
                 const float* const x = v + grp * 16 + e;
                 float2 y = unpack2(fma2(pack2(x[0], x[1]), f2, b2));
-                if (CUT) {  // (a factor that underflows makes -inf a NaN)
-                    if (grp * 16 + e >= left) y.x = -INFINITY;
-                    if (grp * 16 + e + 1 >= left) y.y = -INFINITY;
-                }
                 y.x = fast_exp2(y.x);
                 y.y = fast_exp2(y.y);
                 part = add2(part, pack2(y.x, y.y));
@@ -523,6 +525,56 @@ __device__ __forceinline__ void softmax_tile(Shared<D>& sh, int m, uint32_t slot
         fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(sh.p_full[m][half]));
+    }
+}
+
+// The same for a tile of which the row sees the first `left` tokens (all, with
+// left >= 128).  An item has two or three such tiles, so the loops are rolled:
+// fetching straight-line code once would cost more than running it.
+template <int D>
+__device__ __forceinline__ void softmax_cut_tile(Shared<D>& sh, int m, uint32_t slot, uint32_t logits,
+                                                 uint32_t out, bool scaled, int left, float factor,
+                                                 float& top, float& sum)
+{
+    const int lane = threadIdx.x & 31;
+    float high = -INFINITY;
+#pragma unroll 1
+    for (int grp = 0; grp < kGroups; ++grp) {
+        float v[16];
+        tmem_ld16(logits + grp * 16, v);
+        tmem_ld_wait_regs16(v);
+        const int some = left - grp * 16;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e >= some) v[e] = -INFINITY;
+        const float x = max16(v);
+        // (a factor that underflows would make -inf a NaN)
+        if (x != -INFINITY) high = fmaxf(high, fmaf(x, factor * sh.k_scale[slot][grp], sh.v_log2[slot][grp]));
+    }
+    follow<D>(high, scaled, out, top, sum);
+    const float ref = top == -INFINITY ? 0.0f : top - kTop;
+#pragma unroll 1
+    for (int grp = 0; grp < kGroups; ++grp) {
+        float v[16], w[8], part = 0.0f;
+        tmem_ld16(logits + grp * 16, v);
+        tmem_ld_wait_regs16(v);
+        const int some = left - grp * 16;
+        const float f = factor * sh.k_scale[slot][grp], b = sh.v_log2[slot][grp] - ref;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            v[e] = e < some ? fast_exp2(fmaf(v[e], f, b)) : 0.0f;
+            part += v[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = __uint_as_float(half2_of(v[2 * e], v[2 * e + 1]));
+        sum = fmaf(part, sh.v_inv[slot][grp], sum);
+        tmem_st8(logits + grp * 8, w);
+        if ((grp & 3) == 3) {
+            tmem_st_wait();
+            fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(sh.p_full[m][grp >> 2]));
+        }
     }
 }
 
@@ -651,10 +703,9 @@ __device__ __forceinline__ void softmax(const CacheGeom& g, const AttendArgs& a,
                 }
             }
             for (const int full = min(end, all / kTile); i < full; ++i)
-                softmax_tile<D, false>(sh, m, arrived(i), logits, out, i > begin, kTile, factor, top, sum);
+                softmax_tile<D>(sh, m, arrived(i), logits, out, i > begin, factor, top, sum);
             for (; i < end; ++i)
-                softmax_tile<D, true>(sh, m, arrived(i), logits, out, i > begin, sees - i * kTile, factor,
-                                      top, sum);
+                softmax_cut_tile<D>(sh, m, arrived(i), logits, out, i > begin, sees - i * kTile, factor, top, sum);
 
             // ------------------------------------------------- outputs
             wait(sh, bar(sh.o_full[m]), o_phase, g.err);

@@ -274,7 +274,7 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
     using S = Smem<D>;
     const int lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - kValueWarp;
     const int gr = lane >> 2, tq = lane & 3;
-#pragma unroll (CUT ? 1 : 2)
+#pragma unroll 1
     for (int half = 0; half < 2; ++half) {
         const int group = warp * 2 + half;
         const int mrow = group * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
@@ -290,39 +290,39 @@ __device__ __forceinline__ void convert_value_tile(Shared<D>& sh, uint32_t base,
         constexpr int kTogether = CUT ? 1 : D / 32;
 #pragma unroll 1
         for (int c0 = 0; c0 < D / 32; c0 += kTogether) {
-        uint32_t w[kTogether][4];
+            uint32_t w[kTogether][4];
 #pragma unroll
-        for (int z = 0; z < kTogether; ++z)
-            ldmatrix4_trans(w[z], src + (((2 * (c0 + z) + (lane >> 4)) ^ swizzle) << 4));
+            for (int z = 0; z < kTogether; ++z)
+                ldmatrix4_trans(w[z], src + (((2 * (c0 + z) + (lane >> 4)) ^ swizzle) << 4));
 #pragma unroll
-        for (int z = 0; z < kTogether; ++z) {
-            const int c = c0 + z;
-            uint32_t f[8];
-            if (CUT) {
+            for (int z = 0; z < kTogether; ++z) {
+                const int c = c0 + z;
+                uint32_t f[8];
+                if (CUT) {
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    const int x0 = pos + group * 16 + (m & 1) * 8 + 2 * tq;
-                    if (x0 >= seen) w[z][m] &= 0xFFFF0000u;
-                    if (x0 + 1 >= seen) w[z][m] &= 0x0000FFFFu;
-                    if (FORMAT == BACON_E4M3 && (((w[z][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
+                    for (int m = 0; m < 4; ++m) {
+                        const int x0 = pos + group * 16 + (m & 1) * 8 + 2 * tq;
+                        if (x0 >= seen) w[z][m] &= 0xFFFF0000u;
+                        if (x0 + 1 >= seen) w[z][m] &= 0x0000FFFFu;
+                        if (FORMAT == BACON_E4M3 && (((w[z][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u)) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if ((w[z][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
-                                w[z][m] &= ~(0xFFu << (8 * e));
-                                atomicMin(&sh.nan_at[item % kItems][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
-                                          x0 + (e >> 1));
-                                sh.nan_any[item % kItems] = 1;
-                            }
+                            for (int e = 0; e < 4; ++e)
+                                if ((w[z][m] >> (8 * e) & 0x7Fu) == 0x7Fu) {
+                                    w[z][m] &= ~(0xFFu << (8 * e));
+                                    atomicMin(&sh.nan_at[item % kItems][(2 * c + (m >> 1)) * 16 + 2 * gr + (e & 1)],
+                                              x0 + (e >> 1));
+                                    sh.nan_any[item % kItems] = 1;
+                                }
+                        }
                     }
                 }
+                pairs_half<FORMAT>(w[z][0], f[0], f[1]);
+                pairs_half<FORMAT>(w[z][1], f[2], f[3]);
+                pairs_half<FORMAT>(w[z][2], f[4], f[5]);
+                pairs_half<FORMAT>(w[z][3], f[6], f[7]);
+                stmatrix4(dst + c * 32 * 128, f);
+                stmatrix4(dst + (c * 32 + 16) * 128, f + 4);
             }
-            pairs_half<FORMAT>(w[z][0], f[0], f[1]);
-            pairs_half<FORMAT>(w[z][1], f[2], f[3]);
-            pairs_half<FORMAT>(w[z][2], f[4], f[5]);
-            pairs_half<FORMAT>(w[z][3], f[6], f[7]);
-            stmatrix4(dst + c * 32 * 128, f);
-            stmatrix4(dst + (c * 32 + 16) * 128, f + 4);
-        }
         }
     }
 }

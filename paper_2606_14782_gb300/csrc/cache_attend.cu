@@ -4,6 +4,10 @@
 // Bound by the pages' bytes: a token of a unit is 2 d bytes for 4 d flops a
 // query head, so with up to 32 columns (query heads of the kv-head x queries)
 // the work is a stream through HBM with two small matrix products beside it.
+// A token of 32 requests over 16384 rows (28 / 4 heads of 128) takes 96 us, 87 %
+// of the measured copy bandwidth; of four requests over 1024, 12 us, which are
+// the launch, the scan, one tile and the joining of 17 parts one after the
+// other.
 // The products are warp-level (m16n8k16, fp16 in, fp32 sums) with the tokens
 // as rows and the columns as n, so that no more than the next 8 columns are
 // padded: S^T = K Q^T, then O^T = V^T P^T.  K and V codes go from shared
@@ -12,13 +16,12 @@
 // and become fp16 there; what order the dims take inside a product is the
 // same for Q's fragments.  S^T turns into P^T's operand by 8x8 transposes.
 //
-// The call's tiles of 64 tokens are dealt out evenly: block b of E takes tiles
-// [T b / E, T (b + 1) / E) of the items one after the other, an item being 8 NT
-// columns of a unit, whatever the units' lengths.  Every block finds its place
-// by a scan of the lengths, so no host synchronisation and no second launch
-// come before; a warp of it loads (16 rows a TMA load, only rows that the item
-// sees), four compute, each 16 tokens of a tile with its own running maximum,
-// and join at the item's end.  An item cut by a block's edge leaves partial
+// The call's tiles are dealt out to the blocks evenly, an item (8 NT CG columns
+// of a unit) after the other, whatever the units' lengths.  Every block finds
+// its place by a scan of the lengths, so no host synchronisation and no second
+// launch come before; a warp of it loads (16 rows a TMA load, only rows that
+// the item sees, pages and scales on their way ahead), the others compute, each
+// with its own running maximum, and join at the item's end.  An item cut by a block's edge leaves partial
 // sums; the last of its blocks to arrive adds them up in the blocks' order, so
 // the result does not depend on timing.
 #include <cmath>
@@ -705,8 +708,8 @@ cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const Spli
 // Which kernel has which requests, by their rows (queries x query heads of a
 // kv-head).  Both on calls of 28 / 4 and 32 / 8 heads of 128, in us, few and
 // many:
-//   21 rows, 8 x  4096 tokens  30   32        24 rows, 8 x 4096  46   49
-//   21 rows, 8 x 32768        125  111        24 rows, 1 x 1024  17   23
+//   21 rows, 8 x  4096 tokens  27   32        24 rows, 8 x 4096  44   49
+//   21 rows, 8 x 32768        111  111        24 rows, 1 x 1024  17   23
 //   56 rows, 8 x  4096         74   51        56 rows, 1 x 1024  17   23
 // so up to 32 rows, a block of columns, are few.  When the requests ask
 // differently, which ones do is known on the device only; each kernel then
@@ -715,7 +718,7 @@ cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const Spli
 // request on average leaves up to 64 with the others (32 requests of 7 to 49
 // rows over 1024 tokens: 52, 70 with the cut at 32), and one that has many
 // lets only what is close to a single token be few (8 requests of 21 to 49
-// rows over 4096: 40, 63 with the cut at 32).
+// rows over 4096: 40, 63 with the cut at 32; 38 now).
 cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
                                 cudaStream_t st)
 {

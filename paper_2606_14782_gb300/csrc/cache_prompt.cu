@@ -2,6 +2,10 @@
 // or a prompt over a cache.
 //
 // Bound by the tensor cores: 4 d flops for every query head and token it sees.
+// 4096 queries over 16384 tokens (28 / 4 heads of 128) take 555 us, 1517 TFLOP/s,
+// 79 % of the measured burst rate of a library product; 100 queries each of
+// three requests over 2000 tokens 31 us, most of it filling, draining and
+// joining.
 // An item is 256 rows (query x head of the kv-head) of a unit, two 128-row
 // tiles of S = Q K^T and O = P V on tcgen05 (fp16 in, fp32 in tensor memory),
 // against tiles of 128 tokens.  Codes cannot be operands beside 16-bit
@@ -17,8 +21,11 @@
 // one thread issues products, in the order P0 V, Q0 K', P1 V, Q1 K' (K' the
 // next tile), so that one row tile's softmax runs beside the other's products;
 // one warp loads.  A row's reference M follows its maximum when that has grown
-// by more than a factor of two; only then O is scaled, in tensor memory, which
-// is idle for this row tile while its softmax runs.
+// by more than 2^8; only then O is scaled, in tensor memory, which is idle for
+// this row tile while its softmax runs.  (The weights lie between 2^7 and 2^15
+// at most and may lie 2^31 below before they vanish.)  The roles' code runs at
+// the same time and shares the instruction cache: what runs once an item or on
+// its last tiles only is rolled (555 us for 647 with straight-line code there).
 //
 // Tiles are dealt out and cut items joined as in cache_attend.cu.
 #include <cmath>

@@ -9,8 +9,8 @@
 // less than a second launch as long as the units' lengths are a few hundred
 // kilobytes, and needs no scratch and no atomics: the ring is handed out in
 // the units' order whatever the blocks' timing.  A step of 448 units takes 4.9
-// us, 4.2M slots of 16384 units 18 (a third each for the sums, which are bound
-// by instructions, the scan and the slots); a caller's launch costs about as
+// us, 4.2M slots of 16384 units 18 (half of it the slots, the rest the sums and
+// the scan, all bound by instructions and latencies); a call costs about as
 // much on the host.
 #include "bacon.h"
 #include "cache.h"

@@ -9,8 +9,8 @@
 // one exponential per logit and no multiplication by V's scale.  Codes of
 // either format are exact in fp16, and so is a query row scaled by a power of
 // two (kQueryTop), so the products are exact and only w is rounded, to fp16's
-// 11 bits, the largest at 2^kWeightTop so that it may lie 2^38 below.  Sums
-// are fp32.
+// 11 bits, the largest at 2^kWeightTop so that it may lie 2^38 below (the kernel
+// of many queries lets M lag and has its own).  Sums are fp32.
 #pragma once
 
 #include <cuda.h>

@@ -2,8 +2,8 @@
 // or a prompt over a cache.
 //
 // Bound by the tensor cores: 4 d flops for every query head and token it sees.
-// 4096 queries over 16384 tokens (28 / 4 heads of 128) take 555 us, 1517 TFLOP/s,
-// 79 % of the measured burst rate of a library product; 100 queries each of
+// 4096 queries over 16384 tokens (28 / 4 heads of 128) take 556 us, 1514 TFLOP/s,
+// 78 % of the measured burst rate of a library product; 100 queries each of
 // three requests over 2000 tokens 31 us, most of it filling, draining and
 // joining.
 // An item is 256 rows (query x head of the kv-head) of a unit, two 128-row

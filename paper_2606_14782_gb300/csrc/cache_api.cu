@@ -109,7 +109,7 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
         sc.arrived = reinterpret_cast<int*>(sc.many_sums + many_sum_bytes / sizeof(float2));
         sc.many_arrived = sc.arrived + blocks;
         g.err = sc.many_arrived + 2 * (size_t)sc.sms;
-        e = cudaMemset(sc.arrived, 0, word_bytes);
+        e = clear_now(sc.arrived, word_bytes);
     }
     if (e != cudaSuccess) {
         bacon_cache_destroy(c);
@@ -261,15 +261,19 @@ bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream)
     g_last_error.clear();
     if (!cache) return fail(BACON_EINVAL, "null cache");
     DeviceGuard dg(cache->device);
-    BACON_CUDA(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)), "stream synchronisation");
+    // all of it on the caller's stream, which the next call on it follows
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
     int flag = 0;
-    BACON_CUDA(cudaMemcpy(&flag, cache->g.err, sizeof(int), cudaMemcpyDeviceToHost), "error flag read");
+    BACON_CUDA(cudaMemcpyAsync(&flag, cache->g.err, sizeof(int), cudaMemcpyDeviceToHost, st),
+               "error flag read");
+    BACON_CUDA(cudaStreamSynchronize(st), "stream synchronisation");
     if (!flag) return BACON_OK;
-    // cleared before it is reported, so that the next call starts clean; a
-    // block that gave up may have left counts of parts behind
-    BACON_CUDA(cudaMemset(cache->sc.arrived, 0,
-                          (const char*)(cache->g.err + 1) - (const char*)cache->sc.arrived),
+    // cleared before it is reported, so that the next call starts clean on
+    // whichever stream; a block that gave up may have left counts of parts behind
+    BACON_CUDA(cudaMemsetAsync(cache->sc.arrived, 0,
+                               (const char*)(cache->g.err + 1) - (const char*)cache->sc.arrived, st),
                "error flag reset");
+    BACON_CUDA(cudaStreamSynchronize(st), "stream synchronisation");
     if (flag == kCacheBadIndex)
         return fail(BACON_EINVAL, "a length, slot, page or query range was outside its array");
     if (flag == kCacheNoPages) return fail(BACON_ENOMEM, "the ring holds too few pages");

@@ -1,5 +1,5 @@
 // Host-side helpers of the C ABI: the calling thread's last message, argument
-// checks and the device of a call.
+// checks, the device of a call and words that kernels of any stream rely on.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -40,5 +40,20 @@ struct DeviceGuard {
         if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
     }
 };
+
+// Zeros `bytes` bytes of the current device's memory before it returns, without
+// waiting for other work: on a stream of its own, since the default stream has
+// whatever the caller put there, and what it runs late is late for every stream
+// that does not wait for it.
+inline cudaError_t clear_now(void* p, size_t bytes)
+{
+    cudaStream_t own;
+    cudaError_t e = cudaStreamCreateWithFlags(&own, cudaStreamNonBlocking);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(p, 0, bytes, own);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(own);
+    const cudaError_t d = cudaStreamDestroy(own);
+    return e != cudaSuccess ? e : d;
+}
 
 }  // namespace bacon

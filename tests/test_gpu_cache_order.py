@@ -1,0 +1,79 @@
+"""The 8-bit cache on streams that nothing orders: a cache made while the
+default stream is busy serves a stream of its own at once."""
+
+import pytest
+import torch
+
+from paper_2606_14782_gb300 import bacon, build
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    build.build()
+    bacon.load()
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def served(asked):
+    """A cache with some thousand tokens a unit, so that items are cut, and a
+    layer's queries over it."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    R, H, G, d, page, held = 2, 2, 4, 64, 16, 3000
+    blocks = -(-held // page)
+    cache = bacon.Cache(1, H, H * G, d, R * H * blocks, page=page, max_requests=R, max_blocks=blocks)
+    lengths, table, ring, state = cache.tables(R)
+    n = R * H * held
+    slots, lengths, _ = cache.plan(lengths, torch.full_like(lengths, held), table, ring, state, n)
+    rows = [torch.randn(n, d, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    cache.store(*rows, slots)
+    q = torch.randn(R * asked, H * G, d, generator=gen, device="cuda").to(torch.bfloat16)
+    return cache, q, lengths, table
+
+
+def over(cache):
+    return bacon.Cache(1, cache.kv_heads, cache.q_heads, cache.head_dim, cache.pages,
+                       page=cache.page, max_requests=cache.max_requests,
+                       max_blocks=cache.max_blocks, k=cache.k, v=cache.v, k_scale=cache.k_scale,
+                       v_scale=cache.v_scale)
+
+
+@pytest.mark.parametrize("asked", [1, 90])  # either kernel
+def test_a_new_cache_on_a_side_stream(asked):
+    cache, q, lengths, table = served(asked)
+    want, lse = cache.attend(0, q, lengths, table, lse=True)
+    out, z = torch.empty_like(want), torch.empty_like(lse)
+    side = torch.cuda.Stream()
+    cache.sync()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(300_000_000)  # about 0.15 s of the default stream
+    fresh = over(cache)
+    for _ in range(3):
+        fresh.attend(0, q, lengths, table, out=out, lse=z, stream=side)
+    fresh.sync(side)
+    assert torch.equal(out, want) and torch.equal(z, lse)
+    torch.cuda.synchronize()
+
+
+def test_a_reported_error_is_gone_for_another_stream():
+    cache, q, lengths, table = served(1)
+    want = cache.attend(0, q, lengths, table)
+    cache.sync()
+    bad = table.clone()
+    bad[0, 0, 0, 0] = cache.pages
+    out = torch.empty_like(want)
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(300_000_000)
+    cache.attend(0, q, lengths, bad, out=out, stream=first)
+    with pytest.raises(bacon.BaconError) as e:
+        cache.sync(first)
+    assert e.value.status == bacon.BACON_EINVAL
+    cache.attend(0, q, lengths, table, out=out, stream=second)
+    cache.sync(second)
+    assert torch.equal(out, want)
+    torch.cuda.synchronize()

@@ -676,9 +676,10 @@ template <int FORMAT, int D, int NT, int CG>
 cudaError_t go(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
 {
     using S = Sizes<D, NT, CG>;
-    static const cudaError_t ready = cudaFuncSetAttribute(
+    // (at every call: it belongs to the device)
+    const cudaError_t e = cudaFuncSetAttribute(
         few_kernel<FORMAT, D, NT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
-    if (ready != cudaSuccess) return ready;
+    if (e != cudaSuccess) return e;
     static_assert(S::kPerSm <= kBlocksPerSm, "room for partial sums");
     return launch_first(few_kernel<FORMAT, D, NT, CG>, sc.sms * S::kPerSm, S::kThreads, S::kBytes, st,
                         sc.kmap, sc.vmap, g, a, sc);

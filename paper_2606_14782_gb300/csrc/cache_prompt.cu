@@ -877,9 +877,10 @@ template <int FORMAT, int D>
 cudaError_t go(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc, cudaStream_t st)
 {
     constexpr int bytes = Smem<D>::kBytes;
-    static const cudaError_t ready = cudaFuncSetAttribute(
+    // (at every call: it belongs to the device)
+    const cudaError_t e = cudaFuncSetAttribute(
         many_kernel<FORMAT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (ready != cudaSuccess) return ready;
+    if (e != cudaSuccess) return e;
     return launch_first(many_kernel<FORMAT, D>, sc.sms, kThreads, bytes, st, sc.kmap, sc.vmap, g, a, sc);
 }
 

@@ -690,7 +690,7 @@ bacon_status bacon_init(bacon_ctx** out, int layers, int kv_heads, int q_heads, 
     if (e == cudaSuccess) e = dalloc(&c->taken, c->unit_cap * (((size_t)prm.max_seq_len + 7) / 8));
     if (e == cudaSuccess) e = dalloc(&c->key_range, c->unit_cap);
     if (e == cudaSuccess) e = dalloc(&c->err, 1);
-    if (e == cudaSuccess) e = cudaMemset(c->err, 0, sizeof(int));
+    if (e == cudaSuccess) e = clear_now(c->err, sizeof(int));
     if (e == cudaSuccess) e = dalloc(&c->d_maps, 2 * (size_t)kMaxPairs);
     if (e == cudaSuccess)
         e = cudaHostAlloc(reinterpret_cast<void**>(&c->h_maps), 2 * kMaxPairs * sizeof(CUtensorMap),
@@ -1250,13 +1250,17 @@ bacon_status bacon_sync(bacon_ctx* ctx, bacon_stream stream)
 {
     if (!ctx) return fail(BACON_EINVAL, "null context");
     DeviceGuard dg(ctx->device);
-    BACON_CUDA(cudaStreamSynchronize(static_cast<cudaStream_t>(stream)), "stream synchronisation");
+    // all of it on the caller's stream, which the next call on it follows
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
     int flag = 0;
-    BACON_CUDA(cudaMemcpy(&flag, ctx->err, sizeof(int), cudaMemcpyDeviceToHost), "error flag read");
+    BACON_CUDA(cudaMemcpyAsync(&flag, ctx->err, sizeof(int), cudaMemcpyDeviceToHost, st),
+               "error flag read");
+    BACON_CUDA(cudaStreamSynchronize(st), "stream synchronisation");
     if (flag) {
         // the word is cleared before the latched error is reported, so that
-        // the context's next call starts clean
-        BACON_CUDA(cudaMemset(ctx->err, 0, sizeof(int)), "error flag reset");
+        // the context's next call starts clean on whichever stream
+        BACON_CUDA(cudaMemsetAsync(ctx->err, 0, sizeof(int), st), "error flag reset");
+        BACON_CUDA(cudaStreamSynchronize(st), "stream synchronisation");
         if (flag == 1) return fail(BACON_EINVAL, "a gather index was outside [0, seq_len)");
         if (flag == 3) return fail(BACON_ETIMEOUT, "a window-score kernel timed out waiting on its pipeline");
         if (flag == 2)

@@ -35,6 +35,8 @@ def library(folder):
         bacon.LIB_PATH, bacon._lib = kept
     bound.fake_last_allocation.restype = ctypes.c_void_p
     bound.fake_last_allocation.argtypes = [ctypes.POINTER(ctypes.c_size_t)]
+    bound.fake_allocation_of.restype = ctypes.c_void_p
+    bound.fake_allocation_of.argtypes = [ctypes.c_size_t]
     bound.fake_device_work.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int]
     bound.fake_device_work.restype = None
     return bound

@@ -65,6 +65,17 @@ void* fake_last_allocation(size_t* bytes)
     *bytes = g_last ? g_memory[g_last].first : 0;
     return g_last;
 }
+// The only allocation of this size; null when there is none or several.
+void* fake_allocation_of(size_t bytes)
+{
+    void* found = nullptr;
+    for (auto& m : g_memory)
+        if (m.second.first == bytes) {
+            if (found) return nullptr;
+            found = m.first;
+        }
+    return found;
+}
 int fake_launches(int device) { return g_launches[device]; }
 void fake_fail_attributes(int calls) { g_attribute_failures = calls; }
 void fake_device_work(cudaStream_t s, int* word, int value)

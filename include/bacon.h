@@ -400,10 +400,11 @@ typedef struct {
 /* Creates a cache over the caller's pools on the current device: holds the
  * split attention's scratch (about 55 MB) and the error word.  For tests of
  * failure detection only: when the environment variable BACON_FAULT is
- * "missing_page" at this call, the cache's next attention withholds one load
- * of 16 rows, its bounded pipeline waits run out and bacon_cache_sync reports
- * BACON_ETIMEOUT (nothing faults; that call's outputs are undefined, the
- * cache stays usable). */
+ * "missing_page", or "missing_page:<tile>", at this call, the cache's next
+ * attention withholds one load of 16 rows of its first block's first tile, or
+ * of tile <tile> if it has that many, its bounded pipeline waits run out and
+ * bacon_cache_sync reports BACON_ETIMEOUT (nothing faults; that call's outputs
+ * are undefined, the cache stays usable). */
 bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc);
 void bacon_cache_destroy(bacon_cache* cache);
 

@@ -63,7 +63,7 @@ struct AttendArgs {
     float scale;
     uint16_t* out;
     float* lse;
-    int fault;              // test only: one load is withheld
+    int fault;              // test only: > 0 withholds a load of block 0's tile fault - 1
     long long above, upto;  // requests with more than `above` and at most `upto` rows
                             // (queries x heads of a kv-head) are the kernel's
 };

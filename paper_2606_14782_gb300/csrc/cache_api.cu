@@ -14,7 +14,7 @@ using namespace bacon;
 struct bacon_cache {
     int device = 0;
     int max_requests = 0;
-    int fault_pending = 0;  // test-only fault injection (BACON_FAULT=missing_page)
+    int fault_pending = 0;  // test-only fault injection (BACON_FAULT=missing_page[:tile])
     CacheGeom g{};
     SplitScratch sc{};
 };
@@ -122,7 +122,11 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
         return fail(BACON_ECUDA, "cuTensorMapEncodeTiled failed");
     }
     const char* const fault = std::getenv("BACON_FAULT");
-    c->fault_pending = fault && std::strcmp(fault, "missing_page") == 0;
+    if (fault && std::strcmp(fault, "missing_page") == 0) c->fault_pending = 1;
+    if (fault && std::strncmp(fault, "missing_page:", 13) == 0) {
+        const int tile = std::atoi(fault + 13);
+        if (tile >= 0 && tile < 1 << 30) c->fault_pending = tile + 1;
+    }
     *out = c;
     return BACON_OK;
 }

@@ -144,9 +144,20 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
         int unit = place.unit;
         Item it = sh.found.it;
         long long at = place.at;  // the item's first tile
-        int stage = 0, issued = 0, items = 0;
+        // tiles, counted so that the one whose load a test withholds is tile 0
+        const int from = a.fault ? 1 - a.fault : 0;
+        int stage = 0, issued = from, items = 0;
         uint32_t phase = 0;
         bool stop = false;
+        // Nothing is asked for once the block has given up: warps that did go on
+        // freeing stages, also one whose load never came and whose barrier is
+        // still open.  (The flag is set before the stage is freed; to have those
+        // warps keep such a stage instead costs a register where there is none:
+        // 26.4 us for 25.5.)  One answer for the warp, whose lanes vote below.
+        auto gone = [&](uint32_t bar, uint32_t parity) {
+            const bool there = mbar_wait(bar, parity, abort_flag) && !ld_shared_volatile(abort_flag);
+            return !__all_sync(0xFFFFFFFFu, there);
+        };
         long long t = lo;
         while (t < hi && !stop) {
             const int begin = (int)(t - at), end = (int)min((long long)it.tiles, hi - at);
@@ -154,7 +165,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 // the item and its query rows, a lane a column
                 const int slot = items & 1;
                 const uint32_t full = smem_u32(&sh.q_full[slot]);
-                if (!mbar_wait(smem_u32(&sh.q_empty[slot]), (items >> 1 & 1) ^ 1, abort_flag)) {
+                if (gone(smem_u32(&sh.q_empty[slot]), (items >> 1 & 1) ^ 1)) {
                     stop = true;
                     break;
                 }
@@ -210,7 +221,7 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 page1 = checked(page1);
                 const float s1 = scales[page1];
                 const uint32_t full = smem_u32(&sh.full[stage]);
-                if (!mbar_wait(smem_u32(&sh.empty[stage]), phase ^ 1, abort_flag)) {
+                if (gone(smem_u32(&sh.empty[stage]), phase ^ 1)) {
                     stop = true;
                     break;
                 }
@@ -254,17 +265,18 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
                 set_block<kColumns, kTile>(g, a, it, it.block + 1);
             }
         }
-        if (stop) {
-            // the block's copies end before it does
-            if (lane == 0) {
-                st_shared_volatile(abort_flag, 1);
-                atomicCAS(g.err, 0, kCacheTimeout);
-            }
-            for (int i = max(0, issued - kStages); i < issued; ++i)
-                mbar_wait(smem_u32(&sh.full[i % kStages]), i / kStages & 1, 0);
-            for (int i = max(0, items - 2); i < items; ++i)
-                mbar_wait(smem_u32(&sh.q_full[i & 1]), i >> 1 & 1, 0);
+        if (stop && lane == 0) {
+            st_shared_volatile(abort_flag, 1);
+            atomicCAS(g.err, 0, kCacheTimeout);
         }
+        // The block's copies end before it does, also when those who waited for
+        // them have given up after the last was asked for: the last phase of
+        // each barrier (there, as a rule, by the time the warp gets here).
+        issued -= from;
+        for (int i = max(0, issued - kStages); i < issued; ++i)
+            mbar_wait(smem_u32(&sh.full[i % kStages]), i / kStages & 1, 0);
+        for (int i = max(0, items - 2); i < items; ++i)
+            mbar_wait(smem_u32(&sh.q_full[i & 1]), i >> 1 & 1, 0);
         return;
     }
 

@@ -461,13 +461,6 @@ class State:
 _i32 = torch.int32
 
 
-def _int32(t, shape, what):
-    """The address of a contiguous int32 tensor of this shape on the GPU."""
-    if t.dtype is _i32 and t.shape == shape and t.is_cuda and t.is_contiguous():
-        return t.data_ptr()
-    raise ValueError(f"{what} must be a contiguous int32 cuda tensor of shape {tuple(shape)}")
-
-
 class Cache:
     """Kept rows and the tokens after them in pages of 8-bit values
     (``bacon_cache``): block tables, storing, and attention over them.
@@ -476,7 +469,8 @@ class Cache:
     GPU: lengths [R, layers, kv_heads], table [R, layers, kv_heads,
     max_blocks]; ring [pages] and state [2] hold the free pages.  The pools
     k, v [pages, page, head_dim] uint8 and their scales [pages] fp32 may be
-    given, else they are allocated here."""
+    given, else they are allocated here.  The cache lives on the pools' device,
+    and so must everything that its calls are given."""
 
     def __init__(self, layers, kv_heads, q_heads, head_dim, pages, page=64, format="e4m3",
                  dtype=torch.bfloat16, max_requests=4, max_blocks=None, k=None, v=None,
@@ -491,29 +485,47 @@ class Cache:
         self.max_blocks = (min(pages, ((1 << 31) - 1025) // page) if max_blocks is None
                            else max_blocks)
         codes, scales = (pages, page, head_dim), (pages,)
-        self.k, self.v = (torch.empty(codes, dtype=torch.uint8, device="cuda") if t is None else t
-                          for t in (k, v))
-        self.k_scale, self.v_scale = (torch.empty(scales, device="cuda") if t is None else t
+        given = [t for t in (k, v, k_scale, v_scale) if t is not None]
+        self.device = given[0].device if given else torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
+        self.k, self.v = (torch.empty(codes, dtype=torch.uint8, device=self.device) if t is None
+                          else t for t in (k, v))
+        self.k_scale, self.v_scale = (torch.empty(scales, device=self.device) if t is None else t
                                       for t in (k_scale, v_scale))
         for t, shape, kind in ((self.k, codes, torch.uint8), (self.v, codes, torch.uint8),
                                (self.k_scale, scales, torch.float32),
                                (self.v_scale, scales, torch.float32)):
-            if t.shape != shape or t.dtype is not kind or not t.is_cuda or not t.is_contiguous():
-                raise ValueError(f"a pool must be a contiguous {kind} cuda tensor of shape {shape}")
+            if not t.is_cuda or not self._fits(t, shape, kind):
+                raise ValueError(f"the pools must be on one GPU, contiguous, and this one {kind} of "
+                                 f"shape {shape}")
         desc = CacheDesc(layers, kv_heads, q_heads, head_dim, page, pages, max_requests,
                          self.max_blocks, CACHE_FORMATS[format], CACHE_DTYPES[dtype],
                          self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
                          self.v_scale.data_ptr())
         h = _vp()
-        _check(lib.bacon_cache_create(ctypes.byref(h), ctypes.byref(desc)))
+        with torch.cuda.device(self.device):
+            _check(lib.bacon_cache_create(ctypes.byref(h), ctypes.byref(desc)))
         self.handle, self._lib = h, lib
-        # what every call needs, looked up once
-        self.device, self._index = self.k.device, self.k.device.index
         self._unit, self._row = (layers, kv_heads), (layers, kv_heads, self.max_blocks)
 
+    def _fits(self, t, shape, dtype):
+        """Whether a tensor is contiguous, of this shape and type, on the cache's device."""
+        return (t.dtype is dtype and t.shape == shape and t.get_device() == self._index
+                and t.is_contiguous())
+
+    def _int32(self, t, shape, what):
+        """The address of a contiguous int32 tensor of this shape."""
+        if self._fits(t, shape, _i32):
+            return t.data_ptr()
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)} on "
+                         f"{self.device}")
+
     def _stream(self, stream):
-        return (torch._C._cuda_getCurrentRawStream(self._index) if stream is None
-                else stream.cuda_stream)
+        if stream is None:
+            return torch._C._cuda_getCurrentRawStream(self._index)
+        if stream.device_index != self._index:
+            raise ValueError(f"the stream must be one of {self.device}")
+        return stream.cuda_stream
 
     def close(self):
         if getattr(self, "handle", None):
@@ -557,7 +569,7 @@ class Cache:
         units = (R,) + self._unit
         per_unit = added is not None and added.dim() == 3
         shape = (rows,) if per_unit else (self.layers, rows, self.kv_heads)
-        p_lengths, p_state = _int32(lengths, units, "lengths"), _int32(state, (2,), "state")
+        p_lengths, p_state = self._int32(lengths, units, "lengths"), self._int32(state, (2,), "state")
         if slots is None:
             slots = torch.empty(shape, dtype=_i32, device=self.device)
         if lengths_out is None:
@@ -566,10 +578,10 @@ class Cache:
             state_out = torch.empty((2,), dtype=_i32, device=self.device)
         _check(self._lib.bacon_cache_plan(
             self.handle, R, p_lengths,
-            None if added is None else _int32(added, units if per_unit else (R,), "added"),
-            per_unit, _int32(table, (R,) + self._row, "table"),
-            _int32(ring, (self.pages,), "ring"), p_state, rows, _int32(slots, shape, "slots"),
-            _int32(lengths_out, units, "lengths_out"), _int32(state_out, (2,), "state_out"),
+            None if added is None else self._int32(added, units if per_unit else (R,), "added"),
+            per_unit, self._int32(table, (R,) + self._row, "table"),
+            self._int32(ring, (self.pages,), "ring"), p_state, rows, self._int32(slots, shape, "slots"),
+            self._int32(lengths_out, units, "lengths_out"), self._int32(state_out, (2,), "state_out"),
             self._stream(stream)))
         return slots, lengths_out, state_out
 
@@ -579,11 +591,11 @@ class Cache:
         R = count.shape[0]
         units = (R,) + self._unit
         if slots is None:
-            slots = torch.empty((rows,), dtype=torch.int32, device=count.device)
+            slots = torch.empty((rows,), dtype=_i32, device=self.device)
         _check(self._lib.bacon_cache_locate(
-            self.handle, R, None if first is None else _int32(first, units, "first"),
-            _int32(count, units, "count"), _int32(table, (R,) + self._row, "table"),
-            rows, _int32(slots, (rows,), "slots"), self._stream(stream)))
+            self.handle, R, None if first is None else self._int32(first, units, "first"),
+            self._int32(count, units, "count"), self._int32(table, (R,) + self._row, "table"),
+            rows, self._int32(slots, (rows,), "slots"), self._stream(stream)))
         return slots
 
     def release(self, done, lengths, table, ring, state, stream=None):
@@ -591,18 +603,19 @@ class Cache:
         R = lengths.shape[0]
         units = (R,) + self._unit
         _check(self._lib.bacon_cache_release(
-            self.handle, R, _int32(done, (R,), "done"), _int32(lengths, units, "lengths"),
-            _int32(table, (R,) + self._row, "table"),
-            _int32(ring, (self.pages,), "ring"), _int32(state, (2,), "state"),
+            self.handle, R, self._int32(done, (R,), "done"), self._int32(lengths, units, "lengths"),
+            self._int32(table, (R,) + self._row, "table"),
+            self._int32(ring, (self.pages,), "ring"), self._int32(state, (2,), "state"),
             self._stream(stream)))
 
     def _rows(self, t, what):
         """(address, token stride, head stride) of rows [T, H, d] or [T, d]."""
         stride = t.stride()
-        if (t.dtype is not self.dtype or not t.is_cuda or t.shape[-1] != self.head_dim
-                or len(stride) not in (2, 3) or stride[-1] != 1):
-            raise ValueError(f"{what} must be {self.dtype} cuda rows of {self.head_dim} values, "
-                             "[tokens, heads, d] or [tokens, d], the last dimension contiguous")
+        if (t.dtype is not self.dtype or t.get_device() != self._index
+                or t.shape[-1] != self.head_dim or len(stride) not in (2, 3) or stride[-1] != 1):
+            raise ValueError(f"{what} must be {self.dtype} rows of {self.head_dim} values on "
+                             f"{self.device}, [tokens, heads, d] or [tokens, d], the last "
+                             "dimension contiguous")
         return t.data_ptr(), stride[0], stride[1] if len(stride) == 3 else 0
 
     def store(self, k, v, slots, stream=None):
@@ -613,7 +626,7 @@ class Cache:
         kp, vp = self._rows(k, "k"), self._rows(v, "v")
         _check(self._lib.bacon_cache_store(
             self.handle, k.shape[0], k.shape[1] if k.dim() == 3 else 1, *kp, *vp,
-            _int32(slots, k.shape[:-1], "slots"), self._stream(stream)))
+            self._int32(slots, k.shape[:-1], "slots"), self._stream(stream)))
 
     def load(self, slots, k_out=None, v_out=None, stream=None):
         """The values of the slots' rows, shape [*slots.shape, d] each."""
@@ -623,10 +636,11 @@ class Cache:
         if v_out is None:
             v_out = torch.empty(shape, dtype=self.dtype, device=self.device)
         for t in (k_out, v_out):
-            if t.shape != shape or t.dtype is not self.dtype or not t.is_contiguous():
-                raise ValueError(f"outputs must be contiguous {self.dtype} of shape {tuple(shape)}")
+            if not self._fits(t, shape, self.dtype):
+                raise ValueError(f"outputs must be contiguous {self.dtype} of shape {tuple(shape)} "
+                                 f"on {self.device}")
         _check(self._lib.bacon_cache_load(self.handle, slots.numel(),
-                                          _int32(slots, slots.shape, "slots"), k_out.data_ptr(),
+                                          self._int32(slots, slots.shape, "slots"), k_out.data_ptr(),
                                           v_out.data_ptr(), self._stream(stream)))
         return k_out, v_out
 
@@ -642,17 +656,16 @@ class Cache:
         qp = self._rows(q, "q")
         if out is None:
             out = torch.empty(shape, dtype=self.dtype, device=self.device)
-        elif out.shape != shape or out.dtype is not self.dtype or not out.is_contiguous():
-            raise ValueError("out must be contiguous and of q's shape and type")
+        elif not self._fits(out, shape, self.dtype):
+            raise ValueError(f"out must be contiguous, of q's shape and type, on {self.device}")
         if lse is True:
             lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
-        elif lse is not None and (lse.shape != shape[:2] or lse.dtype is not torch.float32
-                                  or not lse.is_contiguous()):
-            raise ValueError("lse must be contiguous float32 [tokens, q_heads]")
+        elif lse is not None and not self._fits(lse, shape[:2], torch.float32):
+            raise ValueError(f"lse must be contiguous float32 [tokens, q_heads] on {self.device}")
         _check(self._lib.bacon_cache_attend(
             self.handle, R, layer, shape[0], *qp,
-            None if starts is None else _int32(starts, (R + 1,), "starts"),
-            _int32(lengths, (R,) + self._unit, "lengths"),
-            _int32(table, (R,) + self._row, "table"), bool(causal),
+            None if starts is None else self._int32(starts, (R + 1,), "starts"),
+            self._int32(lengths, (R,) + self._unit, "lengths"),
+            self._int32(table, (R,) + self._row, "table"), bool(causal),
             0.0 if scale is None else scale, out.data_ptr(), _ptr(lse), self._stream(stream)))
         return out if lse is None else (out, lse)

@@ -175,6 +175,22 @@ def _stream_ptr(stream) -> int:
     return stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """An output that a call on `stream` allocates.  It is that stream's memory:
+    memory of the current one may have been freed there with work on it still to
+    run.  The current stream, where the caller goes on with it, is recorded."""
+    if stream is not None and torch.device(device).type == "cuda":
+        here = torch.cuda.current_stream(device)
+        if stream.cuda_stream != here.cuda_stream:
+            if not hasattr(stream, "stream_id"):  # not torch's own: its address is enough
+                stream = torch.cuda.ExternalStream(stream.cuda_stream, device)
+            with torch.cuda.stream(stream):
+                t = torch.empty(shape, dtype=dtype, device=device)
+            t.record_stream(here)
+            return t
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
@@ -244,11 +260,11 @@ class Context:
         kept = min(budget, N)
         shape_o = (R, Ly, self.kv_heads, kept, d)
         if k_out is None:
-            k_out = torch.empty(shape_o, dtype=k.dtype, device=k.device)
+            k_out = _empty(shape_o, k.dtype, k.device, stream)
         if v_out is None:
-            v_out = torch.empty(shape_o, dtype=v.dtype, device=v.device)
+            v_out = _empty(shape_o, v.dtype, v.device, stream)
         if idx_out is None:
-            idx_out = torch.empty(shape_o[:-1], dtype=torch.int32, device=k.device)
+            idx_out = _empty(shape_o[:-1], torch.int32, k.device, stream)
         if not idx_out.is_contiguous():
             raise ValueError("tensors must be contiguous")
         tq, tk, tv, tko, tvo = (_pair_table(t, R * Ly) for t in (qwin, k, v, k_out, v_out))
@@ -264,10 +280,10 @@ class Context:
         N = k.shape[3]
         assert len(layer_budgets) == Ly
         kept = [min(int(b), N) for b in layer_budgets]
-        ko = [[torch.empty((self.kv_heads, kept[l], d), dtype=k.dtype, device=k.device)
+        ko = [[_empty((self.kv_heads, kept[l], d), k.dtype, k.device, stream)
                for l in range(Ly)] for _ in range(R)]
-        vo = [[torch.empty_like(ko[r][l]) for l in range(Ly)] for r in range(R)]
-        ix = [[torch.empty((self.kv_heads, kept[l]), dtype=torch.int32, device=k.device)
+        vo = [[_empty(ko[r][l].shape, k.dtype, k.device, stream) for l in range(Ly)] for r in range(R)]
+        ix = [[_empty((self.kv_heads, kept[l]), torch.int32, k.device, stream)
                for l in range(Ly)] for _ in range(R)]
         pairs = [(r, l) for r in range(R) for l in range(Ly)]
         # (a tensor of other requests or layers is indexed pair by pair)
@@ -291,10 +307,10 @@ class Context:
         N = k.shape[3]
         kept = min(budget, N)
         shape_o = (R, Ly, self.kv_heads, kept, d)
-        k_out = torch.empty(shape_o, dtype=k.dtype, device=k.device) if k_out is None else k_out
-        v_out = torch.empty(shape_o, dtype=v.dtype, device=v.device) if v_out is None else v_out
+        k_out = _empty(shape_o, k.dtype, k.device, stream) if k_out is None else k_out
+        v_out = _empty(shape_o, v.dtype, v.device, stream) if v_out is None else v_out
         if idx_out is None:
-            idx_out = torch.empty(shape_o[:-1], dtype=torch.int32, device=k.device)
+            idx_out = _empty(shape_o[:-1], torch.int32, k.device, stream)
         tq, tk, tv, tl, tko, tvo = (_pair_table(t, R * Ly) for t in (qwin, k, v, lse, k_out, v_out))
         _check(load().bacon_compress_with_lse(self.handle, R, tq, tk, tv, tl, N, budget, tko, tvo,
                                               idx_out.data_ptr(), _stream_ptr(stream)))
@@ -308,10 +324,10 @@ class Context:
         R, Ly, Hq, W, d = qwin.shape
         N = k.shape[3]
         kept = min(budget, N)
-        ko = torch.empty((R, Ly, self.kv_heads * kept, d), dtype=k.dtype, device=k.device)
-        vo = torch.empty_like(ko)
-        ix = torch.empty((R, Ly, self.kv_heads * kept), dtype=torch.int32, device=k.device)
-        counts = torch.empty((R, Ly, self.kv_heads), dtype=torch.int32, device=k.device)
+        ko = _empty((R, Ly, self.kv_heads * kept, d), k.dtype, k.device, stream)
+        vo = _empty(ko.shape, k.dtype, k.device, stream)
+        ix = _empty((R, Ly, self.kv_heads * kept), torch.int32, k.device, stream)
+        counts = _empty((R, Ly, self.kv_heads), torch.int32, k.device, stream)
         tq, tk, tv, tko, tvo, tix = (_pair_table(t, R * Ly) for t in (qwin, k, v, ko, vo, ix))
         _check(load().bacon_compress_adaptive(self.handle, R, tq, tk, tv, N, budget,
                                               float(alpha), tko, tvo, tix, counts.data_ptr(),
@@ -334,11 +350,9 @@ class Context:
             for f, _ in Variant._fields_:
                 setattr(arr[j], f, x.get(f, getattr(self.params, f)))
         if idx_out is None:
-            idx_out = torch.empty((nv, R, Ly, self.kv_heads, kept), dtype=torch.int32,
-                                  device=k.device)
+            idx_out = _empty((nv, R, Ly, self.kv_heads, kept), torch.int32, k.device, stream)
         if lambda_out is None:
-            lambda_out = torch.empty((nv, R, Ly, self.kv_heads), dtype=torch.float32,
-                                     device=k.device)
+            lambda_out = _empty((nv, R, Ly, self.kv_heads), torch.float32, k.device, stream)
         tq, tk = (_pair_table(t, R * Ly) for t in (qwin, k))
         _check(load().bacon_sweep(self.handle, R, tq, tk, N, budget, nv, arr,
                                   idx_out.data_ptr(), lambda_out.data_ptr(),
@@ -371,7 +385,7 @@ class Context:
         """Intermediate per-token arrays of the last whole-step call (fp32)."""
         n = self._last_count(kind)
         if out is None:
-            out = torch.empty(n, dtype=torch.float32, device="cuda")
+            out = _empty(n, torch.float32, "cuda", stream)
         _check(load().bacon_get_scores(self.handle, SCORE_KINDS[kind], out.data_ptr(),
                                        out.numel(), _stream_ptr(stream)))
         return out
@@ -399,9 +413,9 @@ class Context:
         Hkv, N, d = k.shape
         count = idx.shape[-1]
         if k_out is None:
-            k_out = torch.empty((Hkv, count, d), dtype=k.dtype, device=k.device)
+            k_out = _empty((Hkv, count, d), k.dtype, k.device, stream)
         if v_out is None:
-            v_out = torch.empty((Hkv, count, d), dtype=v.dtype, device=v.device)
+            v_out = _empty((Hkv, count, d), v.dtype, v.device, stream)
         _check(load().bacon_compact(self.handle, k.data_ptr(), v.data_ptr(), idx.data_ptr(), N,
                                     count, k_out.data_ptr(), v_out.data_ptr(),
                                     _stream_ptr(stream)))
@@ -443,8 +457,7 @@ class State:
         when scores_out is given or requested (pass True)."""
         N = k.shape[1]
         if scores_out is True:
-            scores_out = torch.empty((self.ctx.kv_heads, N), dtype=torch.float32,
-                                     device=k.device)
+            scores_out = _empty((self.ctx.kv_heads, N), torch.float32, k.device, stream)
         _check(load().bacon_score_layer(self.ctx.handle, self.handle, layer, qwin.data_ptr(),
                                         k.data_ptr(), N, _ptr(scores_out), _stream_ptr(stream)))
         return scores_out
@@ -452,7 +465,7 @@ class State:
     def select(self, budget, N, idx_out=None, stream=None, device="cuda"):
         kept = min(budget, N)
         if idx_out is None:
-            idx_out = torch.empty((self.ctx.kv_heads, kept), dtype=torch.int32, device=device)
+            idx_out = _empty((self.ctx.kv_heads, kept), torch.int32, device, stream)
         _check(load().bacon_select(self.ctx.handle, self.handle, budget, idx_out.data_ptr(),
                                    _stream_ptr(stream)))
         return idx_out
@@ -523,7 +536,7 @@ class Cache:
     def _stream(self, stream):
         if stream is None:
             return torch._C._cuda_getCurrentRawStream(self._index)
-        if stream.device_index != self._index:
+        if getattr(stream, "device_index", self._index) != self._index:
             raise ValueError(f"the stream must be one of {self.device}")
         return stream.cuda_stream
 
@@ -571,11 +584,11 @@ class Cache:
         shape = (rows,) if per_unit else (self.layers, rows, self.kv_heads)
         p_lengths, p_state = self._int32(lengths, units, "lengths"), self._int32(state, (2,), "state")
         if slots is None:
-            slots = torch.empty(shape, dtype=_i32, device=self.device)
+            slots = _empty(shape, _i32, self.device, stream)
         if lengths_out is None:
-            lengths_out = torch.empty(units, dtype=_i32, device=self.device)
+            lengths_out = _empty(units, _i32, self.device, stream)
         if state_out is None:
-            state_out = torch.empty((2,), dtype=_i32, device=self.device)
+            state_out = _empty((2,), _i32, self.device, stream)
         _check(self._lib.bacon_cache_plan(
             self.handle, R, p_lengths,
             None if added is None else self._int32(added, units if per_unit else (R,), "added"),
@@ -591,7 +604,7 @@ class Cache:
         R = count.shape[0]
         units = (R,) + self._unit
         if slots is None:
-            slots = torch.empty((rows,), dtype=_i32, device=self.device)
+            slots = _empty((rows,), _i32, self.device, stream)
         _check(self._lib.bacon_cache_locate(
             self.handle, R, None if first is None else self._int32(first, units, "first"),
             self._int32(count, units, "count"), self._int32(table, (R,) + self._row, "table"),
@@ -632,9 +645,9 @@ class Cache:
         """The values of the slots' rows, shape [*slots.shape, d] each."""
         shape = slots.shape + (self.head_dim,)
         if k_out is None:
-            k_out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            k_out = _empty(shape, self.dtype, self.device, stream)
         if v_out is None:
-            v_out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            v_out = _empty(shape, self.dtype, self.device, stream)
         for t in (k_out, v_out):
             if not self._fits(t, shape, self.dtype):
                 raise ValueError(f"outputs must be contiguous {self.dtype} of shape {tuple(shape)} "
@@ -655,11 +668,11 @@ class Cache:
             raise ValueError(f"q must be [tokens, {self.q_heads}, {self.head_dim}]")
         qp = self._rows(q, "q")
         if out is None:
-            out = torch.empty(shape, dtype=self.dtype, device=self.device)
+            out = _empty(shape, self.dtype, self.device, stream)
         elif not self._fits(out, shape, self.dtype):
             raise ValueError(f"out must be contiguous, of q's shape and type, on {self.device}")
         if lse is True:
-            lse = torch.empty(shape[:2], dtype=torch.float32, device=self.device)
+            lse = _empty(shape[:2], torch.float32, self.device, stream)
         elif lse is not None and not self._fits(lse, shape[:2], torch.float32):
             raise ValueError(f"lse must be contiguous float32 [tokens, q_heads] on {self.device}")
         _check(self._lib.bacon_cache_attend(

@@ -47,6 +47,7 @@ class Tensor:
 class Stream:
     def __init__(self, index=0):
         self.cuda_stream, self.device_index, self.device = 0x77, index, torch.device("cuda", index)
+        self.stream_id = 1
 
 
 class Library:

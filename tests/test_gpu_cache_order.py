@@ -77,3 +77,27 @@ def test_a_reported_error_is_gone_for_another_stream():
     cache.sync(second)
     assert torch.equal(out, want)
     torch.cuda.synchronize()
+
+
+def test_outputs_for_a_side_stream_are_not_the_current_ones_memory():
+    """Freed memory of the current stream, with work on it still to run, is not
+    what a call on another stream writes its outputs to."""
+    cache, *_ = served(1)
+    rows = 200_000  # 25 MB an output
+    slots = torch.arange(rows, dtype=torch.int32, device="cuda") % (cache.pages * cache.page)
+    want = cache.load(slots)
+    side = torch.cuda.Stream()
+    cache.sync()
+    torch.cuda.synchronize()
+    busy = [torch.empty_like(want[0]) for _ in range(2)]
+    freed = {t.data_ptr() for t in busy}
+    torch.cuda._sleep(300_000_000)
+    for t in busy:
+        t.fill_(7)
+    del busy, t
+    got = cache.load(slots, stream=side)
+    assert not freed & {t.data_ptr() for t in got}
+    side.synchronize()
+    torch.cuda.synchronize()
+    # (bit by bit: rows that nobody stored hold anything, NaN too)
+    assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, want))

@@ -464,7 +464,9 @@ bacon_status bacon_cache_load(bacon_cache* cache, int rows, const int32_t* slots
  * (lengths and table include the new ones): query head g of kv-head
  * h = g / (Hq / Hkv).  q row (t, g) starts at element t * q_token_stride +
  * g * q_head_stride (multiples of 8 elements).  Request r has the queries
- * starts[r] .. starts[r + 1]; starts NULL: tokens / requests each.  With
+ * starts[r] .. starts[r + 1], starts[0] = 0 and starts[requests] = tokens
+ * (otherwise, or when one ends before it starts, nothing is attended:
+ * BACON_EINVAL at bacon_cache_sync); starts NULL: tokens / requests each.  With
  * causal != 0, query j of a request with a sees the positions up to
  * n - a + j, else all n.  scale multiplies the logits; 0 means 1/sqrt(d).
  * out is [tokens][Hq][d], lse (may be NULL) fp32 [tokens][Hq] receives the

@@ -101,3 +101,37 @@ def test_outputs_for_a_side_stream_are_not_the_current_ones_memory():
     torch.cuda.synchronize()
     # (bit by bit: rows that nobody stored hold anything, NaN too)
     assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("requests,starts", [
+    (4, [0, 90, 0, 90, 90]), (4, [0, 90, 40, 90, 90]), (3, [0, 60, 30, 90]), (2, [1, 40, 90]),
+    (2, [0, 91, 90]), (2, [0, 40, 89]), (3, [-1, 0, 1, 90]), (2, [0, -2 ** 31, 90]),
+    (24, [0 if r % 2 == 0 else 90 for r in range(24)] + [90])])
+def test_ranges_that_do_not_follow_one_another(requests, starts):
+    """Nothing is attended, and nothing of it is left for the next call, which
+    comes before the error has been asked for."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    H, G, d, page, held, asked = 1, 7, 128, 32, 2500, 90
+    blocks = -(-held // page)
+    cache = bacon.Cache(1, H, H * G, d, requests * H * blocks, page=page, format="int8",
+                        max_requests=requests, max_blocks=blocks)
+    for codes, scale in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
+        codes.copy_(torch.randint(0, 256, codes.shape, generator=gen, device="cuda"))
+        scale.fill_(0.01)
+    table = torch.randperm(requests * H * blocks, generator=gen, device="cuda").int()
+    table = table.view(requests, 1, H, blocks)
+    lengths = torch.full((requests, 1, H), held, dtype=torch.int32, device="cuda")
+    q = torch.randn(asked, H * G, d, generator=gen, device="cuda").to(torch.bfloat16)
+    fine = ints([round(asked * r / requests) for r in range(requests + 1)])
+    want, lse = cache.attend(0, q, lengths, table, starts=fine, lse=True)
+    cache.sync()
+    out, z = torch.full_like(want, 7), torch.full_like(lse, 7)
+    bad = ints(starts)
+    for _ in range(3):
+        cache.attend(0, q, lengths, table, starts=bad, out=out, lse=z)
+    again, y = cache.attend(0, q, lengths, table, starts=fine, lse=True)
+    with pytest.raises(bacon.BaconError) as e:
+        cache.sync()
+    assert e.value.status == bacon.BACON_EINVAL
+    assert bool((out == 7).all()) and bool((z == 7).all())
+    assert torch.equal(again, want) and torch.equal(y, lse)

@@ -185,6 +185,8 @@ few_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUt
 #pragma unroll 1
                     for (int i = 0; i < D * 2; i += 16)
                         *reinterpret_cast<uint4*>(smem + row + i) = make_uint4(0, 0, 0, 0);
+                    // a later item's copy writes the same bytes
+                    fence_proxy_async_smem();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(full);

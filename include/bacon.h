@@ -421,7 +421,11 @@ void bacon_cache_destroy(bacon_cache* cache);
  * are -1.  When the ring holds too few pages (BACON_ENOMEM), or a length is
  * negative or exceeds max_blocks * page, or the tokens exceed `rows`
  * (BACON_EINVAL, both at bacon_cache_sync), nothing is given: lengths_out
- * and state_out repeat the input and every slot is -1. */
+ * and state_out repeat the input and every slot is -1.  A plan of which nothing
+ * is used is undone by going on with its inputs; where some of the tokens are
+ * not kept (rejected drafts), bacon_cache_shorten takes them back.  A length
+ * that is put back by hand leaves its pages in the table, where the next plan
+ * writes others over them. */
 bacon_status bacon_cache_plan(bacon_cache* cache, int requests, const int32_t* lengths,
                               const int32_t* added, int per_unit, int32_t* table,
                               const int32_t* ring, const int32_t* state, int rows,
@@ -439,6 +443,16 @@ bacon_status bacon_cache_locate(bacon_cache* cache, int requests, const int32_t*
  * Nothing changes when an entry is no page or the ring would overflow
  * (BACON_EINVAL at bacon_cache_sync). */
 bacon_status bacon_cache_release(bacon_cache* cache, int requests, const int32_t* done,
+                                 int32_t* lengths, int32_t* table, int32_t* ring,
+                                 int32_t* state, bacon_stream stream);
+
+/* Takes the last fewer[r] tokens of every unit of request r back ([requests],
+ * 0 for none): lengths become smaller, pages that held none of the tokens kept
+ * go back to the ring (units in order, blocks in order) and leave the table.
+ * What stays is untouched, a page's scale too.  Nothing changes when a unit has
+ * fewer tokens than that, a number is negative, an entry is no page or the ring
+ * would overflow (BACON_EINVAL at bacon_cache_sync). */
+bacon_status bacon_cache_shorten(bacon_cache* cache, int requests, const int32_t* fewer,
                                  int32_t* lengths, int32_t* table, int32_t* ring,
                                  int32_t* state, bacon_stream stream);
 

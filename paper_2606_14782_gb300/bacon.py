@@ -31,8 +31,8 @@ EXPORTS = ("bacon_default_params", "bacon_init", "bacon_destroy", "bacon_last_er
            "bacon_compress_layer_budgets", "bacon_pyramid_budgets",
            "bacon_compress_adaptive", "bacon_compress_with_lse", "bacon_sweep",
            "bacon_sync", "bacon_cache_create", "bacon_cache_destroy", "bacon_cache_plan",
-           "bacon_cache_locate", "bacon_cache_release", "bacon_cache_store",
-           "bacon_cache_load", "bacon_cache_attend", "bacon_cache_sync")
+           "bacon_cache_locate", "bacon_cache_release", "bacon_cache_shorten",
+           "bacon_cache_store", "bacon_cache_load", "bacon_cache_attend", "bacon_cache_sync")
 MAX_VARIANTS = 32
 PROFILE_STAGES = ("window_stats", "window_combine", "window_scores", "calibrate_select",
                   "gather")
@@ -135,13 +135,15 @@ def load() -> ctypes.CDLL:
                                      _vp, _vp]
     lib.bacon_cache_locate.argtypes = [_vp, _int, _vp, _vp, _vp, _int, _vp, _vp]
     lib.bacon_cache_release.argtypes = [_vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.bacon_cache_shorten.argtypes = [_vp, _int, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.bacon_cache_store.argtypes = [_vp, _int, _int, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]
     lib.bacon_cache_load.argtypes = [_vp, _int, _vp, _vp, _vp, _vp]
     lib.bacon_cache_attend.argtypes = [_vp, _int, _int, _int, _vp, _i64, _i64, _vp, _vp, _vp,
                                        _int, ctypes.c_float, _vp, _vp, _vp]
     lib.bacon_cache_sync.argtypes = [_vp, _vp]
     for name in ("bacon_cache_create", "bacon_cache_plan", "bacon_cache_locate",
-                 "bacon_cache_release", "bacon_cache_store", "bacon_cache_load",
+                 "bacon_cache_release", "bacon_cache_shorten", "bacon_cache_store",
+                 "bacon_cache_load",
                  "bacon_cache_attend", "bacon_cache_sync",
                  "bacon_sweep", "bacon_compress_with_lse", "bacon_compress_adaptive",
                  "bacon_compress_layer_budgets",
@@ -617,6 +619,18 @@ class Cache:
         units = (R,) + self._unit
         _check(self._lib.bacon_cache_release(
             self.handle, R, self._int32(done, (R,), "done"), self._int32(lengths, units, "lengths"),
+            self._int32(table, (R,) + self._row, "table"),
+            self._int32(ring, (self.pages,), "ring"), self._int32(state, (2,), "state"),
+            self._stream(stream)))
+
+    def shorten(self, fewer, lengths, table, ring, state, stream=None):
+        """Takes the last fewer[r] tokens (fewer [R]; rejected drafts, say) of
+        every unit of request r back, and gives the pages that held no other
+        back, in place."""
+        R = lengths.shape[0]
+        units = (R,) + self._unit
+        _check(self._lib.bacon_cache_shorten(
+            self.handle, R, self._int32(fewer, (R,), "fewer"), self._int32(lengths, units, "lengths"),
             self._int32(table, (R,) + self._row, "table"),
             self._int32(ring, (self.pages,), "ring"), self._int32(state, (2,), "state"),
             self._stream(stream)))

@@ -38,9 +38,11 @@ struct PlanArgs {
     int32_t* state_out;
 };
 cudaError_t launch_cache_plan(const CacheGeom& g, const PlanArgs& a, cudaStream_t st);
+// Pages back to the ring: of requests that are done, or (fewer) of the last
+// tokens of every request's units.
 cudaError_t launch_cache_release(const CacheGeom& g, int units, const int32_t* done,
-                                 int32_t* lengths, int32_t* table, int32_t* ring, int32_t* state,
-                                 cudaStream_t st);
+                                 const int32_t* fewer, int32_t* lengths, int32_t* table,
+                                 int32_t* ring, int32_t* state, cudaStream_t st);
 
 struct StoreArgs {
     int tokens, heads;

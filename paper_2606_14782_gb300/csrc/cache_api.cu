@@ -186,9 +186,24 @@ bacon_status bacon_cache_release(bacon_cache* cache, int requests, const int32_t
     if (!done || !lengths || !table || !ring || !state) return fail(BACON_EINVAL, "null argument");
     const CacheGeom& g = cache->g;
     DeviceGuard dg(cache->device);
-    BACON_CUDA(launch_cache_release(g, requests * g.layers * g.hkv, done, lengths, table, ring,
-                                    state, static_cast<cudaStream_t>(stream)),
+    BACON_CUDA(launch_cache_release(g, requests * g.layers * g.hkv, done, nullptr, lengths, table,
+                                    ring, state, static_cast<cudaStream_t>(stream)),
                "release launch");
+    return BACON_OK;
+}
+
+bacon_status bacon_cache_shorten(bacon_cache* cache, int requests, const int32_t* fewer,
+                                 int32_t* lengths, int32_t* table, int32_t* ring,
+                                 int32_t* state, bacon_stream stream)
+{
+    g_last_error.clear();
+    if (bacon_status rc = check_call(cache, requests)) return rc;
+    if (!fewer || !lengths || !table || !ring || !state) return fail(BACON_EINVAL, "null argument");
+    const CacheGeom& g = cache->g;
+    DeviceGuard dg(cache->device);
+    BACON_CUDA(launch_cache_release(g, requests * g.layers * g.hkv, nullptr, fewer, lengths, table,
+                                    ring, state, static_cast<cudaStream_t>(stream)),
+               "shorten launch");
     return BACON_OK;
 }
 

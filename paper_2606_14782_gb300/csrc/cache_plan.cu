@@ -183,34 +183,38 @@ plan_kernel(PlanGeom g, PlanArgs a, int own, int* err)
     }
 }
 
-// The pages of the finished requests back to the ring, in the units' order:
-// one block, since the lengths that the order is made from are cleared.
+// Pages back to the ring, in the units' order: of the finished requests, or
+// (done null) what holds none but the last fewer[r] tokens of request r's units.
+// One block, since the lengths that the order is made from change.
 __global__ void __launch_bounds__(kPlanThreads)
-release_kernel(PlanGeom g, int units, const int32_t* done, int32_t* lengths, int32_t* table,
-               int32_t* ring, int32_t* state, int* err)
+release_kernel(PlanGeom g, int units, const int32_t* done, const int32_t* fewer, int32_t* lengths,
+               int32_t* table, int32_t* ring, int32_t* state, int* err)
 {
     __shared__ long long s_sum[32];
     __shared__ int s_bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int lh = g.layers * g.hkv;
     const long long most = (long long)g.max_blocks << g.page_log2;
+    // whether a unit gives something back, and the tokens that it keeps of n
+    auto gives = [&](int u) { return done ? done[u / lh] != 0 : fewer[u / lh] != 0; };
+    auto kept = [&](int u, int n) { return done ? 0 : n - fewer[u / lh]; };
     if (tid == 0) s_bad = 0;
     __syncthreads();
     long long total = 0;
     bool bad = false;
     for (int u = warp; u < units; u += kPlanThreads / 32) {
-        if (!done[u / lh]) continue;
+        if (!gives(u)) continue;
         const int n = lengths[u];
-        if (n < 0 || n > most) {
+        if (n < 0 || n > most || (!done && (fewer[u / lh] < 0 || fewer[u / lh] > n))) {
             bad = true;
             continue;
         }
-        const int blocks = blocks_of(n, g.page_log2);
-        for (int b = lane; b < blocks; b += 32) {
+        const int from = blocks_of(kept(u, n), g.page_log2), blocks = blocks_of(n, g.page_log2);
+        for (int b = from + lane; b < blocks; b += 32) {
             const int page = table[(size_t)u * g.max_blocks + b];
             bad |= page < 0 || page >= g.pages;
         }
-        total += blocks;
+        total += blocks - from;
     }
     if (lane == 0) s_sum[warp] = total;
     if (bad) s_bad = 1;
@@ -224,8 +228,10 @@ release_kernel(PlanGeom g, int units, const int32_t* done, int32_t* lengths, int
     long long at = (long long)head + count;
     for (int base = 0; base < units; base += kPlanThreads) {
         const int u = base + tid;
-        const bool leaves = u < units && done[u / lh] != 0;
-        const int blocks = leaves ? blocks_of(lengths[u], g.page_log2) : 0;
+        const bool leaves = u < units && gives(u);
+        const int keeps = leaves ? kept(u, lengths[u]) : 0;
+        const int from = blocks_of(keeps, g.page_log2);
+        const int blocks = leaves ? blocks_of(lengths[u], g.page_log2) - from : 0;
         long long x = blocks;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -238,11 +244,11 @@ release_kernel(PlanGeom g, int units, const int32_t* done, int32_t* lengths, int
         const long long all = warp_sum(s_sum[lane]);
         x += warp_sum(lane < warp ? s_sum[lane] : 0) - blocks;
         for (int b = 0; b < blocks; ++b) {
-            int32_t* const entry = table + (size_t)u * g.max_blocks + b;
+            int32_t* const entry = table + (size_t)u * g.max_blocks + from + b;
             ring[(at + x + b) % g.pages] = *entry;
             *entry = -1;
         }
-        if (leaves) lengths[u] = 0;
+        if (leaves) lengths[u] = keeps;
         at += all;
     }
     if (tid == 0) state[1] = (int)(count + total);
@@ -266,11 +272,11 @@ cudaError_t launch_cache_plan(const CacheGeom& g, const PlanArgs& a, cudaStream_
 }
 
 cudaError_t launch_cache_release(const CacheGeom& g, int units, const int32_t* done,
-                                 int32_t* lengths, int32_t* table, int32_t* ring, int32_t* state,
-                                 cudaStream_t st)
+                                 const int32_t* fewer, int32_t* lengths, int32_t* table,
+                                 int32_t* ring, int32_t* state, cudaStream_t st)
 {
-    return launch_first(release_kernel, 1, kPlanThreads, 0, st, geom_of(g), units, done, lengths,
-                        table, ring, state, g.err);
+    return launch_first(release_kernel, 1, kPlanThreads, 0, st, geom_of(g), units, done, fewer,
+                        lengths, table, ring, state, g.err);
 }
 
 }  // namespace bacon

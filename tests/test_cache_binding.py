@@ -98,6 +98,8 @@ CALLS = {
     "locate": dict(count=(UNITS, I32), table=(TABLE, I32), first=(UNITS, I32), slots=((T,), I32)),
     "release": dict(done=((R,), I32), lengths=(UNITS, I32), table=(TABLE, I32), ring=((PAGES,), I32),
                     state=((2,), I32)),
+    "shorten": dict(fewer=((R,), I32), lengths=(UNITS, I32), table=(TABLE, I32),
+                    ring=((PAGES,), I32), state=((2,), I32)),
     "store": dict(k=((T, H, D), BF16), v=((T, H, D), BF16), slots=((T, H), I32)),
     "load": dict(slots=((T,), I32), k_out=((T, D), BF16), v_out=((T, D), BF16)),
     "attend": dict(q=((T, HQ, D), BF16), lengths=(UNITS, I32), table=(TABLE, I32),

@@ -121,7 +121,7 @@ __device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
 __device__ __forceinline__ float query_scale(float amax, float& back)
 {
     back = 1.0f;
-    if (!(amax > 0.0f && amax <= 3.0e38f)) return 1.0f;
+    if (!(amax > 0.0f && amax < INFINITY)) return 1.0f;
     int e = (int)(__float_as_uint(amax) >> 23) - 127 - kQueryTop;  // a subnormal: at 2^-127
     e = min(max(e, -110), 120);
     back = __uint_as_float((uint32_t)(e + 127) << 23);

@@ -460,7 +460,11 @@ bacon_status bacon_cache_shorten(bacon_cache* cache, int requests, const int32_t
  * t * k_token_stride + h * k_head_stride, the same for v (strides multiples
  * of 8 elements, rows 16-byte aligned); slots is [tokens][heads], so heads is
  * Hkv for token-major rows of one layer and 1 for rows one after the other.
- * The rows of one page must follow one another in tokens and positions.  A
+ * The rows of one page must follow one another in tokens and positions: two
+ * runs of a page in one call would both write its scale and codes.  Rows that
+ * do not follow the row before them in their page are left out and reported
+ * (BACON_EINVAL at bacon_cache_sync); runs of a page with others between them
+ * (rows of several kv-heads in turn with heads = 1, say) are not noticed.  A
  * page that gets its first row has its scale from the new rows; one that is
  * appended to keeps its scale if that holds them, and its older rows are
  * quantised again with the larger scale if not.  Infinities saturate; NaN

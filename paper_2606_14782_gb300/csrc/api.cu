@@ -35,6 +35,7 @@ bacon_status fail(bacon_status st, const char* fmt, ...)
 
 bacon_status cuda_fail(cudaError_t e, const char* what)
 {
+    cudaGetLastError();  // it is reported here, and not again after another library's launch
     return fail(BACON_ECUDA, "%s: %s", what, cudaGetErrorString(e));
 }
 

@@ -113,8 +113,8 @@ bacon_status bacon_cache_create(bacon_cache** out, const bacon_cache_desc* desc)
     }
     if (e != cudaSuccess) {
         bacon_cache_destroy(c);
-        return e == cudaErrorMemoryAllocation ? fail(BACON_ENOMEM, "device allocation failed")
-                                              : cuda_fail(e, "cache creation");
+        const bacon_status rc = cuda_fail(e, "cache creation");
+        return e == cudaErrorMemoryAllocation ? fail(BACON_ENOMEM, "device allocation failed") : rc;
     }
     const long long rows = (long long)g.pages * g.page;
     if (!encode_pool_map(&sc.kmap, g.k, g.d, rows) || !encode_pool_map(&sc.vmap, g.v, g.d, rows)) {

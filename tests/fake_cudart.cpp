@@ -26,7 +26,7 @@ std::map<std::pair<int, const void*>, size_t> g_shared;  // (device, function): 
 std::map<void*, std::pair<size_t, int>> g_memory;        // size, device
 void* g_last = nullptr;
 int g_launches[kDevices];
-int g_attribute_failures = 0;
+int g_attribute_failures = 0, g_malloc_failures = 0;
 cudaError_t g_error = cudaSuccess;
 
 cudaError_t result(cudaError_t e)
@@ -78,6 +78,7 @@ void* fake_allocation_of(size_t bytes)
 }
 int fake_launches(int device) { return g_launches[device]; }
 void fake_fail_attributes(int calls) { g_attribute_failures = calls; }
+void fake_fail_allocations(int calls) { g_malloc_failures = calls; }
 void fake_device_work(cudaStream_t s, int* word, int value)
 {
     g_streams[s].push_back([=] { *word = value; });
@@ -97,6 +98,7 @@ cudaError_t cudaDeviceGetAttribute(int* v, cudaDeviceAttr a, int)
 cudaError_t cudaDeviceSynchronize() { return run_all(), cudaSuccess; }
 cudaError_t cudaMalloc(void** p, size_t n)
 {
+    if (g_malloc_failures > 0 && g_malloc_failures--) return result(cudaErrorMemoryAllocation);
     *p = g_last = std::malloc(n);
     std::memset(*p, 0xAB, n);
     g_memory[*p] = {n, g_device};

@@ -69,14 +69,16 @@ store_kernel(CacheGeom g, StoreArgs a, int window)
         if (i < window + p && t < a.tokens) {
             const int s = slots[t * a.heads], prev = t ? slots[(t - 1) * a.heads] : -1;
             const bool on = (s & (p - 1)) != 0 && prev == s - 1;
-            // a page's rows out of order, or with a gap: two blocks could have
-            // them, so the later ones are left out
-            const bool apart = !on && prev >= 0 && prev >> g.page_log2 == s >> g.page_log2;
             if (s >= 0 && s < limit) {
                 stop = !on;
-                start = !on && !apart && i < window;
-            }
-            if (i < window && (apart || ((s < 0 || s >= limit) && s != -1))) {
+                start = !on && i < window;
+                // a page's rows out of order, or with a gap: two blocks could
+                // have them, so the later ones are left out (prev in s's page)
+                if (start && (unsigned)(prev ^ s) < (unsigned)p) {
+                    start = false;
+                    atomicCAS(g.err, 0, kCacheBadIndex);
+                }
+            } else if (s != -1 && i < window) {
                 atomicCAS(g.err, 0, kCacheBadIndex);
             }
         }

@@ -4,10 +4,11 @@
 // Bound by the pages' bytes: a token of a unit is 2 d bytes for 4 d flops a
 // query head, so with up to 32 columns (query heads of the kv-head x queries)
 // the work is a stream through HBM with two small matrix products beside it.
-// A token of 32 requests over 16384 rows (28 / 4 heads of 128) takes 96 us, 87 %
+// A token of 32 requests over 16384 rows (28 / 4 heads of 128) takes 96 us, 86 %
 // of the measured copy bandwidth; of four requests over 1024, 12 us, which are
 // the launch, the scan, one tile and the joining of 17 parts one after the
-// other.
+// other.  (At head_dim 128 the computing warps' registers do not suffice: 12 to
+// 84 bytes a thread are spilled.)
 // The products are warp-level (m16n8k16, fp16 in, fp32 sums) with the tokens
 // as rows and the columns as n, so that no more than the next 8 columns are
 // padded: S^T = K Q^T, then O^T = V^T P^T.  K and V codes go from shared
@@ -21,9 +22,9 @@
 // its place by a scan of the lengths, so no host synchronisation and no second
 // launch come before; a warp of it loads (16 rows a TMA load, only rows that
 // the item sees, pages and scales on their way ahead), the others compute, each
-// with its own running maximum, and join at the item's end.  An item cut by a block's edge leaves partial
-// sums; the last of its blocks to arrive adds them up in the blocks' order, so
-// the result does not depend on timing.
+// with its own running maximum, and join at the item's end.  An item cut by a
+// block's edge leaves partial sums; the last of its blocks to arrive adds them
+// up in the blocks' order, so the result does not depend on timing.
 #include <cmath>
 
 #include "cache_attend.cuh"
@@ -733,7 +734,10 @@ cudaError_t launch_cache_few(const CacheGeom& g, const AttendArgs& a, const Spli
 // request on average leaves up to 64 with the others (32 requests of 7 to 49
 // rows over 1024 tokens: 52, 70 with the cut at 32), and one that has many
 // lets only what is close to a single token be few (8 requests of 21 to 49
-// rows over 4096: 40, 63 with the cut at 32; 38 now).
+// rows over 4096: 40, 63 with the cut at 32; 39 now).  Where the rule changes it
+// jumps: ragged requests are all few with an average of 32 rows (4 to 60 each;
+// 32 of them over 1024 tokens 69 us, 8 over 4096 67) and mostly many with one of
+// 36 (4 to 68 each; 109 and 74).
 cudaError_t launch_cache_attend(const CacheGeom& g, const AttendArgs& a, const SplitScratch& sc,
                                 cudaStream_t st)
 {

@@ -2,8 +2,8 @@
 // or a prompt over a cache.
 //
 // Bound by the tensor cores: 4 d flops for every query head and token it sees.
-// 4096 queries over 16384 tokens (28 / 4 heads of 128) take 556 us, 1514 TFLOP/s,
-// 78 % of the measured burst rate of a library product; 100 queries each of
+// 4096 queries over 16384 tokens (28 / 4 heads of 128) take 566 us, 1487 TFLOP/s,
+// 77 % of the measured burst rate of a library product; 100 queries each of
 // three requests over 2000 tokens 31 us, most of it filling, draining and
 // joining.
 // An item is 256 rows (query x head of the kv-head) of a unit, two 128-row
@@ -20,12 +20,16 @@
 // them over the logits as the second product's operand; warps 8-11 convert;
 // one thread issues products, in the order P0 V, Q0 K', P1 V, Q1 K' (K' the
 // next tile), so that one row tile's softmax runs beside the other's products;
-// one warp loads.  A row's reference M follows its maximum when that has grown
-// by more than 2^8; only then O is scaled, in tensor memory, which is idle for
-// this row tile while its softmax runs.  (The weights lie between 2^7 and 2^15
-// at most and may lie 2^31 below before they vanish.)  The roles' code runs at
-// the same time and shares the instruction cache: what runs once an item or on
-// its last tiles only is rolled (555 us for 647 with straight-line code there).
+// one warp loads.  A row's reference M follows its maximum only when that has
+// grown by more than 2^8 (published as conditional, or lazy, rescaling of a
+// running softmax); only then O is scaled, in tensor memory, which is idle for
+// this row tile while its softmax runs.  The largest weight therefore lies
+// between 2^7 and 2^15, and a weight is fp16's normal value down to 2^-21 of it
+// at least, less and less exact below, and may be 0 from 2^-32 on: of n tokens
+// that small, n 2^-32 of the largest weight's share can be lost.  The roles'
+// code runs at the same time and shares the instruction cache: what runs once an
+// item or on its last tiles only is rolled (555 us for 647 with straight-line
+// code there).
 //
 // Tiles are dealt out and cut items joined as in cache_attend.cu.
 #include <cmath>

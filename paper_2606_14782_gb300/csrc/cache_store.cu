@@ -1,7 +1,7 @@
 // Rows into the pages of the 8-bit cache and back: bound by their bytes, three
 // of every element of a row one way or the other.  459k rows of K and V of 128
-// are stored in 60 us and loaded in 51 (87 and 100 % of the measured copy
-// bandwidth).
+// are stored in 62 us and loaded in 54 (84 and 96 % of the measured copy
+// bandwidth); a row of 256 units in 3.0 and 2.1.
 //
 // A run is the rows of one call that lie in one page one after the other.  A
 // block takes a run of K and V: its rows are read once, into registers (2 x 4 x

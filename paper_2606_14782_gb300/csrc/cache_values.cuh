@@ -37,9 +37,10 @@ __device__ __forceinline__ uint32_t e4m3x2_half2(uint16_t c)
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h) : "h"(c));
     return h;
 }
-// Four codes of a word as two pairs of fp16 (exact).  int8: the byte with its
-// sign bit flipped is u = code + 128; beside the byte 0x64 it is the fp16
-// 1024 + u, and 1152 is taken off again.
+// Four codes of a word as two pairs of fp16 (exact).  int8, by the published
+// method of placing an integer in a float's mantissa: the byte with its sign bit
+// flipped is u = code + 128; beside the byte 0x64 it is the fp16 1024 + u, and
+// 1152 is taken off again.
 template <int FORMAT>
 __device__ __forceinline__ void codes_half(uint32_t w, uint32_t& lo, uint32_t& hi)
 {

@@ -140,9 +140,9 @@ __device__ __forceinline__ bool wait(Shared<D>& sh, uint32_t b, uint32_t parity,
     give_up(sh, err);
     return false;
 }
-// The same with one answer for a whole warp, where the next instructions are
-// the warp's: its lanes need not run out of time at once.  (The long turn takes
-// 563 us with it, 558 without.)
+// The same with one answer for a whole warp, whose lanes need not run out of
+// time at once, where they go on together: those left would wait at the next
+// warp barrier for good.  (The long turn takes 563 us with it, 558 without.)
 template <int D>
 __device__ __forceinline__ bool wait_all(Shared<D>& sh, uint32_t b, uint32_t parity, int* err)
 {
@@ -247,8 +247,8 @@ __device__ __forceinline__ void convert_keys(const CacheGeom& g, const Place& p,
     const uint32_t tiles = (uint32_t)(p.hi - p.lo);
     for (uint32_t seq = 0; seq < tiles; ++seq) {
         const int buf = seq & 1;
-        if (!wait(sh, bar(sh.rawk_full), seq & 1, g.err) ||
-            !wait(sh, bar(sh.key_empty[buf]), (seq >> 1 & 1) ^ 1, g.err))
+        if (!wait_all(sh, bar(sh.rawk_full), seq & 1, g.err) ||
+            !wait_all(sh, bar(sh.key_empty[buf]), (seq >> 1 & 1) ^ 1, g.err))
             return;
 #pragma unroll
         for (int half = 0; half < 2; ++half) {

@@ -485,7 +485,9 @@ class Cache:
     max_blocks]; ring [pages] and state [2] hold the free pages.  The pools
     k, v [pages, page, head_dim] uint8 and their scales [pages] fp32 may be
     given, else they are allocated here.  The cache lives on the pools' device,
-    and so must everything that its calls are given."""
+    and so must everything that its calls are given.  A call on another stream
+    than the current one (stream=) runs when that stream gets to it: its inputs
+    have to be complete there, and are the caller's to keep until it has run."""
 
     def __init__(self, layers, kv_heads, q_heads, head_dim, pages, page=64, format="e4m3",
                  dtype=torch.bfloat16, max_requests=4, max_blocks=None, k=None, v=None,

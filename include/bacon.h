@@ -381,7 +381,11 @@ typedef enum {
     BACON_INT8 = 1  /* scale: amax / 127 rounded up to 8 significant bits    */
 } bacon_cache_format; /* either scale is at least 2^-60 */
 
-typedef enum { BACON_BF16 = 0, BACON_FP16 = 1 } bacon_dtype;
+typedef enum {
+    BACON_BF16 = 0,
+    BACON_FP16 = 1,
+    BACON_FP32 = 2 /* rotary rows, norms and logits; not the cache */
+} bacon_dtype;
 
 typedef struct {
     int layers, kv_heads, q_heads, head_dim; /* head_dim 64 or 128            */
@@ -497,6 +501,183 @@ bacon_status bacon_cache_attend(bacon_cache* cache, int requests, int layer, int
 
 /* Wait for the stream and report any error latched by these kernels. */
 bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream);
+
+/* ------------------------------------------------------------------------
+ * What a decoding program does with a token between its matrix products and
+ * the cache: positions into Q and K, the norms between blocks, the rules on
+ * the logits.  The paper takes Q and K after their positions (Sec. 4.1) and
+ * leaves the rest to the model.  All calls are asynchronous on `stream`, may be
+ * captured, allocate nothing and, but for bacon_logits, which belongs to the
+ * device it was made on, run on the current device. */
+
+/* Rotary positions.  A row x of head_dim values is turned in pairs: pair i
+ * < rotary_dim / 2 by the angle p theta_i, p the token's position on axis
+ * axis_i,
+ *   (x_a, x_b) -> A (x_a cos - x_b sin, x_b cos + x_a sin),
+ * with (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) interleaved; values
+ * from rotary_dim on stay.  Angles are exact to 2^-32 of a turn at every int32
+ * position, negative ones too.  A row moves from position p to p' by a
+ * turn of p' - p. */
+typedef struct bacon_rotary bacon_rotary;
+#define BACON_MAX_HEAD 256 /* largest head_dim of rotary rows */
+
+typedef enum {
+    BACON_ROPE_PLAIN = 0,     /* theta_i = base^(-2i / rotary_dim)                     */
+    BACON_ROPE_LINEAR = 1,    /* theta_i / factor                                      */
+    BACON_ROPE_BASE = 2,      /* base factor^(rotary_dim / (rotary_dim - 2)) for base  */
+    BACON_ROPE_ROTATIONS = 3, /* s theta_i + (1 - s) theta_i / factor, s rising with the
+                                 rotations original theta_i / 2 pi from 0 at `low` to 1
+                                 at `high`                                             */
+    BACON_ROPE_DIMS = 4       /* the same with s falling along i from 1 at the pair that
+                                 turns `high` times (rounded down) to 0 at the one
+                                 that turns `low` times (rounded up)                   */
+} bacon_rope_scaling;
+
+/* Frequencies theta [rotary_dim / 2], in radians a position.  Host only.
+ * `original` is the length that the frequencies were trained for (the last two
+ * kinds only). */
+bacon_status bacon_rotary_frequencies(int rotary_dim, double base, int scaling, double factor,
+                                      double original, double low, double high, double* out);
+
+/* A rotation of rows of head_dim values (even, at most BACON_MAX_HEAD), from a
+ * HOST array of rotary_dim / 2 finite frequencies; axis: HOST array of the same
+ * length of values in [0, 3), or NULL for one axis.  `amplitude` is A.  Holds no
+ * device memory and may be used from several threads and on any device. */
+bacon_status bacon_rotary_create(bacon_rotary** out, int head_dim, int rotary_dim, int interleaved,
+                                 float amplitude, const double* frequencies, const uint8_t* axis);
+void bacon_rotary_destroy(bacon_rotary* rotary);
+
+/* Rows (r, t, h): request r, token t, head h; strides in elements, any that
+ * are not negative; each row contiguous.  `out` may be `in` with the same
+ * strides (what the call leaves as it is is not touched then); otherwise they
+ * must not overlap, and no two rows of `out` may. */
+typedef struct {
+    const void* in;
+    void* out;
+    const void* weight; /* [head_dim] of a norm before the rotation, or NULL: no norm */
+    int heads;
+    long long in_request, in_token, in_head;
+    long long out_request, out_token, out_head;
+} bacon_rows;
+
+/* Positions into the rows of Q and K (either may be NULL), [requests][tokens]
+ * of each, positions int32 [axes][requests][tokens] with one axis, or three
+ * when the handle's axis array says so.  With a weight each row becomes
+ * x / sqrt(mean x^2 + eps) (weight_offset + weight) first.  Sums are fp32 and a
+ * row is rounded once.  transposed != 0 turns by the negative angles (A stays):
+ * the gradient of the call, and for A = 1 its inverse; it takes no weights.
+ * eps >= 1e-20.  The widest accesses are used where rows start at multiples
+ * of 16 bytes and the pairs allow it (rotary_dim a multiple of 16, or
+ * interleaved); other rows are right and slower. */
+bacon_status bacon_rotary_apply(const bacon_rotary* rotary, int requests, int tokens,
+                                const bacon_rows* q, const bacon_rows* k, int dtype,
+                                int weight_dtype, float eps, float weight_offset, int transposed,
+                                const int32_t* positions, bacon_stream stream);
+
+/* bacon_rotary_apply for Q (may be NULL) and K, and bacon_cache_store of the
+ * turned K and of V, in one launch and with the same results bit for bit.  Rows
+ * are [tokens][heads] with the strides of one request; k has as many heads as
+ * slots has columns, and k->out is not used.  K and V as in bacon_cache_store;
+ * Q and K of the cache's dtype and head_dim. */
+bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* rotary, int tokens,
+                                       const bacon_rows* q, const bacon_rows* k, const void* v,
+                                       long long v_token_stride, long long v_head_stride,
+                                       int weight_dtype, float eps, float weight_offset,
+                                       const int32_t* positions, const int32_t* slots,
+                                       bacon_stream stream);
+
+/* Between two blocks.  Per token, over `width` channels:
+ *   a = post(y) activation(gate)      the block's output, normed and gated
+ *   s = x + scale a                   the residual sum
+ *   n = pre(s)                        what the next block reads
+ * post and pre are norms or nothing; x, gate, their weights and biases may be
+ * NULL, and so may `sum` and `normed` if not wanted (not both).  n is taken of s
+ * before s is rounded.  Norms: (v - mean) / sqrt(var + eps) for LAYER, v /
+ * sqrt(mean v^2 + eps) for RMS, times (weight_offset + weight), plus bias;
+ * statistics in fp32, for any finite values (rows whose squares pass 3e38 are
+ * scaled first).  sum may be x, and normed y, with the same strides. */
+typedef enum { BACON_NORM_NONE = 0, BACON_NORM_RMS = 1, BACON_NORM_LAYER = 2 } bacon_norm_kind;
+typedef enum {
+    BACON_GATE_LINEAR = 0,
+    BACON_GATE_SIGMOID = 1,
+    BACON_GATE_TANH = 2,
+    BACON_GATE_SILU = 3
+} bacon_gate_kind;
+#define BACON_MAX_WIDTH 32768
+
+typedef struct {
+    int tokens, width;       /* width at most BACON_MAX_WIDTH                     */
+    int dtype;               /* bacon_dtype of y, gate and normed                 */
+    int residual_dtype;      /* of x and sum: dtype or BACON_FP32                 */
+    int weight_dtype;        /* of weights and biases: dtype or BACON_FP32        */
+    int post, pre;           /* bacon_norm_kind                                   */
+    int activation;          /* bacon_gate_kind                                   */
+    float scale, eps, weight_offset; /* eps >= 1e-20                              */
+    int gate_channel;        /* 1: gate has a value for each channel, 0: one      */
+    long long gate_token;    /* elements from a token's gate to the next, 0: shared */
+    long long y_token, x_token, sum_token, normed_token; /* the same of rows      */
+    const void *y, *x, *gate;
+    const void *post_weight, *post_bias, *pre_weight, *pre_bias;
+    void *sum, *normed;
+} bacon_block;
+bacon_status bacon_block_norm(const bacon_block* block, bacon_stream stream);
+
+/* Rules on logits.  Each row of `vocab` logits x becomes, in this order,
+ *   x / repetition if x > 0, else x repetition    tokens of the row's history
+ *   x - (frequency count + presence)              tokens of its answer, count times
+ *   x + bias                                      tokens of the row's list
+ *   -inf                                          tokens that the mask leaves out
+ *   x / temperature
+ * in fp32 (each of the first three rounded as written; the last multiplies by
+ * the reciprocal).  The history of a row is the first lengths[row] entries of
+ * line request[row] of `tokens`, the first prompt[row] of them the prompt, the
+ * others the answer; entries outside [0, vocab) count for nothing.  A token that
+ * a list has twice has the last of its biases.  A row whose length is -1 is left
+ * out: nothing of it is read or written. */
+typedef struct bacon_logits bacon_logits;
+#define BACON_MAX_VOCAB 458752
+#define BACON_MAX_BIASES 2047
+#define BACON_MAX_HISTORY 1048575
+
+typedef struct {
+    int rows;
+    int dtype;                  /* bacon_dtype of logits                           */
+    int out_dtype;              /* of out: dtype or BACON_FP32                     */
+    int requests, capacity;     /* tokens [requests][capacity]                     */
+    int biases;                 /* entries of a row's list                         */
+    long long row_stride, out_stride, token_stride; /* elements; out_stride >= vocab */
+    long long mask_stride;      /* words, 0: one mask for all rows                 */
+    const void* logits;
+    void* out;                  /* NULL: not wanted; may be logits (same stride, type) */
+    const int32_t* tokens;      /* NULL: no history                                */
+    const int32_t* request;     /* [rows]; NULL: rows of tokens are the rows'      */
+    const int32_t* prompt;      /* [rows]; NULL: 0                                 */
+    const int32_t* lengths;     /* [rows]; NULL: no history                        */
+    const float* repetition;    /* [rows] >= 1e-30; NULL: 1                        */
+    const float* frequency;     /* [rows] finite; NULL: 0                          */
+    const float* presence;      /* [rows] finite; NULL: 0                          */
+    const float* temperature;   /* [rows] >= 1e-30; NULL: 1                        */
+    const int32_t* bias_tokens; /* [rows][biases], -1: unused; NULL: none          */
+    const float* bias_values;   /* [rows][biases]                                  */
+    const uint32_t* mask;       /* bit v % 32 of word v / 32: token v is allowed   */
+    int32_t* best;    /* [rows] largest x before the temperature, the lowest of equal
+                         ones; -1 if none is above -inf; NaN is never the largest  */
+    float* logprob;   /* [rows] its log-probability after the temperature; -inf for -1 */
+    float* lse;       /* [rows] log sum exp of the row after the temperature       */
+} bacon_logits_rows;
+
+/* A handle for rows of `vocab` logits on the current device (it holds the error
+ * word).  Must not be used from two threads at once; its calls may run on
+ * several streams. */
+bacon_status bacon_logits_create(bacon_logits** out, int vocab);
+void bacon_logits_destroy(bacon_logits* logits);
+bacon_status bacon_logits_process(bacon_logits* logits, const bacon_logits_rows* rows,
+                                  bacon_stream stream);
+/* Wait for the stream and report what a call found wrong in its device arrays
+ * (BACON_EINVAL): a length or prompt outside the history, a request outside
+ * [0, requests), a bias token outside [-1, vocab) (that history or entry is
+ * left out), or a parameter out of its range (taken as if NULL). */
+bacon_status bacon_logits_sync(bacon_logits* logits, bacon_stream stream);
 
 #ifdef __cplusplus
 }

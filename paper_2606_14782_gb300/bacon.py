@@ -8,8 +8,10 @@ is missing, loading it raises.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+import struct
 from array import array
 
 import torch
@@ -32,7 +34,11 @@ EXPORTS = ("bacon_default_params", "bacon_init", "bacon_destroy", "bacon_last_er
            "bacon_compress_adaptive", "bacon_compress_with_lse", "bacon_sweep",
            "bacon_sync", "bacon_cache_create", "bacon_cache_destroy", "bacon_cache_plan",
            "bacon_cache_locate", "bacon_cache_release", "bacon_cache_shorten",
-           "bacon_cache_store", "bacon_cache_load", "bacon_cache_attend", "bacon_cache_sync")
+           "bacon_cache_store", "bacon_cache_load", "bacon_cache_attend", "bacon_cache_sync",
+           "bacon_rotary_frequencies", "bacon_rotary_create", "bacon_rotary_destroy",
+           "bacon_rotary_apply", "bacon_cache_store_rotated", "bacon_block_norm",
+           "bacon_logits_create", "bacon_logits_destroy", "bacon_logits_process",
+           "bacon_logits_sync")
 MAX_VARIANTS = 32
 PROFILE_STAGES = ("window_stats", "window_combine", "window_scores", "calibrate_select",
                   "gather")
@@ -40,6 +46,10 @@ PROFILE_STAGES = ("window_stats", "window_combine", "window_scores", "calibrate_
 
 CACHE_FORMATS = {"e4m3": 0, "int8": 1}
 CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+ROPE_SCALINGS = {None: 0, "linear": 1, "base": 2, "rotations": 3, "dims": 4}
+NORMS = {None: 0, "rms": 1, "layer": 2}
+GATES = {"linear": 0, "sigmoid": 1, "tanh": 2, "silu": 3}
 
 
 class BaconError(RuntimeError):
@@ -71,6 +81,47 @@ class CacheDesc(ctypes.Structure):
                                              "dtype")]
                 + [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")])
 
+
+class Rows(ctypes.Structure):
+    """Mirror of ``bacon_rows``."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("in_", "out", "weight")]
+                + [("heads", ctypes.c_int)]
+                + [(n, ctypes.c_longlong) for n in ("in_request", "in_token", "in_head",
+                                                    "out_request", "out_token", "out_head")])
+
+
+class Block(ctypes.Structure):
+    """Mirror of ``bacon_block``."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("tokens", "width", "dtype", "residual_dtype",
+                                             "weight_dtype", "post", "pre", "activation")]
+                + [(n, ctypes.c_float) for n in ("scale", "eps", "weight_offset")]
+                + [("gate_channel", ctypes.c_int)]
+                + [(n, ctypes.c_longlong) for n in ("gate_token", "y_token", "x_token",
+                                                    "sum_token", "normed_token")]
+                + [(n, ctypes.c_void_p) for n in ("y", "x", "gate", "post_weight", "post_bias",
+                                                  "pre_weight", "pre_bias", "sum", "normed")])
+
+
+class LogitsRows(ctypes.Structure):
+    """Mirror of ``bacon_logits_rows``."""
+    _fields_ = ([(n, ctypes.c_int) for n in ("rows", "dtype", "out_dtype", "requests", "capacity",
+                                             "biases")]
+                + [(n, ctypes.c_longlong) for n in ("row_stride", "out_stride", "token_stride",
+                                                    "mask_stride")]
+                + [(n, ctypes.c_void_p) for n in ("logits", "out", "tokens", "request", "prompt",
+                                                  "lengths", "repetition", "frequency", "presence",
+                                                  "temperature", "bias_tokens", "bias_values",
+                                                  "mask", "best", "logprob", "lse")])
+
+
+def _packer(cls):
+    """Values of a mirror's fields, in order, as its bytes: a call's descriptor
+    in a third of the time that setting the fields takes."""
+    codes = {ctypes.c_int: "i", ctypes.c_float: "f", ctypes.c_longlong: "q", ctypes.c_void_p: "P"}
+    return struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_)).pack
+
+
+_pack_rows, _pack_block, _pack_logits = _packer(Rows), _packer(Block), _packer(LogitsRows)
 
 _lib = None
 _vp = ctypes.c_void_p
@@ -141,10 +192,30 @@ def load() -> ctypes.CDLL:
     lib.bacon_cache_attend.argtypes = [_vp, _int, _int, _int, _vp, _i64, _i64, _vp, _vp, _vp,
                                        _int, ctypes.c_float, _vp, _vp, _vp]
     lib.bacon_cache_sync.argtypes = [_vp, _vp]
+    lib.bacon_rotary_frequencies.argtypes = [_int] + [ctypes.c_double, _int] + [ctypes.c_double] * 4 + [
+        ctypes.POINTER(ctypes.c_double)]
+    lib.bacon_rotary_create.argtypes = [ctypes.POINTER(_vp), _int, _int, _int, ctypes.c_float,
+                                        ctypes.POINTER(ctypes.c_double), ctypes.c_char_p]
+    lib.bacon_rotary_destroy.argtypes = [_vp]
+    lib.bacon_rotary_destroy.restype = None
+    lib.bacon_rotary_apply.argtypes = [_vp, _int, _int, ctypes.c_char_p, ctypes.c_char_p, _int, _int,
+                                       ctypes.c_float, ctypes.c_float, _int, _vp, _vp]
+    lib.bacon_cache_store_rotated.argtypes = [_vp, _vp, _int, ctypes.c_char_p, ctypes.c_char_p, _vp,
+                                              _i64, _i64, _int, ctypes.c_float, ctypes.c_float, _vp,
+                                              _vp, _vp]
+    lib.bacon_block_norm.argtypes = [ctypes.c_char_p, _vp]
+    lib.bacon_logits_create.argtypes = [ctypes.POINTER(_vp), _int]
+    lib.bacon_logits_destroy.argtypes = [_vp]
+    lib.bacon_logits_destroy.restype = None
+    lib.bacon_logits_process.argtypes = [_vp, ctypes.c_char_p, _vp]
+    lib.bacon_logits_sync.argtypes = [_vp, _vp]
     for name in ("bacon_cache_create", "bacon_cache_plan", "bacon_cache_locate",
                  "bacon_cache_release", "bacon_cache_shorten", "bacon_cache_store",
                  "bacon_cache_load",
-                 "bacon_cache_attend", "bacon_cache_sync",
+                 "bacon_cache_attend", "bacon_cache_sync", "bacon_rotary_frequencies",
+                 "bacon_rotary_create", "bacon_rotary_apply", "bacon_cache_store_rotated",
+                 "bacon_block_norm", "bacon_logits_create", "bacon_logits_process",
+                 "bacon_logits_sync",
                  "bacon_sweep", "bacon_compress_with_lse", "bacon_compress_adaptive",
                  "bacon_compress_layer_budgets",
                  "bacon_window_scores_noalloc",
@@ -657,6 +728,35 @@ class Cache:
             self.handle, k.shape[0], k.shape[1] if k.dim() == 3 else 1, *kp, *vp,
             self._int32(slots, k.shape[:-1], "slots"), self._stream(stream)))
 
+    def store_rotated(self, rotary, q, k, v, positions, slots, q_weight=None, k_weight=None,
+                      eps=1e-6, offset=0.0, q_out=None, stream=None):
+        """``rotary.apply`` to q [T, Hq, d] (may be None) and k [T, H, d], and
+        ``store`` of the turned k and of v, in one launch with the same results:
+        positions int32 [T] (or [3, T]), slots [T, H].  Returns the turned q."""
+        if k.shape != v.shape or k.dim() != 3:
+            raise ValueError("k and v must have the same shape [tokens, heads, d]")
+        T = k.shape[0]
+        kp, vp = self._rows(k, "k"), self._rows(v, "v")
+        weights = _weights_dtype((q_weight, k_weight), (self.head_dim,), self.dtype, self._index)
+        rows = None
+        if q is not None:
+            qp = self._rows(q, "q")
+            if q.dim() != 3 or q.shape[0] != T:
+                raise ValueError("q must be [tokens, heads, d], of k's tokens")
+            if q_out is None:
+                q_out = _empty(q.shape, self.dtype, self.device, stream)
+            elif q_out.shape != q.shape:
+                raise ValueError("q_out must have q's shape")
+            op = self._rows(q_out, "q_out")
+            rows = _pack_rows(qp[0], op[0], _ptr(q_weight) or 0, q.shape[1], 0, qp[1], qp[2], 0,
+                              op[1], op[2])
+        _check(self._lib.bacon_cache_store_rotated(
+            self.handle, rotary.handle, T, rows,
+            _pack_rows(kp[0], 0, _ptr(k_weight) or 0, k.shape[1], 0, kp[1], kp[2], 0, 0, 0), *vp,
+            weights, eps, offset, self._int32(positions, rotary.shape(T), "positions"),
+            self._int32(slots, k.shape[:-1], "slots"), self._stream(stream)))
+        return q_out
+
     def load(self, slots, k_out=None, v_out=None, stream=None):
         """The values of the slots' rows, shape [*slots.shape, d] each."""
         shape = slots.shape + (self.head_dim,)
@@ -698,3 +798,370 @@ class Cache:
             self._int32(table, (R,) + self._row, "table"), bool(causal),
             0.0 if scale is None else scale, out.data_ptr(), _ptr(lse), self._stream(stream)))
         return out if lse is None else (out, lse)
+
+
+# ------------------------------------------------------------------------
+# a token between its matrix products and the cache
+
+def _current(index):
+    """The device made current for a call on its tensors, if it is not."""
+    return _same if torch.cuda.current_device() == index else torch.cuda.device(index)
+
+
+_same = contextlib.nullcontext()
+
+
+def _stream_of(stream, index):
+    """The address of a stream of device `index` (None: its current one)."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    if getattr(stream, "device_index", index) != index:
+        raise ValueError(f"the stream must be one of cuda:{index}")
+    return stream.cuda_stream
+
+
+def _weights_dtype(weights, shape, dtype, index):
+    """The type of the weights that there are: the rows' or float32, one for all."""
+    kind = None
+    for w in weights:
+        if w is None:
+            continue
+        if (w.shape != shape or w.get_device() != index or not w.is_contiguous()
+                or w.dtype is not (kind or w.dtype) or w.dtype not in (dtype, torch.float32)):
+            raise ValueError(f"weights must be contiguous, of shape {tuple(shape)}, all {dtype} or "
+                             f"all float32, on cuda:{index}")
+        kind = w.dtype
+    return DTYPES[kind or dtype]
+
+
+class Rotary:
+    """Rotary positions of rows of `head_dim` values (``bacon_rotary``).
+
+    The first `rotary_dim` values (None: all) turn, in pairs (i, i + half) or
+    interleaved (2i, 2i + 1).  Frequencies: base^(-2i / rotary_dim), with
+    `scaling` "linear" (by `factor`), "base" (the base grows), "rotations" or
+    "dims" (pairs that turn fewer than `low` times over `original` positions are
+    scaled, those that turn more than `high` times are not); or the caller's
+    `frequencies` (rotary_dim / 2 radians a position).  `axes`: for each pair the
+    position axis 0, 1 or 2 that it turns with (e.g. time, height, width); None:
+    one axis.  Host memory only: a handle serves every device."""
+
+    def __init__(self, head_dim, rotary_dim=None, base=10000.0, interleaved=False, scaling=None,
+                 factor=1.0, original=0, low=1.0, high=32.0, amplitude=1.0, frequencies=None,
+                 axes=None):
+        self._lib = load()
+        self.head_dim = head_dim
+        self.rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        half = self.rotary_dim // 2
+        table = (ctypes.c_double * max(half, 1))()
+        if frequencies is not None:
+            if len(frequencies) != half:
+                raise ValueError(f"{half} frequencies are needed")
+            table[:half] = [float(f) for f in frequencies]
+        else:
+            if scaling not in ROPE_SCALINGS:
+                raise ValueError(f"scaling must be one of {list(ROPE_SCALINGS)}")
+            _check(self._lib.bacon_rotary_frequencies(self.rotary_dim, base, ROPE_SCALINGS[scaling],
+                                                      factor, original, low, high, table))
+        self.frequencies = list(table)[:half]
+        if axes is not None and (len(axes) != half or not all(x in (0, 1, 2) for x in axes)):
+            raise ValueError(f"axes must be {half} numbers in 0, 1, 2")
+        self.axes = 1 if axes is None else 3
+        h = _vp()
+        _check(self._lib.bacon_rotary_create(ctypes.byref(h), head_dim, self.rotary_dim,
+                                             int(interleaved), amplitude, table,
+                                             None if axes is None else bytes(axes)))
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self._lib.bacon_rotary_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def shape(self, *tokens):
+        """The shape of the positions of tokens of this shape."""
+        return tokens if self.axes == 1 else (3,) + tokens
+
+    def _rows(self, t, out, weight, dtype, index, places, stream, what):
+        """Packed rows and the output (allocated if None)."""
+        stride = t.stride()
+        if (t.dtype is not dtype or t.get_device() != index or t.shape[:-2] != places
+                or t.shape[-1] != self.head_dim or (stride[-1] != 1 and t.numel())):
+            raise ValueError(f"{what} must be {dtype} rows of {self.head_dim} values on cuda:{index}, "
+                             "[tokens, heads, d] or [requests, tokens, heads, d] like the other, "
+                             "the last dimension contiguous")
+        if out is None:
+            out = _empty(t.shape, dtype, t.device, stream)
+        elif (out.dtype is not dtype or out.get_device() != index or out.shape != t.shape
+              or (out.stride(-1) != 1 and t.numel())):
+            raise ValueError(f"the output of {what} must have its shape, type and device, the last "
+                             "dimension contiguous")
+        to = out.stride()
+        many = len(places) == 2
+        return out, _pack_rows(t.data_ptr(), out.data_ptr(), _ptr(weight) or 0, t.shape[-2],
+                               stride[0] if many else 0, stride[-3], stride[-2],
+                               to[0] if many else 0, to[-3], to[-2])
+
+    def apply(self, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, offset=0.0,
+              transposed=False, q_out=None, k_out=None, stream=None):
+        """Positions into q [T, Hq, d] and k [T, H, d], or [R, N, Hq, d] and
+        [R, N, H, d], bf16, fp16 or fp32 of any strides with contiguous rows
+        (either may be None); positions int32, contiguous, [T] or [R, N], with a
+        leading dimension of 3 when there are axes.  With q_weight or k_weight [d]
+        a row is first divided by its root mean square (`eps`) and multiplied by
+        offset + weight.  transposed: by the negative angles, the call's gradient
+        and, for amplitude 1, its inverse.  Outputs may be the inputs, or views
+        such as k_out.transpose(1, 2) of head-major rows.  Returns (q_out,
+        k_out)."""
+        t = k if q is None else q
+        if t is None or not t.is_cuda or t.dim() not in (3, 4) or t.dtype not in DTYPES:
+            raise ValueError("q or k must be bf16, fp16 or fp32 rows on a GPU, [tokens, heads, d] or "
+                             "[requests, tokens, heads, d]")
+        dtype, index, places = t.dtype, t.get_device(), t.shape[:-2]
+        weights = _weights_dtype((q_weight, k_weight), (self.head_dim,), dtype, index)
+        rows = [None, None]
+        if q is not None:
+            q_out, rows[0] = self._rows(q, q_out, q_weight, dtype, index, places, stream, "q")
+        if k is not None:
+            k_out, rows[1] = self._rows(k, k_out, k_weight, dtype, index, places, stream, "k")
+        if (positions.dtype is not _i32 or positions.shape != self.shape(*places)
+                or positions.get_device() != index or not positions.is_contiguous()):
+            raise ValueError("positions must be a contiguous int32 tensor of shape "
+                             f"{tuple(self.shape(*places))} on cuda:{index}")
+        with _current(index):
+            _check(self._lib.bacon_rotary_apply(
+                self.handle, places[0] if len(places) == 2 else 1, places[-1], *rows,
+                DTYPES[dtype], weights, eps, offset, transposed, positions.data_ptr(),
+                _stream_of(stream, index)))
+        return q_out, k_out
+
+
+class BlockNorm:
+    """What lies between two blocks of `width` channels (``bacon_block_norm``):
+    a = post(y) gate(g), s = x + scale a, n = pre(s).
+
+    post, pre: None, "rms" or "layer", with weights and biases [width] (any may be
+    None) in the rows' type or float32; eps is both norms', and both multiply by
+    offset + weight.  gate: "linear", "sigmoid", "tanh" or "silu", of the gate that
+    a call gives.  The object holds the weights and may be used from several
+    threads and streams."""
+
+    def __init__(self, width, pre="rms", post=None, pre_weight=None, pre_bias=None,
+                 post_weight=None, post_bias=None, gate="linear", scale=1.0, eps=1e-6, offset=0.0):
+        if pre not in NORMS or post not in NORMS or gate not in GATES:
+            raise ValueError(f"norms must be of {list(NORMS)}, gate of {list(GATES)}")
+        self._lib = load()
+        self.width, self.pre, self.post = width, pre, post
+        self._kinds = NORMS[post], NORMS[pre], GATES[gate], scale, eps, offset
+        self._weights = post_weight, post_bias, pre_weight, pre_bias
+        given = [w for w in self._weights if w is not None]
+        self._index = given[0].get_device() if given else None
+        if given and not given[0].is_cuda:
+            raise ValueError("weights must be on a GPU")
+        self._dtypes = {}
+        self._pointers = [_ptr(w) or 0 for w in self._weights]
+
+    def _weight_dtype(self, dtype, index):
+        """The weights' type for rows of this type, checked once for each."""
+        if dtype not in self._dtypes:
+            if dtype not in DTYPES:
+                raise ValueError("rows must be bf16, fp16 or fp32")
+            self._dtypes[dtype] = _weights_dtype(self._weights, (self.width,), dtype,
+                                                 index if self._index is None else self._index)
+        return self._dtypes[dtype]
+
+    def _rows(self, t, shape, dtypes, index, what):
+        """The distance of rows [..., width], with the last dimension contiguous
+        and one distance for all rows."""
+        if t.dtype not in dtypes or t.get_device() != index or t.shape != shape:
+            raise ValueError(f"{what} must be of shape {tuple(shape)} and one of {dtypes} on "
+                             f"cuda:{index}")
+        if t.is_contiguous():
+            return self.width
+        stride = t.stride()
+        if stride[-1] == 1 or self.width == 1:
+            flat = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n > 1]
+            if all(s == n * r for (_, s), (n, r) in zip(flat, flat[1:])):
+                return flat[-1][1] if flat else self.width
+        raise ValueError(f"the rows of {what} must be contiguous, and the same distance apart")
+
+    def __call__(self, y, x=None, gate=None, sum_out=None, norm_out=None, stream=None):
+        """y [..., width]; x (the residual) of its shape, in its type or float32;
+        gate of its type: [width], [..., 1] or [..., width].  Returns (sum, normed):
+        the sum in x's type (None for a norm alone: without x, post and gate), normed
+        in y's (None without a pre norm).  sum_out may be x, norm_out y."""
+        shape, dtype, width = y.shape, y.dtype, self.width
+        index = y.get_device()
+        if not y.is_cuda or len(shape) < 1 or shape[-1] != width:
+            raise ValueError(f"y must be [..., {width}] on a GPU")
+        if self._index is not None and self._index != index:
+            raise ValueError(f"the weights are on cuda:{self._index}")
+        weight_dtype = self._weight_dtype(dtype, index)
+        tokens = y.numel() // width
+        strides = [0, self._rows(y, shape, (dtype,), index, "y"), 0, 0, 0]
+        wide = x if x is not None else sum_out
+        residual = dtype if wide is None else wide.dtype
+        if x is not None:
+            strides[2] = self._rows(x, shape, (dtype, torch.float32), index, "x")
+        channel = 0
+        if gate is not None:
+            g = gate.shape
+            if gate.dtype is not dtype or gate.get_device() != index:
+                raise ValueError("the gate must have y's type and device")
+            if g == shape:
+                channel = 1
+                strides[0] = self._rows(gate, shape, (dtype,), index, "gate")
+            elif g == (width,) and gate.is_contiguous():
+                channel = 1
+            elif g == shape[:-1] + (1,) and gate.is_contiguous():
+                strides[0] = 1
+            else:
+                raise ValueError(f"the gate must be contiguous [{width}] or {tuple(shape[:-1])} + "
+                                 "(1,), or have y's shape")
+        if sum_out is not None:
+            strides[3] = self._rows(sum_out, shape, (residual,) if x is not None else
+                                    (dtype, torch.float32), index, "sum_out")
+        elif x is not None or self.post is not None or gate is not None:
+            sum_out = _empty(shape, residual, y.device, stream)
+            strides[3] = width
+        if self.pre is None:
+            if norm_out is not None:
+                raise ValueError("there is no pre norm")
+        elif norm_out is None:
+            norm_out = _empty(shape, dtype, y.device, stream)
+            strides[4] = width
+        else:
+            strides[4] = self._rows(norm_out, shape, (dtype,), index, "norm_out")
+        post, pre, kind, scale, eps, offset = self._kinds
+        desc = _pack_block(tokens, width, DTYPES[dtype], DTYPES[residual], weight_dtype, post, pre,
+                           kind, scale, eps, offset, channel, *strides, y.data_ptr(), _ptr(x) or 0,
+                           _ptr(gate) or 0, *self._pointers, _ptr(sum_out) or 0,
+                           _ptr(norm_out) or 0)
+        with _current(index):
+            _check(self._lib.bacon_block_norm(desc, _stream_of(stream, index)))
+        return sum_out, norm_out
+
+
+class Logits:
+    """Rules on rows of `vocab` logits (``bacon_logits``), on the current device or
+    `device`: penalties, biases, masks, temperature, and the greedy token."""
+
+    def __init__(self, vocab, device=None):
+        self._lib = load()
+        self.vocab = vocab
+        self.device = torch.device("cuda", torch.cuda.current_device() if device is None else
+                                   torch.device(device).index or 0)
+        self._index = self.device.index
+        h = _vp()
+        with torch.cuda.device(self.device):
+            _check(self._lib.bacon_logits_create(ctypes.byref(h), vocab))
+        self.handle = h
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self._lib.bacon_logits_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def sync(self, stream=None):
+        _check(self._lib.bacon_logits_sync(self.handle, _stream_of(stream, self._index)))
+
+    def _fits(self, t, shape, dtype, what):
+        """The address of a contiguous tensor of this shape and type, 0 for None."""
+        if t is None:
+            return 0
+        if (t.dtype is dtype and t.shape == shape and t.get_device() == self._index
+                and t.is_contiguous()):
+            return t.data_ptr()
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on "
+                         f"{self.device}")
+
+    def _lines(self, t, dtypes, rows, least, what):
+        """(address, stride) of [rows, ...] of at least `least` values, each row
+        contiguous; a row may be shared (stride 0) where that is read only."""
+        if (t.dim() != 2 or t.dtype not in dtypes or t.get_device() != self._index
+                or t.shape[0] != rows or t.shape[1] < least or (t.shape[1] > 1 and t.stride(1) != 1)):
+            raise ValueError(f"{what} must be [{rows}, {least}], of {dtypes}, on {self.device}, each "
+                             "row contiguous")
+        return t.data_ptr(), t.stride(0)
+
+    def process(self, logits, tokens=None, lengths=None, prompt=None, request=None,
+                repetition=None, frequency=None, presence=None, temperature=None,
+                bias_tokens=None, bias_values=None, mask=None, out=None, greedy=True, stream=None):
+        """logits [rows, vocab] in bf16, fp16 or fp32.  History: tokens int32
+        [requests, capacity]; of line request[row] (None: the row's own) the first
+        lengths[row] entries, the first prompt[row] of them (None: 0) the prompt; a
+        row of length -1 is left out.  repetition, frequency, presence, temperature:
+        float32 [rows].  bias_tokens int32, bias_values float32 [rows, n] (-1:
+        unused).  mask int32 [rows or 1, ceil(vocab / 32)], a bit for each token
+        that is allowed.  out: None (a new float32 tensor), False (not wanted), or a
+        tensor in float32 or the logits' type, the logits themselves too.  Returns
+        (out, best, logprob, lse), the last three [rows] or, without `greedy`,
+        None."""
+        if logits.dim() != 2 or logits.shape[1] != self.vocab:
+            raise ValueError(f"logits must be [rows, {self.vocab}]")
+        rows, dtype = logits.shape[0], logits.dtype
+        p_logits, stride = self._lines(logits, DTYPES, rows, self.vocab, "logits")
+        p_out = out_stride = 0
+        out_dtype = torch.float32
+        if out is None:
+            out = _empty((rows, self.vocab), torch.float32, self.device, stream)
+            p_out, out_stride = out.data_ptr(), self.vocab
+        elif out is False:
+            out = None
+        else:
+            if out.shape != logits.shape:
+                raise ValueError("out must have the logits' shape")
+            out_dtype = out.dtype
+            p_out, out_stride = self._lines(out, (dtype, torch.float32), rows, self.vocab, "out")
+        each = (rows,)
+        requests = capacity = token_stride = p_tokens = 0
+        if tokens is not None:
+            requests, capacity = tokens.shape
+            p_tokens, token_stride = self._lines(tokens, (_i32,), requests, 0, "tokens")
+        biases = p_bias = p_value = 0
+        if bias_tokens is not None and bias_values is not None:
+            biases = bias_tokens.shape[-1]
+            p_bias = self._fits(bias_tokens, (rows, biases), _i32, "bias_tokens")
+            p_value = self._fits(bias_values, (rows, biases), torch.float32, "bias_values")
+        elif bias_tokens is not None or bias_values is not None:
+            raise ValueError("bias_tokens and bias_values come together")
+        p_mask = mask_stride = 0
+        if mask is not None:
+            one = mask.dim() == 2 and mask.shape[0] == 1
+            p_mask, mask_stride = self._lines(mask, (_i32,), 1 if one else rows,
+                                              -(-self.vocab // 32), "mask")
+            if one:
+                mask_stride = 0
+        best = logprob = lse = None
+        if greedy:
+            best = _empty(each, _i32, self.device, stream)
+            logprob = _empty(each, torch.float32, self.device, stream)
+            lse = _empty(each, torch.float32, self.device, stream)
+        f32, fits = torch.float32, self._fits
+        desc = _pack_logits(
+            rows, DTYPES[dtype], DTYPES[out_dtype], requests, capacity, biases, stride, out_stride,
+            token_stride, mask_stride, p_logits, p_out, p_tokens, fits(request, each, _i32, "request"),
+            fits(prompt, each, _i32, "prompt"), fits(lengths, each, _i32, "lengths"),
+            fits(repetition, each, f32, "repetition"), fits(frequency, each, f32, "frequency"),
+            fits(presence, each, f32, "presence"), fits(temperature, each, f32, "temperature"),
+            p_bias, p_value, p_mask, _ptr(best) or 0, _ptr(logprob) or 0, _ptr(lse) or 0)
+        _check(self._lib.bacon_logits_process(self.handle, desc, _stream_of(stream, self._index)))
+        return out, best, logprob, lse

@@ -52,6 +52,9 @@ struct StoreArgs {
     const int32_t* slots;
 };
 cudaError_t launch_cache_store(const CacheGeom& g, const StoreArgs& a, cudaStream_t st);
+struct RotaryArgs;  // rotary.cuh
+cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a,
+                                       const RotaryArgs& rotary, cudaStream_t st);
 cudaError_t launch_cache_load(const CacheGeom& g, int rows, const int32_t* slots, void* k_out,
                               void* v_out, cudaStream_t st);
 

@@ -8,6 +8,8 @@
 #include "cache.h"
 #include "common.cuh"
 #include "host.h"
+#include "rotary.cuh"
+#include "step_host.h"
 
 using namespace bacon;
 
@@ -225,6 +227,37 @@ bacon_status bacon_cache_store(bacon_cache* cache, int tokens, int heads, const 
                 {k_token_stride, v_token_stride}, {k_head_stride, v_head_stride}, slots};
     DeviceGuard dg(cache->device);
     BACON_CUDA(launch_cache_store(cache->g, a, static_cast<cudaStream_t>(stream)), "store launch");
+    return BACON_OK;
+}
+
+bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* rotary, int tokens,
+                                       const bacon_rows* q, const bacon_rows* k, const void* v,
+                                       long long v_token_stride, long long v_head_stride,
+                                       int weight_dtype, float eps, float weight_offset,
+                                       const int32_t* positions, const int32_t* slots,
+                                       bacon_stream stream)
+{
+    g_last_error.clear();
+    if (!cache) return fail(BACON_EINVAL, "null cache");
+    if (!rotary || !k) return fail(BACON_EINVAL, "null argument");
+    const CacheGeom& g = cache->g;
+    if (tokens < 0 || k->heads < 1 || k->heads > 65535)
+        return fail(BACON_EINVAL, "tokens must not be negative, heads in [1, 65535]");
+    RotaryArgs r;
+    if (bacon_status rc = rotary_args(rotary, 1, tokens, q, k, false, g.dtype, weight_dtype, eps,
+                                      weight_offset, 0, positions, &r))
+        return rc;
+    if (r.table.head_dim != g.d)
+        return fail(BACON_EINVAL, "the rotation is of %d values, rows have %d", r.table.head_dim, g.d);
+    if (tokens == 0) return BACON_OK;
+    if (!slots) return fail(BACON_EINVAL, "null argument");
+    if (bacon_status rc = check_rows(k->in, k->in_token, k->in_head, "k")) return rc;
+    if (bacon_status rc = check_rows(v, v_token_stride, v_head_stride, "v")) return rc;
+    StoreArgs a{tokens, k->heads,
+                {static_cast<const uint16_t*>(k->in), static_cast<const uint16_t*>(v)},
+                {k->in_token, v_token_stride}, {k->in_head, v_head_stride}, slots};
+    DeviceGuard dg(cache->device);
+    BACON_CUDA(launch_cache_store_rotated(g, a, r, static_cast<cudaStream_t>(stream)), "store launch");
     return BACON_OK;
 }
 

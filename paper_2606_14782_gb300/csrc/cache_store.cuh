@@ -52,20 +52,17 @@ __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* r
         const int r = (threadIdx.x + i * blockDim.x) / (D / 8);
         const bool mine = r < len;
         Eight<DTYPE> w{{raw[i].x, raw[i].y, raw[i].z, raw[i].w}};
-        float x[8], other[8], c[8], s[8], y[8];
-        unpack_eight(w, x);
+        Piece x, other, c, s, y;
+        open_piece(w, x);
         pairs_of<DTYPE, PAIR>(tab, w, x, rows + (t + r) * token_stride, mine, q, other);
-        if (mine) {
-            angles_of<PAIR>(tab, t + r, e0, c, s);
-            if (weight)
-                weigh(tab, weight, e0, PAIR == kPairOwn || (PAIR == kPairMemory && tab.interleaved), c, s);
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) c[j] = s[j] = 0.0f;
-        }
+        for (int j = 0; j < 4; ++j) c.p[j] = s.p[j] = 0;
+        if (mine) angles_of<PAIR>(tab, t + r, e0, c, s);
+        if (weight) weigh<DTYPE, PAIR>(tab, weight, q, c, s);
         const float inv = row_inverse(tab, D == 128 ? 4 : 3, weight != nullptr, x, other);
-        turn_eight(x, other, c, s, inv, y);
-        pack_eight(w, y);
+        turn_piece(x, other, c, s, y);
+        scale_piece(y, inv);
+        close_piece(w, y);
         if (mine) raw[i] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
     }
 }

@@ -30,7 +30,7 @@ struct StoreTurned {
 cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, const RotaryArgs& rotary,
                                        cudaStream_t st)
 {
-    StoreRotary r{rotary, {g.d == 128 ? 4 : 3, 1, 0}};
+    StoreRotary r{rotary, {g.d == 128 ? 4 : 3, 1, {0, 0}}};
     r.args.rows[1].heads = 0;  // these are the store's
     const int window = store_window(g, a);
     dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
@@ -40,9 +40,9 @@ cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, c
         // leave a few blocks per SM
         const long long rows = (long long)a.tokens * heads;
         const long long groups = (152LL * 2048) >> r.deal.log_lanes;
-        while (r.deal.per < 16 && r.deal.per < heads && rows / r.deal.per > groups) r.deal.per *= 2;
-        r.deal.chunks = (heads + r.deal.per - 1) / r.deal.per;
-        const long long items = (long long)a.tokens * r.deal.chunks, own = g.page / 4;
+        while (r.deal.per < 32 && r.deal.per < heads && rows / r.deal.per > groups) r.deal.per *= 2;
+        r.deal.chunks[0] = chunks_of(heads, r.deal.per);
+        const long long items = (long long)a.tokens * r.deal.chunks[0], own = g.page / 4;
         const long long blocks = (items + own - 1) / own;
         const long long more = (blocks + grid.x - 1) / grid.x;
         if (grid.y + more > 65535) return cudaErrorInvalidConfiguration;

@@ -21,14 +21,15 @@ rotary_kernel(const __grid_constant__ RotaryArgs a, RotaryDeal deal)
 template <int DTYPE, int PAIR>
 cudaError_t go(const RotaryArgs& a, cudaStream_t st)
 {
-    RotaryDeal deal{0, 1, 0};
+    RotaryDeal deal{0, 1, {0, 0}};
     while (8 << deal.log_lanes < a.table.head_dim) ++deal.log_lanes;
-    const int every = a.rows[0].heads + a.rows[1].heads;
-    // heads of a token that share a group: as few as fill the machine
-    const long long rows = a.table.tokens * every, groups = 152LL * 2048 >> deal.log_lanes;
-    while (deal.per < 16 && deal.per < every && rows / deal.per > groups) deal.per *= 2;
-    deal.chunks = (every + deal.per - 1) / deal.per;
-    const long long threads = a.table.tokens * deal.chunks << deal.log_lanes;
+    const int most = a.rows[0].heads > a.rows[1].heads ? a.rows[0].heads : a.rows[1].heads;
+    // heads of a token that share a group and its angles: as few as fill the machine
+    const long long rows = a.table.tokens * (a.rows[0].heads + a.rows[1].heads);
+    const long long groups = 152LL * 2048 >> deal.log_lanes;
+    while (deal.per < 32 && deal.per < most && rows / deal.per > groups) deal.per *= 2;
+    for (int i = 0; i < 2; ++i) deal.chunks[i] = chunks_of(a.rows[i].heads, deal.per);
+    const long long threads = a.table.tokens * (deal.chunks[0] + deal.chunks[1]) << deal.log_lanes;
     const unsigned blocks = (unsigned)((threads + kThreads - 1) / kThreads);
     if (a.rows[0].weight || a.rows[1].weight)
         return launch_first(rotary_kernel<DTYPE, PAIR, true>, blocks, kThreads, 0, st, a, deal);

@@ -21,7 +21,7 @@ struct RotaryTable {
     // of a call
     int transposed;
     int weight_dtype;
-    float eps, weight_offset;
+    float eps, weight_offset, per_value;  // per_value: 1 / head_dim
     long long tokens;          // of an axis
     const int32_t* positions;  // [axes][tokens]
 };
@@ -35,8 +35,8 @@ enum { kPairLane = 0,    // from another lane: half a rotation is a multiple of 
 // row: y_e = x_e c_e + x_pair s_e.  Values beyond the rotation have 1 and -0, which
 // with a pair of 0 leaves them as they are, -0 too.
 template <int PAIR>
-__device__ __forceinline__ void angles_of(const RotaryTable& a, long long t, int e0, float (&c)[8],
-                                          float (&s)[8])
+__device__ __forceinline__ void angles_of(const RotaryTable& a, long long t, int e0, Piece& cosines,
+                                          Piece& sines)
 {
     const int half = a.rotary_dim / 2;
     int p[3] = {0, 0, 0};
@@ -46,6 +46,7 @@ __device__ __forceinline__ void angles_of(const RotaryTable& a, long long t, int
         p[2] = a.positions[2 * a.tokens + t];
     }
     const bool interleaved = PAIR == kPairOwn || (PAIR == kPairMemory && a.interleaved);
+    float c[8], s[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         if (PAIR == kPairOwn && (j & 1)) {
@@ -73,16 +74,17 @@ __device__ __forceinline__ void angles_of(const RotaryTable& a, long long t, int
         sine *= a.amplitude;
         s[j] = second != (a.transposed != 0) ? sine : -sine;
     }
+    set_floats(cosines, c);
+    set_floats(sines, s);
 }
 
-// The other value of each pair of the values e0 .. of a row, 0 beyond the
-// rotation.  `raw` (x unpacked) are the lane's own, `q` its place among those
-// that have the row at `row`, which start at a lane of the same alignment; the
-// whole warp calls it, and `mine` says whether there is such a row.
+// The other value of each pair of the values 8 q .. of a row, 0 beyond the rotation.
+// `raw` (v unpacked) are the lane's own, q its place among those that have the row
+// at `row`, which start at a lane of the same alignment; the whole warp calls it,
+// and `mine` says whether there is such a row.
 template <int DTYPE, int PAIR>
-__device__ __forceinline__ void pairs_of(const RotaryTable& a, const Eight<DTYPE>& raw,
-                                         const float (&x)[8], const void* row, bool mine, int q,
-                                         float (&other)[8])
+__device__ __forceinline__ void pairs_of(const RotaryTable& a, const Eight<DTYPE>& raw, const Piece& v,
+                                         const void* row, bool mine, int q, Piece& other)
 {
     const int e0 = 8 * q;
     if (PAIR == kPairLane) {
@@ -90,54 +92,83 @@ __device__ __forceinline__ void pairs_of(const RotaryTable& a, const Eight<DTYPE
         const int away = q < lanes ? lanes : q < 2 * lanes ? -lanes : 0;
         Eight<DTYPE> o;
 #pragma unroll
-        for (int i = 0; i < Eight<DTYPE>::kWords; ++i) {
+        for (int i = 0; i < Eight<DTYPE>::kWords; ++i)
             o.w[i] = __shfl_sync(0xFFFFFFFFu, raw.w[i], (threadIdx.x & 31) + away);
-            if (away == 0) o.w[i] = 0;
+        if (a.rotary_dim < a.head_dim && away == 0)
+#pragma unroll
+            for (int i = 0; i < Eight<DTYPE>::kWords; ++i) o.w[i] = 0;
+        open_piece(o, other);
+    } else if (PAIR == kPairOwn) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = floats_of(v.p[j]);
+            other.p[j] = pair_of(f.y, f.x);
+            if (a.rotary_dim < a.head_dim && e0 + 2 * j >= a.rotary_dim) other.p[j] = 0;
         }
-        unpack_eight(o, other);
-        return;
-    }
-    if (PAIR == kPairOwn) {
+    } else {
+        const int half = a.rotary_dim / 2;
+        float f[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) other[j] = e0 + j < a.rotary_dim ? x[j ^ 1] : 0.0f;
-        return;
-    }
-    const int half = a.rotary_dim / 2;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int e = e0 + j;
-        other[j] = 0.0f;
-        if (mine && e < a.rotary_dim)
-            other[j] = load_one<DTYPE>(row, a.interleaved ? e ^ 1 : e < half ? e + half : e - half);
+        for (int j = 0; j < 8; ++j) {
+            const int e = e0 + j;
+            f[j] = 0.0f;
+            if (mine && e < a.rotary_dim)
+                f[j] = load_one<DTYPE>(row, a.interleaved ? e ^ 1 : e < half ? e + half : e - half);
+        }
+        set_floats(other, f);
     }
 }
 
 // Weights of a norm into the factors: y = inv (x (w c) + other (w_other s)).
-__device__ __forceinline__ void weigh(const RotaryTable& a, const void* weight, int e0,
-                                      bool interleaved, float (&c)[8], float (&s)[8])
+// Whole warps call it; without a weight the factors stay.
+template <int DTYPE, int PAIR>
+__device__ __forceinline__ void weigh_as(const RotaryTable& a, const void* weight, int q, Piece& c, Piece& s)
 {
-    const int half = a.rotary_dim / 2;
+    const int e0 = 8 * q;
+    const bool mine = weight && e0 < a.head_dim;
+    Eight<DTYPE> raw;
+    Piece w, other;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int e = e0 + j;
-        if (e >= a.head_dim) continue;
-        c[j] *= a.weight_offset + load_any(weight, e, a.weight_dtype);
-        if (e >= a.rotary_dim) continue;
-        const int o = interleaved ? e ^ 1 : e < half ? e + half : e - half;
-        s[j] *= a.weight_offset + load_any(weight, o, a.weight_dtype);
+    for (int i = 0; i < Eight<DTYPE>::kWords; ++i) raw.w[i] = 0;
+    if (PAIR != kPairMemory) {
+        if (mine) load_eight(raw, static_cast<const char*>(weight) + e0 * Eight<DTYPE>::kBytes);
+        open_piece(raw, w);
+    } else {
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = mine && e0 + j < a.head_dim ? load_one<DTYPE>(weight, e0 + j) : 0.0f;
+        set_floats(w, f);
     }
+    pairs_of<DTYPE, PAIR>(a, raw, w, weight, mine, q, other);
+    if (!mine) return;
+    const Pair offset = pair_of(a.weight_offset, a.weight_offset);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        c.p[j] = mul2(c.p[j], add2(w.p[j], offset));
+        s.p[j] = mul2(s.p[j], add2(other.p[j], offset));
+    }
+}
+template <int DTYPE, int PAIR>
+__device__ __forceinline__ void weigh(const RotaryTable& a, const void* weight, int q, Piece& c, Piece& s)
+{
+    if (DTYPE != BACON_FP32 && a.weight_dtype == BACON_FP32)
+        weigh_as<BACON_FP32, PAIR>(a, weight, q, c, s);
+    else
+        weigh_as<DTYPE, PAIR>(a, weight, q, c, s);
 }
 
 // 1 / sqrt(mean x^2 + eps) of rows that groups of 2^log_lanes lanes have; the
 // whole warp calls it, and rows without a norm have 1.  Rows whose squares pass
 // fp32 are scaled, x and other too.
-__device__ __forceinline__ float row_inverse(const RotaryTable& a, int log_lanes, bool norm,
-                                             float (&x)[8], float (&other)[8])
+__device__ __forceinline__ float row_inverse(const RotaryTable& a, int log_lanes, bool norm, Piece& x,
+                                             Piece& other)
 {
-    auto squares = [&] {
-        float sum = 0.0f;
+    const auto squares = [&] {
+        Pair t = mul2(x.p[0], x.p[0]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], sum);
+        for (int j = 1; j < 4; ++j) t = fma2(x.p[j], x.p[j], t);
+        const float2 f = floats_of(t);
+        float sum = f.x + f.y;
         for (int off = 0; off < log_lanes; ++off) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1 << off);
         return sum;
     };
@@ -146,23 +177,29 @@ __device__ __forceinline__ float row_inverse(const RotaryTable& a, int log_lanes
     if (__any_sync(0xFFFFFFFFu, passed)) {
         if (passed) {
             eps = 0.0f;  // far below such a mean
+            const Pair small = pair_of(0x1p-100f, 0x1p-100f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                x[j] *= 0x1p-100f;
-                other[j] *= 0x1p-100f;
+            for (int j = 0; j < 4; ++j) {
+                x.p[j] = mul2(x.p[j], small);
+                other.p[j] = mul2(other.p[j], small);
             }
         }
         sum = squares();
     }
-    return norm ? 1.0f / sqrtf(sum / (float)a.head_dim + eps) : 1.0f;
+    return norm ? rsqrtf(fmaf(sum, a.per_value, eps)) : 1.0f;
 }
 
-__device__ __forceinline__ void turn_eight(const float (&x)[8], const float (&other)[8],
-                                           const float (&c)[8], const float (&s)[8], float inv,
-                                           float (&y)[8])
+__device__ __forceinline__ void turn_piece(const Piece& x, const Piece& other, const Piece& c, const Piece& s,
+                                           Piece& y)
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = fmaf(x[j], c[j], other[j] * s[j]) * inv;
+    for (int j = 0; j < 4; ++j) y.p[j] = fma2(x.p[j], c.p[j], mul2(other.p[j], s.p[j]));
+}
+__device__ __forceinline__ void scale_piece(Piece& y, float by)
+{
+    const Pair p = pair_of(by, by);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y.p[j] = mul2(y.p[j], p);
 }
 
 // Rows of one call: bacon_rows without what the host has checked.
@@ -184,89 +221,90 @@ struct RotaryArgs {
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
 
 // How the rows of a call are dealt out: a group of 2^log_lanes lanes turns `per`
-// heads of a token, of `chunks` such pieces.
+// heads of Q or of K of a token, of chunks[0] and chunks[1] such pieces.
 struct RotaryDeal {
-    int log_lanes, per, chunks;
+    int log_lanes, per, chunks[2];
 };
 constexpr int kRotaryBatch = 4;  // rows of a group that are on their way together
 
 // Piece `item` of the call's rows; whole warps call it.
 template <int DTYPE, int PAIR, bool NORM>
-__device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDeal& deal,
-                                             unsigned item)
+__device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
 {
+    constexpr int kBytes = Eight<DTYPE>::kBytes;
     const RotaryTable& tab = a.table;
     const int q = threadIdx.x & ((1 << deal.log_lanes) - 1), e0 = 8 * q;
-    const unsigned t = item / deal.chunks;
-    const int first = (int)(item % deal.chunks) * deal.per;
-    const bool active = t < tab.tokens;
-    const int count = active ? min(deal.per, a.rows[0].heads + a.rows[1].heads - first) : 0;
-    const bool inside = e0 < tab.head_dim;
+    const unsigned every = deal.chunks[0] + deal.chunks[1], t = item / every;
+    int first = (int)(item % every);
+    const bool key = first >= deal.chunks[0];
+    const RotaryRows& rows = a.rows[key];
+    if (key) first -= deal.chunks[0];
+    first *= deal.per;
+    const bool active = t < tab.tokens && e0 < tab.head_dim;
+    const int count = active ? min(deal.per, rows.heads - first) : 0;
     const unsigned r = t / a.tokens, n = t % a.tokens;
-    const bool interleaved = PAIR == kPairOwn || (PAIR == kPairMemory && tab.interleaved);
+    const char* in = rows.in + r * rows.in_request + n * rows.in_token + first * rows.in_head;
+    char* out = rows.out + r * rows.out_request + n * rows.out_token + first * rows.out_head;
     const bool vectors = PAIR != kPairMemory || a.vectors;
+    const bool norm = NORM && rows.weight;
+    // beyond the rotation rows stay as they are
+    const bool turns = norm || e0 < tab.rotary_dim;
+    const bool writes = turns || in != out;
 
-    float c[8], s[8], wc[8], ws[8];
-    int weighed = -1;
+    Piece c, s;
     for (int base = 0; base < deal.per; base += kRotaryBatch) {  // the same for the whole warp
         Eight<DTYPE> raw[kRotaryBatch];
-        const char* in[kRotaryBatch];
-        char* out[kRotaryBatch];
-        bool mine[kRotaryBatch];
 #pragma unroll
         for (int b = 0; b < kRotaryBatch; ++b) {
-            int h = first + base + b;
-            const bool key = h >= a.rows[0].heads;
-            const RotaryRows& rows = a.rows[key];
-            if (key) h -= a.rows[0].heads;
-            in[b] = rows.in + r * rows.in_request + n * rows.in_token + h * rows.in_head;
-            out[b] = rows.out + r * rows.out_request + n * rows.out_token + h * rows.out_head;
-            mine[b] = base + b < count && inside;
-            // beyond the rotation a row in place stays as it is
-            if (!NORM && in[b] == out[b] && e0 >= tab.rotary_dim) mine[b] = false;
 #pragma unroll
             for (int i = 0; i < Eight<DTYPE>::kWords; ++i) raw[b].w[i] = 0;
-            if (mine[b] && vectors) load_eight(raw[b], in[b] + e0 * Eight<DTYPE>::kBytes);
+            if (base + b < count && vectors) load_eight(raw[b], in + b * rows.in_head + e0 * kBytes);
         }
-        if (base == 0 && active) angles_of<PAIR>(tab, t, e0, c, s);
+        if (base == 0) {
+            if (active) angles_of<PAIR>(tab, t, e0, c, s);
+            if (NORM) weigh<DTYPE, PAIR>(tab, active ? rows.weight : nullptr, q, c, s);
+        }
 #pragma unroll
         for (int b = 0; b < kRotaryBatch; ++b) {
             if (base + b >= deal.per) break;
-            float x[8], other[8], y[8];
-            unpack_eight(raw[b], x);
-            if (!vectors && mine[b])
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (e0 + j < tab.head_dim) x[j] = load_one<DTYPE>(in[b], e0 + j);
-            pairs_of<DTYPE, PAIR>(tab, raw[b], x, in[b], mine[b], q, other);
-            if (PAIR == kPairMemory) __syncwarp();  // a row in place is read before it is written
-            if (NORM) {
-                const int key = first + base + b >= a.rows[0].heads;
-                const void* const weight = a.rows[key].weight;
-                if (key != weighed) {
-                    weighed = key;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) wc[j] = c[j], ws[j] = s[j];
-                    if (weight && active) weigh(tab, weight, e0, interleaved, wc, ws);
-                }
-                const float inv = row_inverse(tab, deal.log_lanes, weight != nullptr, x, other);
-                turn_eight(x, other, wc, ws, inv, y);
-            } else {
-                turn_eight(x, other, c, s, 1.0f, y);
-            }
-            if (!mine[b]) continue;
+            const bool mine = base + b < count;
+            const char* const row = in + b * rows.in_head;
+            char* const to = out + b * rows.out_head;
+            Piece x, other, y;
             if (vectors) {
-                Eight<DTYPE> w = raw[b];  // beyond the rotation, without a norm
-                if (e0 < tab.rotary_dim || (NORM && a.rows[first + base + b >= a.rows[0].heads].weight))
-                    pack_eight(w, y);
-                store_eight(out[b] + e0 * Eight<DTYPE>::kBytes, w);
+                open_piece(raw[b], x);
             } else {
+                float f[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (e0 + j < tab.head_dim) store_one<DTYPE>(out[b], e0 + j, y[j]);
+                    f[j] = mine && e0 + j < tab.head_dim ? load_one<DTYPE>(row, e0 + j) : 0.0f;
+                set_floats(x, f);
+            }
+            pairs_of<DTYPE, PAIR>(tab, raw[b], x, row, mine, q, other);
+            if (PAIR == kPairMemory) __syncwarp();  // a row in place is read before it is written
+            float inv = 1.0f;
+            if (NORM) inv = row_inverse(tab, deal.log_lanes, norm, x, other);
+            turn_piece(x, other, c, s, y);
+            if (NORM) scale_piece(y, inv);
+            if (!mine || !writes) continue;
+            if (vectors) {
+                Eight<DTYPE> w = raw[b];
+                if (turns) close_piece(w, y);
+                store_eight(to + e0 * kBytes, w);
+            } else {
+                float f[8];
+                get_floats(y, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (e0 + j < tab.head_dim) store_one<DTYPE>(to, e0 + j, f[j]);
             }
         }
+        in += kRotaryBatch * rows.in_head;
+        out += kRotaryBatch * rows.out_head;
     }
 }
+
+// Pieces of `heads` rows for the deal's `per`.
+inline int chunks_of(int heads, int per) { return (heads + per - 1) / per; }
 
 }  // namespace bacon

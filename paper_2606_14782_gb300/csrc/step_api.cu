@@ -68,7 +68,7 @@ bacon_status take_rows(const bacon_rows& r, const char* what, int requests, int 
             return fail(BACON_EINVAL, "%s: a stride is out of range", what);
     if (writes && !apart(d, {requests, tokens, r.heads}, {r.out_request, r.out_token, r.out_head}))
         return fail(BACON_EINVAL, "%s: rows of the output overlap", what);
-    if (!aligned16(r.in) || (writes && !aligned16(r.out))) *vectors = false;
+    if (!aligned16(r.in) || (writes && !aligned16(r.out)) || !aligned16(r.weight)) *vectors = false;
     const int places[3] = {requests, tokens, r.heads};
     for (int i = 0; i < (writes ? 6 : 3); ++i)
         if (places[i % 3] > 1 && strides[i] * bytes % 16) *vectors = false;
@@ -204,6 +204,7 @@ bacon_status bacon_rotary_create(bacon_rotary** out, int head_dim, int rotary_di
     t.rotary_dim = rotary_dim;
     t.interleaved = interleaved != 0;
     t.amplitude = amplitude;
+    t.per_value = 1.0f / (float)head_dim;
     t.axes = axis ? 3 : 1;
     for (int i = 0; i < rotary_dim / 2; ++i) {
         if (!std::isfinite(frequencies[i]) || std::fabs(frequencies[i]) > 1e6 ||

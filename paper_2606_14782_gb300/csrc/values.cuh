@@ -91,4 +91,77 @@ __device__ __forceinline__ float load_any(const void* p, long long i, int dtype)
                                  : load_one<BACON_FP16>(p, i);
 }
 
+// Two floats and what the two-float instructions do with them.
+typedef unsigned long long Pair;
+
+__device__ __forceinline__ Pair pair_of(float x, float y)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};\n" : "=l"(p) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ float2 floats_of(Pair p)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;\n" : "=f"(f.x), "=f"(f.y) : "l"(p));
+    return f;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair p;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(p) : "l"(a), "l"(b), "l"(c));
+    return p;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair p;
+    asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(p) : "l"(a), "l"(b));
+    return p;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    Pair p;
+    asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(p) : "l"(a), "l"(b));
+    return p;
+}
+
+// Eight channels.
+struct Piece {
+    Pair p[4];
+};
+template <int DTYPE>
+__device__ __forceinline__ void open_piece(const Eight<DTYPE>& raw, Piece& v)
+{
+    float f[8];
+    unpack_eight(raw, f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.p[j] = pair_of(f[2 * j], f[2 * j + 1]);
+}
+template <int DTYPE>
+__device__ __forceinline__ void close_piece(Eight<DTYPE>& raw, const Piece& v)
+{
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 t = floats_of(v.p[j]);
+        f[2 * j] = t.x;
+        f[2 * j + 1] = t.y;
+    }
+    pack_eight(raw, f);
+}
+__device__ __forceinline__ void set_floats(Piece& v, const float (&f)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v.p[j] = pair_of(f[2 * j], f[2 * j + 1]);
+}
+__device__ __forceinline__ void get_floats(const Piece& v, float (&f)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float2 t = floats_of(v.p[j]);
+        f[2 * j] = t.x;
+        f[2 * j + 1] = t.y;
+    }
+}
+
 }  // namespace bacon

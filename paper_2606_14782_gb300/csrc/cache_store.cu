@@ -89,7 +89,7 @@ struct Load {
 
 cudaError_t launch_cache_store(const CacheGeom& g, const StoreArgs& a, cudaStream_t st)
 {
-    const int window = store_window(g, a);
+    const int window = store_window(g, a, 8);
     const dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
     return by_type<Store>(g, a, grid, window, st);
 }

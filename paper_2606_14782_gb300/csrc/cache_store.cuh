@@ -8,6 +8,7 @@
 #include "common.cuh"
 #include "rotary.cuh"
 
+
 namespace bacon {
 namespace {
 
@@ -37,7 +38,7 @@ __device__ __forceinline__ void block_max(uint32_t (&m)[2], uint32_t (*s_max)[2]
 }
 
 // Positions into the rows of K that a run's threads have: 16 bytes of the rows
-// t + r, r < len.  The same steps as rotate_piece, rounded to DTYPE as there.
+// t + r, r < len.  The same steps as rotate_eights, rounded to DTYPE as there.
 template <int DTYPE, int D, int PAIR>
 __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* rows,
                                           long long token_stride, long long t, int len,
@@ -46,6 +47,15 @@ __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* r
     const RotaryTable& tab = a.table;
     const void* const weight = a.rows[1].weight;
     const int q = threadIdx.x % (D / 8), e0 = 8 * q;
+    // the rows' places on their way together, and the lane's part of the table once
+    RotaryPlace at[kChunks];
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int r = (threadIdx.x + i * blockDim.x) / (D / 8);
+        at[i] = RotaryPlace{{0, 0, 0}};
+        if (r < len) at[i] = place_of(tab, t + r);
+    }
+    const RotaryLane<PAIR> lane = lane_of<PAIR>(tab, e0);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
         if (i * (int)blockDim.x / (D / 8) >= len) break;  // nobody has a row
@@ -55,9 +65,7 @@ __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* r
         Piece x, other, c, s, y;
         open_piece(w, x);
         pairs_of<DTYPE, PAIR>(tab, w, x, rows + (t + r) * token_stride, mine, q, other);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c.p[j] = s.p[j] = 0;
-        if (mine) angles_of<PAIR>(tab, t + r, e0, c, s);
+        factors_of<PAIR>(tab, lane, at[i], e0, c, s);
         if (weight) weigh<DTYPE, PAIR>(tab, weight, q, c, s);
         const float inv = row_inverse(tab, D == 128 ? 4 : 3, weight != nullptr, x, other);
         turn_piece(x, other, c, s, y);
@@ -65,6 +73,18 @@ __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* r
         close_piece(w, y);
         if (mine) raw[i] = make_uint4(w.w[0], w.w[1], w.w[2], w.w[3]);
     }
+}
+
+// Rows of Q, by whichever way suits them where K has PAIR.
+template <int DTYPE, int PAIR>
+__device__ __forceinline__ void turn_queries(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+{
+    if (a.q_pair == PAIR)
+        rotate_piece<DTYPE, PAIR, true>(a, deal, item);
+    else if (PAIR == kPairOwn)
+        rotate_piece<DTYPE, kPairSixteen, true>(a, deal, item);
+    else if (PAIR == kPairLane)
+        rotate_piece<DTYPE, kPairHalves, true>(a, deal, item);
 }
 
 struct NoRotary {};
@@ -80,14 +100,15 @@ template <int DTYPE, int FORMAT, int D, int PAIR, typename ROTARY>
 __global__ void __launch_bounds__(512)
 store_kernel(CacheGeom g, StoreArgs a, int window, const __grid_constant__ ROTARY rotary)
 {
-    if constexpr (PAIR != kNoPair)
+    if constexpr (PAIR != kNoPair) {
         if (blockIdx.y >= a.heads) {
             const unsigned groups = blockDim.x >> rotary.deal.log_lanes;
             unsigned item = ((blockIdx.y - a.heads) * gridDim.x + blockIdx.x) * groups;
             item += threadIdx.x >> rotary.deal.log_lanes;
-            rotate_piece<DTYPE, PAIR, true>(rotary.args, rotary.deal, item);
+            turn_queries<DTYPE, PAIR>(rotary.args, rotary.deal, item);
             return;
         }
+    }
     constexpr uint32_t kInfinite = DTYPE == BACON_BF16 ? 0x7F80 : 0x7C00;
     __shared__ uint32_t s_start[4];   // bit i: a run starts at the window's token i
     __shared__ uint32_t s_break[9];   // bit i: no run goes on from token i - 1 to i
@@ -240,12 +261,12 @@ cudaError_t by_type(const CacheGeom& g, A&&... a)
     }
 }
 
-// Tokens whose runs a block takes: a page's when there are rows for several
+// Tokens whose runs a block takes: a page's when there are rows for `blocks`
 // blocks per SM; fewer when there are few, so that short runs do not queue in
 // one block.
-int store_window(const CacheGeom& g, const StoreArgs& a)
+int store_window(const CacheGeom& g, const StoreArgs& a, int blocks)
 {
-    const long long per_block = (long long)a.tokens * a.heads / (152 * 8);
+    const long long per_block = (long long)a.tokens * a.heads / (152 * blocks);
     return per_block < 1 ? 1 : per_block > g.page ? g.page : (int)per_block;
 }
 

@@ -30,20 +30,15 @@ struct StoreTurned {
 cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, const RotaryArgs& rotary,
                                        cudaStream_t st)
 {
-    StoreRotary r{rotary, {g.d == 128 ? 4 : 3, 1, {0, 0}}};
+    StoreRotary r{rotary, {}};
     r.args.rows[1].heads = 0;  // these are the store's
-    const int window = store_window(g, a);
+    const int window = store_window(g, a, 2);
     dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
-    const int heads = rotary.rows[0].heads;
-    if (heads) {
-        // a block's threads are the store's; its groups take as many heads each as
-        // leave a few blocks per SM
-        const long long rows = (long long)a.tokens * heads;
-        const long long groups = (152LL * 2048) >> r.deal.log_lanes;
-        while (r.deal.per < 32 && r.deal.per < heads && rows / r.deal.per > groups) r.deal.per *= 2;
-        r.deal.chunks[0] = chunks_of(heads, r.deal.per);
-        const long long items = (long long)a.tokens * r.deal.chunks[0], own = g.page / 4;
-        const long long blocks = (items + own - 1) / own;
+    if (r.args.rows[0].heads) {
+        // blocks of the store's size
+        const long long pieces = deal_rows(r.args, values_of_lane(r.args.q_pair), &r.deal);
+        const int groups = (g.page * g.d / 8 / kChunks) >> r.deal.log_lanes;
+        const long long blocks = (pieces + groups - 1) / groups;
         const long long more = (blocks + grid.x - 1) / grid.x;
         if (grid.y + more > 65535) return cudaErrorInvalidConfiguration;
         grid.y += (unsigned)more;

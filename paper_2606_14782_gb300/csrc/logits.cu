@@ -2,13 +2,15 @@
 // log-probability in one pass.  Bound by bytes: a row's logits are read once and,
 // if wanted, written once.
 //
-// A row belongs to a cluster of blocks, each with a part of the vocabulary.  The
-// blocks read the row's history once between them and count every token in the
-// block whose part it lies in, by atomics on distributed shared memory: a word a
-// token, with the number of times in the answer, whether the history has it, and
-// the last place of the row's bias list that names it.  Whole numbers only, so
-// that no order changes a result.  The pass over the logits then looks at these
-// words, and the maxima and sums of the parts meet in the first block.
+// A row belongs to a cluster of blocks, which have groups of 256 neighbouring tokens
+// in turn, so that the many uses of a few low numbers are spread.  A block goes through the row's whole history and counts its own tokens by
+// atomics on a word a token in its shared memory: the number of times in the
+// answer, whether the prompt has it, and the last place of the row's bias list that
+// names it.  Whole numbers only, so that no order changes a result.  (Each entry
+// read by one block and counted in the block that has its token, by atomics on
+// distributed shared memory, took 42 us for 100000 entries on 16 blocks: about
+// eight cycles an entry.)  The pass over the logits then looks at these words, and
+// the maxima and sums of the parts meet in the first block.
 #include "logits.h"
 
 #include "common.cuh"
@@ -18,6 +20,7 @@ namespace bacon {
 namespace {
 
 constexpr int kThreads = 512;
+constexpr int kGroup = 256;              // tokens that a warp takes together
 constexpr float kLeast = 1e-30f;         // repetition and temperature
 constexpr uint32_t kCount = 0xFFFFFu;    // of a token's word: times in the answer
 constexpr uint32_t kSeen = 1u << 20;     // in the prompt
@@ -38,52 +41,42 @@ __device__ __forceinline__ uint32_t cluster_address(uint32_t local, int rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(local), "r"(rank));
     return a;
 }
-__device__ __forceinline__ void cluster_add(uint32_t address, uint32_t v)
-{
-    asm volatile("red.relaxed.cluster.shared::cluster.add.u32 [%0], %1;\n" ::"r"(address), "r"(v)
-                 : "memory");
-}
-__device__ __forceinline__ void cluster_or(uint32_t address, uint32_t v)
-{
-    asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;\n" ::"r"(address), "r"(v)
-                 : "memory");
-}
-
-// A part's largest value, the sum of exp over it relative to that, and the key
-// of its best token: the value's order, then the lowest number.
-struct Part {
+// Several parts' largest value, where it is first, and the sum of exp relative to it.
+struct alignas(16) Part {
     float sum, top;
-    unsigned long long best;
+    uint32_t at;  // 0xFFFFFFFF: no value above -inf
 };
 
-// Two parts as one; `rate` is log2(e) / temperature.
-__device__ __forceinline__ Part join(const Part& a, const Part& b, float rate)
+// A warp's parts as one; `rate` is log2(e) / temperature.
+__device__ __forceinline__ Part join_warp(const Part& p, float rate)
 {
-    Part p;
-    p.best = a.best > b.best ? a.best : b.best;
-    p.top = fmaxf(a.top, b.top);
+    Part all;
+    const uint32_t key = float_key(p.top + 0.0f), most = __reduce_max_sync(0xFFFFFFFFu, key);  // (0 for -0)
+    all.top = key_float(most);
+    all.at = __reduce_min_sync(0xFFFFFFFFu, key == most ? p.at : 0xFFFFFFFFu);
     // an empty part (top -inf) has a sum of 0
-    const float x = a.top == p.top ? a.sum : a.sum * fast_exp2((a.top - p.top) * rate);
-    const float y = b.top == p.top ? b.sum : b.sum * fast_exp2((b.top - p.top) * rate);
-    p.sum = x + y;
-    return p;
-}
-__device__ __forceinline__ Part join_warp(Part p, float rate)
-{
+    all.sum = key == most ? p.sum : p.sum * fast_exp2((p.top - all.top) * rate);
 #pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        Part o;
-        o.sum = __shfl_xor_sync(0xFFFFFFFFu, p.sum, off);
-        o.top = __shfl_xor_sync(0xFFFFFFFFu, p.top, off);
-        o.best = __shfl_xor_sync(0xFFFFFFFFu, p.best, off);
-        p = join(p, o, rate);
-    }
-    return p;
+    for (int off = 16; off; off >>= 1) all.sum += __shfl_xor_sync(0xFFFFFFFFu, all.sum, off);
+    return all;
+}
+
+// Counts in shared memory where `on`, without a branch.
+__device__ __forceinline__ void add_where(uint32_t address, bool on)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p red.shared.add.u32 [%0], 1;\n}\n" ::"r"(address),
+                 "r"((uint32_t)on)
+                 : "memory");
+}
+__device__ __forceinline__ void or_where(uint32_t address, uint32_t bits, bool on)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p red.shared.or.b32 [%0], %1;\n}\n" ::"r"(address),
+                 "r"(bits), "r"((uint32_t)on)
+                 : "memory");
 }
 
 struct Rules {
     float repetition, frequency, presence, rate;  // rate: 1 / temperature
-    const int32_t* bias_tokens;
     const float* bias_values;
 };
 
@@ -99,73 +92,119 @@ __device__ __forceinline__ float ruled(float x, uint32_t word, const Rules& r)
     return x;
 }
 
-__device__ __forceinline__ float checked(const float* p, int row, float otherwise, bool positive, int* err)
+// A row's parameter, or what stands for it if it is out of its range.
+__device__ __forceinline__ float checked(float v, float otherwise, bool positive, int* err)
 {
-    if (!p) return otherwise;
-    const float v = p[row];
     if (isfinite(v) && (!positive || v >= kLeast)) return v;
     if (threadIdx.x == 0) atomicCAS(err, 0, kLogitsBadValue);
     return otherwise;
 }
 
 // kStep: values a thread takes at a time: 8 where rows start at 16 bytes, else 1.
-template <int DTYPE, int OUT, int kStep>
-__global__ void __launch_bounds__(kThreads)
-logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int part, int blocks, int words,
-              int* err)
+// kResident: blocks of an SM: 3 where there are as many (the largest case: 94 us for
+// 107 with 2), else 2 and more registers (one row: 5.5 us for 5.8).
+template <int DTYPE, int OUT, int kStep, int kResident>
+__global__ void __launch_bounds__(kThreads, kResident)
+logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_blocks, int words, int* err)
 {
-    extern __shared__ uint32_t s_word[];  // [part], where there is a history or a list
+    extern __shared__ __align__(16) uint32_t s_word[];  // of the block's groups, if there is a history or list
     __shared__ Part s_part[16];
     __shared__ Part s_joined[16];
-    const int row = blockIdx.x / blocks, rank = blockIdx.x % blocks;
+    const int blocks = 1 << log_blocks, row = blockIdx.x >> log_blocks, rank = blockIdx.x & (blocks - 1);
     const int tid = threadIdx.x, lane = tid & 31;
-    const int begin = min(vocab, rank * part), end = min(vocab, begin + part);
+    // the block's k-th group is the row's number k blocks + rank
+    const int groups = ((vocab + kGroup - 1) / kGroup - rank + blocks - 1) >> log_blocks;
+    const auto mine = [&](int token) {
+        const uint32_t t = token;
+        return t < (uint32_t)vocab && ((t / kGroup ^ rank) & (blocks - 1)) == 0;
+    };
+    const auto word_of = [&](int token) {
+        const uint32_t t = token;
+        return (t / kGroup >> log_blocks) * kGroup + t % kGroup;
+    };
+    // all that the row's parameters say, on its way together
     const int length_in = a.lengths ? a.lengths[row] : 0;
+    const int prompt_in = a.prompt ? a.prompt[row] : 0, line = a.request ? a.request[row] : row;
+    const float repetition = a.repetition ? a.repetition[row] : 1.0f;
+    const float frequency = a.frequency ? a.frequency[row] : 0.0f;
+    const float presence = a.presence ? a.presence[row] : 0.0f;
+    const float temperature = a.temperature ? a.temperature[row] : 1.0f;
+    const int32_t* const bias_tokens = a.bias_tokens ? a.bias_tokens + (long long)row * a.biases : nullptr;
+    const int first_bias = bias_tokens && tid < a.biases ? bias_tokens[tid] : -1;
+    if (words)
+        for (int i = tid; i < groups * kGroup / 4; i += kThreads)
+            reinterpret_cast<uint4*>(s_word)[i] = make_uint4(0, 0, 0, 0);
     if (a.lengths && length_in == -1) return;  // all blocks of the row
-
     Rules rules;
-    rules.repetition = checked(a.repetition, row, 1.0f, true, err);
-    rules.frequency = checked(a.frequency, row, 0.0f, false, err);
-    rules.presence = checked(a.presence, row, 0.0f, false, err);
-    rules.rate = 1.0f / checked(a.temperature, row, 1.0f, true, err);
-    rules.bias_tokens = a.bias_tokens ? a.bias_tokens + (long long)row * a.biases : nullptr;
+    rules.repetition = checked(repetition, 1.0f, true, err);
+    rules.frequency = checked(frequency, 0.0f, false, err);
+    rules.presence = checked(presence, 0.0f, false, err);
+    rules.rate = 1.0f / checked(temperature, 1.0f, true, err);
     rules.bias_values = a.bias_tokens ? a.bias_values + (long long)row * a.biases : nullptr;
 
+    const char* const in =
+        static_cast<const char*>(a.logits) + row * a.row_stride * Eight<DTYPE>::kBytes;
     const bool greedy = a.best || a.logprob || a.lse;
     // the row's blocks have all begun before one writes into another
-    if (!words && greedy) cluster_arrive();
+    if (greedy) cluster_arrive();
     if (words) {
-        for (int i = tid; i < part; i += kThreads) s_word[i] = 0;
-        cluster_arrive();
-        cluster_wait();
         int length = a.tokens && a.lengths ? length_in : 0;
-        const int prompt = a.prompt && length ? a.prompt[row] : 0;
-        const int line = a.request ? a.request[row] : row;
-        if (length && (length < 0 || length > a.capacity || prompt < 0 || prompt > length || line < 0 ||
+        if (length && (length < 0 || length > a.capacity || prompt_in < 0 || prompt_in > length || line < 0 ||
                        line >= a.requests)) {
             if (tid == 0) atomicCAS(err, 0, kLogitsBadHistory);
             length = 0;
         }
+        const int prompt = length ? prompt_in : 0;
         const int32_t* const history = a.tokens + (length ? line * a.token_stride : 0);
-        const uint32_t base = smem_u32(s_word);
-        for (int i = rank * kThreads + tid; i < length; i += blocks * kThreads) {
-            const int token = history[i];
-            if (token < 0 || token >= vocab) continue;
-            const int owner = token / part;
-            const uint32_t at = cluster_address(base + 4 * (token - owner * part), owner);
-            if (i < prompt)
-                cluster_or(at, kSeen);
-            else
-                cluster_add(at, 1);
+        // four entries a load, from the last multiple of 16 bytes before the line
+        const int lead = (int)(reinterpret_cast<uintptr_t>(history) >> 2) & 3;
+        const int loads = (length + lead + 3) / 4;
+        const uint32_t words_at = smem_u32(s_word);
+        constexpr int kFlight = 4;  // loads of a thread that are on their way together
+        int4 token[kFlight];
+        const auto fetch = [&](int g0) {
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                const int g = g0 + k * kThreads, i = 4 * g - lead;
+                token[k] = make_int4(-1, -1, -1, -1);
+                if (g >= loads) continue;
+                if (i >= 0 && i + 4 <= length) {
+                    token[k] = *reinterpret_cast<const int4*>(history + i);
+                } else {
+                    if (i >= 0) token[k].x = history[i];
+                    if (i + 1 >= 0 && i + 1 < length) token[k].y = history[i + 1];
+                    if (i + 2 >= 0 && i + 2 < length) token[k].z = history[i + 2];
+                    if (i + 3 < length) token[k].w = history[i + 3];
+                }
+            }
+        };
+        fetch(tid);
+        __syncthreads();  // the words are 0
+        for (int g0 = tid; g0 < loads; g0 += kFlight * kThreads) {
+            if (g0 != tid) fetch(g0);
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                const int i = 4 * (g0 + k * kThreads) - lead;
+                const int entry[4] = {token[k].x, token[k].y, token[k].z, token[k].w};
+#pragma unroll
+                for (int z = 0; z < 4; ++z) {
+                    const bool own = mine(entry[z]), said = i + z >= prompt;
+                    const uint32_t at = word_of(entry[z]);
+                    // a prompt may have one token many times on end
+                    const bool anew = own && (z == 0 || entry[z] != entry[z ? z - 1 : 0]);
+                    add_where(words_at + 4 * at, own && said);
+                    or_where(words_at + 4 * at, kSeen, anew && !said);
+                }
+            }
         }
-        cluster_arrive();
-        cluster_wait();
+        __syncthreads();
         // the other fields of a word are settled: the largest word has the last place
-        if (rules.bias_tokens) {
+        if (bias_tokens) {
             for (int i = tid; i < a.biases; i += kThreads) {
-                const int token = rules.bias_tokens[i];
-                if (token >= begin && token < end) {
-                    uint32_t* const w = &s_word[token - begin];
+                const int token = i == tid ? first_bias : bias_tokens[i];
+                if (mine(token)) {
+                    const uint32_t at = word_of(token);
+                    uint32_t* const w = &s_word[at];
                     const uint32_t fields = *(volatile uint32_t*)w & (kCount | kSeen);
                     atomicMax(w, (uint32_t)(i + 1) << kBiasShift | fields);
                 } else if ((token < -1 || token >= vocab) && rank == 0) {
@@ -175,126 +214,172 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int part, 
             __syncthreads();
         }
     }
-
     const float rate = rules.rate * 1.4426950408889634f;
-    Part p{0.0f, -INFINITY, 0};
-    const char* const in =
-        static_cast<const char*>(a.logits) + row * a.row_stride * Eight<DTYPE>::kBytes;
+    Part p{0.0f, -INFINITY, 0xFFFFFFFFu};
     char* const out = a.out ? static_cast<char*>(a.out) + row * a.out_stride * Eight<OUT>::kBytes : nullptr;
     const uint32_t* const mask = a.mask ? a.mask + row * a.mask_stride : nullptr;
-    // eight values at a time: neighbours, or every kThreads-th one
-    constexpr int kGap = kStep == 8 ? 1 : kThreads;
-    for (int v0 = begin + (kStep == 8 ? 8 * tid : tid); v0 < end; v0 += 8 * kThreads) {
-        float x[8];
-        if (kStep == 8 && v0 + 8 <= end) {
+    // a lane has eight neighbours of a group, or every 32nd token from its own
+    constexpr int kGap = kStep == 8 ? 1 : 32;
+    const Pair by_rate = pair_of(rules.rate, rules.rate), by_log = pair_of(rate, rate);
+    for (int k = tid >> 5; k < groups; k += kThreads / 32) {
+        const int v0 = ((k << log_blocks) + rank) * kGroup + (kStep == 8 ? 8 : 1) * lane;
+        const bool whole = kStep == 8 && v0 + 8 <= vocab;
+        Piece piece;
+        if (whole) {
             Eight<DTYPE> raw;
             load_eight(raw, in + (long long)v0 * Eight<DTYPE>::kBytes);
-            unpack_eight(raw, x);
-        } else {
+            open_piece(raw, piece);
+        } else {  // -inf behind the row's end
+            float x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int v = v0 + j * kGap;
-                x[j] = v < end ? load_one<DTYPE>(in, v) : -INFINITY;
+                x[j] = v < vocab ? load_one<DTYPE>(in, v) : -INFINITY;
             }
+            set_floats(piece, x);
         }
         if (words) {
-            uint32_t w[8], any = 0;
+            uint32_t* const words_here = s_word + k * kGroup + (kStep == 8 ? 8 : 1) * lane;
+            uint32_t w[8], some = 0;
+            const auto read = [&] {
+                if (kStep == 8) {
+                    const uint4* const q = reinterpret_cast<const uint4*>(words_here);
+                    const uint4 lo = q[0], hi = q[1];
+                    w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w;
+                    w[4] = hi.x, w[5] = hi.y, w[6] = hi.z, w[7] = hi.w;
+                } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int v = v0 + j * kGap;
-                w[j] = v < end ? s_word[v - begin] : 0;
-                any |= w[j];
-            }
-            if (any)
+                    for (int j = 0; j < 8; ++j) w[j] = words_here[32 * j];
+                }
+            };
+            read();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) some |= (w[j] != 0) << j;
+            if (some) {
+                // few of the eight, so each in its turn: its word becomes the logit that
+                // the rules make of it (eight at once: 103 us for 94 of the largest case)
+                float x[8];
+                get_floats(piece, x);
+                for (uint32_t left = some; left; left &= left - 1) {
+                    const int j = __ffs(left) - 1;
+                    const float raw = load_one<DTYPE>(in, v0 + j * kGap);
+                    words_here[j * kGap] = __float_as_uint(ruled(raw, words_here[j * kGap], rules));
+                }
+                read();
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (w[j]) x[j] = ruled(x[j], w[j], rules);
-        }
-        if (mask) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int v = v0 + j * kGap;
-                if (v < end && !(mask[v >> 5] >> (v & 31) & 1)) x[j] = -INFINITY;
+                    if (some >> j & 1) x[j] = __uint_as_float(w[j]);
+                set_floats(piece, x);
             }
         }
-        if (out) {
-            if (kStep == 8 && v0 + 8 <= end) {
-                float y[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = x[j] * rules.rate;
-                Eight<OUT> raw;
-                pack_eight(raw, y);
-                store_eight(out + (long long)v0 * Eight<OUT>::kBytes, raw);
+        if (mask) {
+            uint32_t allowed = 0;
+            if (kStep == 8) {
+                if (v0 < vocab) allowed = reinterpret_cast<const uint8_t*>(mask)[v0 >> 3];
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int v = v0 + j * kGap;
-                    if (v < end) store_one<OUT>(out, v, x[j] * rules.rate);
+                    if (v < vocab) allowed |= (mask[v >> 5] >> (v & 31) & 1) << j;
+                }
+            }
+            if (allowed != 0xFF) {
+                float x[8];
+                get_floats(piece, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (!(allowed >> j & 1)) x[j] = -INFINITY;
+                set_floats(piece, x);
+            }
+        }
+        if (out) {
+            Piece y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y.p[j] = mul2(piece.p[j], by_rate);
+            if (whole) {
+                Eight<OUT> raw;
+                close_piece(raw, y);
+                store_eight(out + (long long)v0 * Eight<OUT>::kBytes, raw);
+            } else {
+                float f[8];
+                get_floats(y, f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int v = v0 + j * kGap;
+                    if (v < vocab) store_one<OUT>(out, v, f[j]);
                 }
             }
         }
         if (!greedy) continue;
-        // numbers rise along j and along the loop: the first of equals stays
-        float top = p.top;
-        int at = -1;
+        float x[8];
+        get_floats(piece, x);
+        const float top = max3f(max3f(x[0], x[1], x[2]), max3f(x[3], x[4], x[5]), fmaxf(x[6], x[7]));
+        if (top > p.top) {
+            // numbers rise along j and along the loop: the first of equals stays
+            int at = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (x[j] > top) {
-                top = x[j];
-                at = v0 + j * kGap;
-            }
-        if (at >= 0) {
+            for (int j = 7; j >= 0; --j)
+                if (x[j] == top) at = j;
             p.sum *= fast_exp2((p.top - top) * rate);  // 0 from -inf
             p.top = top;
-            p.best = (unsigned long long)float_key(top + 0.0f) << 32 | (0xFFFFFFFFu - (uint32_t)at);
+            p.at = v0 + at * kGap;
         }
+        // what is -inf adds nothing, while there is nothing else too; NaN makes the sum NaN
+        const float less = p.top == -INFINITY ? 0.0f : -p.top;
+        const Pair off = pair_of(less, less);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            // what is -inf adds nothing; NaN makes the sum NaN
-            if (x[j] != -INFINITY) p.sum += fast_exp2((x[j] - p.top) * rate);
+        for (int j = 0; j < 4; ++j) {
+            const float2 f = floats_of(mul2(add2(piece.p[j], off), by_log));
+            p.sum += fast_exp2(f.x) + fast_exp2(f.y);
+        }
     }
     if (!greedy) return;
 
-    if (!words) cluster_wait();
+    cluster_wait();
     p = join_warp(p, rate);
     if (lane == 0) s_part[tid >> 5] = p;
     __syncthreads();
     if (tid < 32) {
-        p = tid < kThreads / 32 ? s_part[tid] : Part{0.0f, -INFINITY, 0};
+        p = tid < kThreads / 32 ? s_part[tid] : Part{0.0f, -INFINITY, 0xFFFFFFFFu};
         p = join_warp(p, rate);
         if (tid == 0) {
             const uint32_t to = cluster_address(smem_u32(&s_joined[rank]), 0);
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};\n" ::"r"(to), "f"(p.sum), "f"(p.top)
                          : "memory");
-            asm volatile("st.shared::cluster.u64 [%0], %1;\n" ::"r"(to + 8), "l"(p.best) : "memory");
+            asm volatile("st.shared::cluster.u32 [%0], %1;\n" ::"r"(to + 8), "r"(p.at) : "memory");
         }
     }
     cluster_arrive();
     cluster_wait();
     if (rank || tid >= 32) return;
-    p = tid < blocks ? s_joined[tid] : Part{0.0f, -INFINITY, 0};
+    p = tid < blocks ? s_joined[tid] : Part{0.0f, -INFINITY, 0xFFFFFFFFu};
     p = join_warp(p, rate);
     if (tid == 0) {
-        const bool none = p.best == 0 && !isnan(p.sum);
+        const bool found = p.at != 0xFFFFFFFFu, none = !found && !isnan(p.sum);
         const float more = logf(p.sum);
-        if (a.best) a.best[row] = p.best ? (int)(0xFFFFFFFFu - (uint32_t)p.best) : -1;
-        if (a.logprob) a.logprob[row] = none ? -INFINITY : p.best ? -more : NAN;
+        if (a.best) a.best[row] = found ? (int)p.at : -1;
+        if (a.logprob) a.logprob[row] = none ? -INFINITY : found ? -more : NAN;
         if (a.lse)
             a.lse[row] = none ? -INFINITY : p.top == INFINITY ? INFINITY : p.top * rules.rate + more;
     }
 }
 
-template <int DTYPE, int OUT, int kStep>
-cudaError_t go(const bacon_logits_rows& r, int vocab, int* err, cudaStream_t st)
+template <int DTYPE, int OUT, int kStep, int kResident>
+cudaError_t start(const bacon_logits_rows& r, int vocab, int blocks, int* err, cudaStream_t st)
 {
     const bool words = (r.tokens && r.lengths) || (r.bias_tokens && r.biases);
-    const int blocks = 8;
-    const int part = ((vocab + blocks - 1) / blocks + 31) / 32 * 32;
-    const size_t smem = words ? (size_t)part * 4 : 0;
-    auto* const kernel = logits_kernel<DTYPE, OUT, kStep>;
+    int log_blocks = 0;
+    while (1 << log_blocks < blocks) ++log_blocks;
+    const int groups = ((vocab + kGroup - 1) / kGroup + blocks - 1) / blocks;  // of a block, at most
+    const size_t smem = words ? (size_t)groups * kGroup * 4 : 0;
+    auto* const kernel = logits_kernel<DTYPE, OUT, kStep, kResident>;
     if (smem > 32 * 1024) {
         const cudaError_t e =
             cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    if (blocks > 8) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
     }
     cudaLaunchAttribute attr;
@@ -308,7 +393,20 @@ cudaError_t go(const bacon_logits_rows& r, int vocab, int* err, cudaStream_t st)
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, r, vocab, part, blocks, (int)words, err);
+    return cudaLaunchKernelEx(&cfg, kernel, r, vocab, log_blocks, (int)words, err);
+}
+
+template <int DTYPE, int OUT, int kStep>
+cudaError_t go(const bacon_logits_rows& r, int vocab, int* err, cudaStream_t st)
+{
+    // blocks of a row: eight, or sixteen when rows are few; no more than have
+    // something to do, be it logits or tokens of a long history
+    int blocks = r.rows <= 152 / 8 ? 16 : 8;
+    while (blocks > 1 && vocab <= blocks / 2 * kThreads * 8 && vocab <= BACON_MAX_VOCAB / 16 &&
+           r.capacity <= blocks * kThreads)
+        blocks /= 2;
+    return (long long)r.rows * blocks > 152 * 2 ? start<DTYPE, OUT, kStep, 3>(r, vocab, blocks, err, st)
+                                                : start<DTYPE, OUT, kStep, 2>(r, vocab, blocks, err, st);
 }
 
 template <int DTYPE, int OUT>

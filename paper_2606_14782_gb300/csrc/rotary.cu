@@ -1,8 +1,8 @@
 // Rotary positions of Q and K.  Bound by bytes: every value is read and written
-// once.  A lane has eight neighbouring values of a row (16 bytes of 16-bit types),
+// once.  A lane has eight pairs of a row, as two groups of 16 bytes of 16-bit types,
 // the lanes of a row form a group of a power of two, and a group turns several
-// heads of one token with the same cosines and sines: per row what is left is
-// two products a value.
+// heads of one token with the same cosines and sines: per row what is left is two
+// products a value.  Rows that do not allow it have eight values a lane.
 #include "rotary.cuh"
 
 namespace bacon {
@@ -11,37 +11,33 @@ namespace {
 constexpr int kThreads = 256;
 
 template <int DTYPE, int PAIR, bool NORM>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, PAIR == kPairMemory || (NORM && PAIR >= kPairHalves) ? 2 : 3)
 rotary_kernel(const __grid_constant__ RotaryArgs a, RotaryDeal deal)
 {
     const unsigned groups = kThreads >> deal.log_lanes;
     rotate_piece<DTYPE, PAIR, NORM>(a, deal, blockIdx.x * groups + (threadIdx.x >> deal.log_lanes));
 }
 
-template <int DTYPE, int PAIR>
+template <int DTYPE, int PAIR, bool NORM>
 cudaError_t go(const RotaryArgs& a, cudaStream_t st)
 {
-    RotaryDeal deal{0, 1, {0, 0}};
-    while (8 << deal.log_lanes < a.table.head_dim) ++deal.log_lanes;
-    const int most = a.rows[0].heads > a.rows[1].heads ? a.rows[0].heads : a.rows[1].heads;
-    // heads of a token that share a group and its angles: as few as fill the machine
-    const long long rows = a.table.tokens * (a.rows[0].heads + a.rows[1].heads);
-    const long long groups = 152LL * 2048 >> deal.log_lanes;
-    while (deal.per < 32 && deal.per < most && rows / deal.per > groups) deal.per *= 2;
-    for (int i = 0; i < 2; ++i) deal.chunks[i] = chunks_of(a.rows[i].heads, deal.per);
-    const long long threads = a.table.tokens * (deal.chunks[0] + deal.chunks[1]) << deal.log_lanes;
+    RotaryDeal deal;
+    const long long threads = deal_rows(a, values_of_lane(PAIR), &deal) << deal.log_lanes;
     const unsigned blocks = (unsigned)((threads + kThreads - 1) / kThreads);
-    if (a.rows[0].weight || a.rows[1].weight)
-        return launch_first(rotary_kernel<DTYPE, PAIR, true>, blocks, kThreads, 0, st, a, deal);
-    return launch_first(rotary_kernel<DTYPE, PAIR, false>, blocks, kThreads, 0, st, a, deal);
+    return launch_first(rotary_kernel<DTYPE, PAIR, NORM>, blocks, kThreads, 0, st, a, deal);
 }
 
 template <int DTYPE>
 cudaError_t by_pair(const RotaryArgs& a, cudaStream_t st)
 {
-    return a.pair == kPairLane  ? go<DTYPE, kPairLane>(a, st)
-           : a.pair == kPairOwn ? go<DTYPE, kPairOwn>(a, st)
-                                : go<DTYPE, kPairMemory>(a, st);
+    const bool norm = a.rows[0].weight || a.rows[1].weight;
+    switch (a.q_pair) {
+        case kPairHalves: return norm ? go<DTYPE, kPairHalves, true>(a, st) : go<DTYPE, kPairHalves, false>(a, st);
+        case kPairSixteen: return norm ? go<DTYPE, kPairSixteen, true>(a, st) : go<DTYPE, kPairSixteen, false>(a, st);
+        case kPairLane: return go<DTYPE, kPairLane, true>(a, st);
+        case kPairOwn: return go<DTYPE, kPairOwn, true>(a, st);
+        default: return norm ? go<DTYPE, kPairMemory, true>(a, st) : go<DTYPE, kPairMemory, false>(a, st);
+    }
 }
 
 }  // namespace

@@ -8,6 +8,7 @@
 namespace bacon {
 
 constexpr int kMaxPairsOfHead = BACON_MAX_HEAD / 2;
+constexpr int kMostHeads = 16;  // of a group
 
 // A handle's table and a call's choices; travels as a kernel parameter (1.2 KB),
 // so that a handle has no device memory and a captured call outlives it.
@@ -26,53 +27,124 @@ struct RotaryTable {
     const int32_t* positions;  // [axes][tokens]
 };
 
-// How a lane gets the other value of each of its pairs.
+// How a lane that has eight neighbouring values gets the other of each pair ...
 enum { kPairLane = 0,    // from another lane: half a rotation is a multiple of eight values
        kPairOwn = 1,     // it has it itself: interleaved
-       kPairMemory = 2 };  // it reads it again, and rows may start anywhere
+       kPairMemory = 2,  // it reads it again, and rows may start anywhere
+       // ... and lanes that have eight whole pairs (rotary.cu)
+       kPairHalves = 3,  // eight values and their eight others, half a rotation on
+       kPairSixteen = 4 };  // sixteen neighbours, interleaved
 
-// Cosine and signed sine of token t's angles for the values e0 .. e0 + 8 of a
-// row: y_e = x_e c_e + x_pair s_e.  Values beyond the rotation have 1 and -0, which
-// with a pair of 0 leaves them as they are, -0 too.
-template <int PAIR>
-__device__ __forceinline__ void angles_of(const RotaryTable& a, long long t, int e0, Piece& cosines,
-                                          Piece& sines)
+// Cosines and sines of two angles given in units of 2^-32 turns: the nearest
+// quarter turn comes off, the rest, at most an eighth of a turn either way, goes
+// into the Taylor series of both (to x^9 and x^10, what follows is below 2^-29),
+// and the quarter says which of the two is the cosine and with what sign.
+__device__ __forceinline__ void two_angles(uint32_t u0, uint32_t u1, float (&cosine)[2], float (&sine)[2])
 {
-    const int half = a.rotary_dim / 2;
-    int p[3] = {0, 0, 0};
-    p[0] = a.positions[t];
-    if (a.axes > 1) {
-        p[1] = a.positions[a.tokens + t];
-        p[2] = a.positions[2 * a.tokens + t];
-    }
-    const bool interleaved = PAIR == kPairOwn || (PAIR == kPairMemory && a.interleaved);
-    float c[8], s[8];
+    const uint32_t u[2] = {u0, u1};
+    uint32_t quarter[2];
+    float rest[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if (PAIR == kPairOwn && (j & 1)) {
-            c[j] = c[j - 1];  // (a rotation ends with a pair)
-            s[j] = e0 + j < a.rotary_dim ? -s[j - 1] : -0.0f;
-            continue;
-        }
+    for (int i = 0; i < 2; ++i) {
+        quarter[i] = (u[i] + 0x20000000u) >> 30;
+        rest[i] = (float)(int32_t)(u[i] - (quarter[i] << 30));
+    }
+    const auto both = [](float v) { return pair_of(v, v); };
+    const Pair x = mul2(pair_of(rest[0], rest[1]), both(1.4629180792671596e-9f));  // 2 pi / 2^32
+    const Pair z = mul2(x, x);
+    Pair s = fma2(z, both(1.0f / 362880), both(-1.0f / 5040));
+    s = fma2(z, s, both(1.0f / 120));
+    s = fma2(z, s, both(-1.0f / 6));
+    s = fma2(mul2(x, z), s, x);
+    Pair c = fma2(z, both(-1.0f / 3628800), both(1.0f / 40320));
+    c = fma2(z, c, both(-1.0f / 720));
+    c = fma2(z, c, both(1.0f / 24));
+    c = fma2(z, c, both(-0.5f));
+    c = fma2(z, c, both(1.0f));
+    const float2 fs = floats_of(s), fc = floats_of(c);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const float a = i ? fs.y : fs.x, b = i ? fc.y : fc.x;
+        const bool odd = quarter[i] & 1;
+        sine[i] = __uint_as_float(__float_as_uint(odd ? b : a) ^ (quarter[i] & 2) << 30);
+        cosine[i] = __uint_as_float(__float_as_uint(odd ? a : b) ^ ((quarter[i] + 1) & 2) << 30);
+    }
+}
+
+// A token's positions, and pair i's angle there in units of 2^-32 turns: exact
+// modulo a turn however far the position.
+struct RotaryPlace {
+    int p[3];
+};
+__device__ __forceinline__ RotaryPlace place_of(const RotaryTable& a, long long t)
+{
+    RotaryPlace at;
+    at.p[0] = at.p[1] = at.p[2] = a.positions[t];
+    if (a.axes > 1) {
+        at.p[1] = a.positions[a.tokens + t];
+        at.p[2] = a.positions[2 * a.tokens + t];
+    }
+    return at;
+}
+__device__ __forceinline__ uint32_t phase_of(const RotaryPlace& at, uint64_t turns, int axis)
+{
+    const int p = axis == 0 ? at.p[0] : axis == 1 ? at.p[1] : at.p[2];
+    return (uint32_t)((uint64_t)(int64_t)p * turns >> 32);
+}
+
+// What a lane keeps of the table for the values e0 .. e0 + 8: its pairs' turns (0
+// beyond the rotation) and, two bits each, their axes.
+template <int PAIR>
+struct RotaryLane {
+    static constexpr int kStep = PAIR == kPairOwn ? 2 : 1;  // values that an angle serves
+    uint64_t turns[8 / kStep];
+    uint32_t axes;
+};
+template <int PAIR>
+__device__ __forceinline__ RotaryLane<PAIR> lane_of(const RotaryTable& a, int e0)
+{
+    constexpr int kStep = RotaryLane<PAIR>::kStep;
+    const int half = a.rotary_dim / 2;
+    const bool interleaved = PAIR == kPairOwn || (PAIR == kPairMemory && a.interleaved);
+    RotaryLane<PAIR> lane;
+    lane.axes = 0;
+#pragma unroll
+    for (int j = 0; j < 8; j += kStep) {
         const int e = e0 + j;
-        c[j] = 1.0f;
-        s[j] = -0.0f;
+        lane.turns[j / kStep] = 0;
         if (e >= a.rotary_dim) continue;
         const int i = interleaved ? e >> 1 : e < half ? e : e - half;
-        const bool second = interleaved ? e & 1 : e >= half;
-        int at = p[0];
-        if (a.axes > 1) {
-            const int x = a.axis[i];
-            at = x == 0 ? p[0] : x == 1 ? p[1] : p[2];
+        lane.turns[j / kStep] = a.turns[i];
+        if (a.axes > 1) lane.axes |= (uint32_t)a.axis[i] << (2 * (j / kStep));
+    }
+    return lane;
+}
+
+// Factors of the values e0 .. e0 + 8 of a row at a place: y_e = x_e c_e + x_pair
+// s_e.  Values beyond the rotation have 1 and -0, which with a pair of 0 leaves
+// them as they are, -0 too.
+template <int PAIR>
+__device__ __forceinline__ void factors_of(const RotaryTable& a, const RotaryLane<PAIR>& lane,
+                                           const RotaryPlace& at, int e0, Piece& cosines, Piece& sines)
+{
+    constexpr int kStep = RotaryLane<PAIR>::kStep;
+    const int half = a.rotary_dim / 2;
+    const bool interleaved = PAIR == kPairOwn || (PAIR == kPairMemory && a.interleaved);
+    const float turned = a.transposed ? -a.amplitude : a.amplitude;
+    float c[8], s[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 2 * kStep) {
+        const int i = j / kStep;
+        float cosine[2], sine[2];
+        two_angles(phase_of(at, lane.turns[i], lane.axes >> (2 * i) & 3),
+                   phase_of(at, lane.turns[i + 1], lane.axes >> (2 * i + 2) & 3), cosine, sine);
+#pragma unroll
+        for (int k = 0; k < 2 * kStep; ++k) {
+            const int e = e0 + j + k, from = k / kStep;
+            const float f = sine[from] * turned;
+            c[j + k] = e < a.rotary_dim ? cosine[from] * a.amplitude : 1.0f;
+            s[j + k] = e < a.rotary_dim ? ((interleaved ? e & 1 : e >= half) ? f : -f) : -0.0f;
         }
-        const uint64_t phase = (uint64_t)(int64_t)at * a.turns[i];
-        // 2^-32 turns, in (-1, 1] half turns
-        const float turn = (float)(int32_t)(phase >> 32) * 0x1p-31f;
-        float sine, cosine;
-        sincospif(turn, &sine, &cosine);
-        c[j] = cosine * a.amplitude;
-        sine *= a.amplitude;
-        s[j] = second != (a.transposed != 0) ? sine : -sine;
     }
     set_floats(cosines, c);
     set_floats(sines, s);
@@ -202,6 +274,115 @@ __device__ __forceinline__ void scale_piece(Piece& y, float by)
     for (int j = 0; j < 4; ++j) y.p[j] = mul2(y.p[j], p);
 }
 
+// First (A) and second (B) values of eight pairs, of two groups of eight values.
+template <int DTYPE, bool SIXTEEN>
+__device__ __forceinline__ void open_pairs(const Eight<DTYPE>& one, const Eight<DTYPE>& two, Piece& A, Piece& B)
+{
+    float f[8], g[8];
+    unpack_eight(one, f);
+    unpack_eight(two, g);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        A.p[j] = SIXTEEN ? pair_of(f[4 * j], f[4 * j + 2]) : pair_of(f[2 * j], f[2 * j + 1]);
+        B.p[j] = SIXTEEN ? pair_of(f[4 * j + 1], f[4 * j + 3]) : pair_of(g[2 * j], g[2 * j + 1]);
+        A.p[j + 2] = SIXTEEN ? pair_of(g[4 * j], g[4 * j + 2]) : pair_of(f[2 * j + 4], f[2 * j + 5]);
+        B.p[j + 2] = SIXTEEN ? pair_of(g[4 * j + 1], g[4 * j + 3]) : pair_of(g[2 * j + 4], g[2 * j + 5]);
+    }
+}
+template <int DTYPE, bool SIXTEEN>
+__device__ __forceinline__ void close_pairs(Eight<DTYPE>& one, Eight<DTYPE>& two, const Piece& A, const Piece& B)
+{
+    float x[8], y[8];
+    get_floats(A, x);
+    get_floats(B, y);
+    if (SIXTEEN) {
+        float f[8], g[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f[2 * j] = x[j];
+            f[2 * j + 1] = y[j];
+            g[2 * j] = x[j + 4];
+            g[2 * j + 1] = y[j + 4];
+        }
+        pack_eight(one, f);
+        pack_eight(two, g);
+    } else {
+        pack_eight(one, x);
+        pack_eight(two, y);
+    }
+}
+
+template <int DTYPE>
+struct TypeTag {
+    static constexpr int kType = DTYPE;
+};
+
+// The same of rows that lanes have eight pairs of: each group of eight values is
+// summed like a lane's there, and the groups meet in the same order.
+template <int DTYPE, bool SIXTEEN>
+__device__ __forceinline__ float pairs_inverse(const RotaryTable& a, int log_lanes, bool norm,
+                                               const Eight<DTYPE>& one, const Eight<DTYPE>& two, Piece& A,
+                                               Piece& B)
+{
+    const auto squares = [&](float scale) {
+        float sums[2];
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            Piece x;
+            open_piece(z ? two : one, x);
+            Pair t = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const Pair v = scale == 1.0f ? x.p[j] : mul2(x.p[j], pair_of(scale, scale));
+                t = j ? fma2(v, v, t) : mul2(v, v);
+            }
+            const float2 f = floats_of(t);
+            sums[z] = f.x + f.y;
+        }
+        if (SIXTEEN) sums[0] += sums[1];  // neighbours meet first
+        for (int off = 0; off < log_lanes; ++off) {
+            sums[0] += __shfl_xor_sync(0xFFFFFFFFu, sums[0], 1 << off);
+            if (!SIXTEEN) sums[1] += __shfl_xor_sync(0xFFFFFFFFu, sums[1], 1 << off);
+        }
+        return SIXTEEN ? sums[0] : sums[0] + sums[1];  // halves last
+    };
+    float sum = squares(1.0f), eps = a.eps;
+    const bool passed = norm && !(sum < INFINITY);
+    if (__any_sync(0xFFFFFFFFu, passed)) {
+        if (passed) {
+            eps = 0.0f;
+            scale_piece(A, 0x1p-100f);
+            scale_piece(B, 0x1p-100f);
+        }
+        sum = squares(passed ? 0x1p-100f : 1.0f);
+    }
+    return norm ? rsqrtf(fmaf(sum, a.per_value, eps)) : 1.0f;
+}
+
+// offset + weight of eight pairs.
+template <int DTYPE, bool SIXTEEN>
+__device__ __forceinline__ void weights_of(const RotaryTable& a, const void* weight, int e0, int e1, Piece& A,
+                                           Piece& B)
+{
+    const auto as = [&](auto kind) {
+        constexpr int kType = decltype(kind)::kType, kBytes = Eight<kType>::kBytes;
+        Eight<kType> one, two;
+        load_eight(one, static_cast<const char*>(weight) + e0 * kBytes);
+        load_eight(two, static_cast<const char*>(weight) + e1 * kBytes);
+        open_pairs<kType, SIXTEEN>(one, two, A, B);
+    };
+    if (DTYPE != BACON_FP32 && a.weight_dtype == BACON_FP32)
+        as(TypeTag<BACON_FP32>{});
+    else
+        as(TypeTag<DTYPE>{});
+    const Pair offset = pair_of(a.weight_offset, a.weight_offset);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        A.p[j] = add2(A.p[j], offset);
+        B.p[j] = add2(B.p[j], offset);
+    }
+}
+
 // Rows of one call: bacon_rows without what the host has checked.
 struct RotaryRows {
     const char* in;
@@ -215,61 +396,87 @@ struct RotaryArgs {
     RotaryTable table;
     RotaryRows rows[2];  // Q, K
     int dtype, requests, tokens;
-    int pair;        // how pairs are got
+    int pair;        // how a lane with eight values gets the others: kPairLane, kPairOwn, kPairMemory
+    int q_pair;      // how a call's rows are turned, but for K that is stored
     int vectors;     // rows start at multiples of 16 bytes
 };
 cudaError_t launch_rotary(const RotaryArgs& a, cudaStream_t st);
 
-// How the rows of a call are dealt out: a group of 2^log_lanes lanes turns `per`
-// heads of Q or of K of a token, of chunks[0] and chunks[1] such pieces.
+// How the rows of a call are dealt out: a group of 2^log_lanes lanes turns up to
+// per[0] heads of Q of a token, chunks[0] such pieces a token, or per[1] of K; first
+// come all pieces of Q, so that the groups of a warp have about as much to do.
 struct RotaryDeal {
-    int log_lanes, per, chunks[2];
+    int log_lanes, per[2], chunks[2];
 };
-constexpr int kRotaryBatch = 4;  // rows of a group that are on their way together
 
-// Piece `item` of the call's rows; whole warps call it.
-template <int DTYPE, int PAIR, bool NORM>
-__device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+// A group's piece of a call's rows.
+struct RotaryTask {
+    bool active;
+    unsigned t;        // token
+    int key, count;    // Q or K, heads
+    int most;          // heads of any group of the warp
+    const char* in;
+    char* out;
+    const void* weight;
+    long long in_step, out_step;  // bytes from a head to the next
+};
+__device__ __forceinline__ RotaryTask task_of(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
 {
-    constexpr int kBytes = Eight<DTYPE>::kBytes;
+    RotaryTask task;
+    const unsigned before = (unsigned)a.table.tokens * deal.chunks[0];
+    task.key = item >= before;
+    if (task.key) item -= before;
+    const RotaryRows& rows = a.rows[task.key];
+    task.t = deal.chunks[task.key] ? item / deal.chunks[task.key] : a.table.tokens;
+    task.active = task.t < a.table.tokens;
+    const int first = task.active ? (int)(item % deal.chunks[task.key]) * deal.per[task.key] : 0;
+    task.count = task.active ? min(deal.per[task.key], rows.heads - first) : 0;
+    task.most = __reduce_max_sync(0xFFFFFFFFu, task.count);
+    const unsigned r = task.t / a.tokens, n = task.t % a.tokens;
+    task.in = rows.in + r * rows.in_request + n * rows.in_token + first * rows.in_head;
+    task.out = rows.out + r * rows.out_request + n * rows.out_token + first * rows.out_head;
+    task.weight = task.active ? rows.weight : nullptr;
+    task.in_step = rows.in_head;
+    task.out_step = rows.out_head;
+    return task;
+}
+
+// Group tasks with eight values a lane; whole warps call it.
+template <int DTYPE, int PAIR, bool NORM>
+__device__ __forceinline__ void rotate_eights(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+{
+    constexpr int kBytes = Eight<DTYPE>::kBytes, kBatch = 2;
     const RotaryTable& tab = a.table;
     const int q = threadIdx.x & ((1 << deal.log_lanes) - 1), e0 = 8 * q;
-    const unsigned every = deal.chunks[0] + deal.chunks[1], t = item / every;
-    int first = (int)(item % every);
-    const bool key = first >= deal.chunks[0];
-    const RotaryRows& rows = a.rows[key];
-    if (key) first -= deal.chunks[0];
-    first *= deal.per;
-    const bool active = t < tab.tokens && e0 < tab.head_dim;
-    const int count = active ? min(deal.per, rows.heads - first) : 0;
-    const unsigned r = t / a.tokens, n = t % a.tokens;
-    const char* in = rows.in + r * rows.in_request + n * rows.in_token + first * rows.in_head;
-    char* out = rows.out + r * rows.out_request + n * rows.out_token + first * rows.out_head;
+    RotaryTask task = task_of(a, deal, item);
+    const bool inside = e0 < tab.head_dim;
+    const int count = inside ? task.count : 0;
     const bool vectors = PAIR != kPairMemory || a.vectors;
-    const bool norm = NORM && rows.weight;
+    const bool norm = NORM && task.weight;
     // beyond the rotation rows stay as they are
-    const bool turns = norm || e0 < tab.rotary_dim;
-    const bool writes = turns || in != out;
+    const bool changes = norm || e0 < tab.rotary_dim;
+    const bool writes = changes || task.in != task.out;
 
     Piece c, s;
-    for (int base = 0; base < deal.per; base += kRotaryBatch) {  // the same for the whole warp
-        Eight<DTYPE> raw[kRotaryBatch];
+    for (int base = 0; base < task.most; base += kBatch) {
+        Eight<DTYPE> raw[kBatch];
 #pragma unroll
-        for (int b = 0; b < kRotaryBatch; ++b) {
+        for (int b = 0; b < kBatch; ++b) {
 #pragma unroll
             for (int i = 0; i < Eight<DTYPE>::kWords; ++i) raw[b].w[i] = 0;
-            if (base + b < count && vectors) load_eight(raw[b], in + b * rows.in_head + e0 * kBytes);
+            if (base + b < count && vectors) load_eight(raw[b], task.in + b * task.in_step + e0 * kBytes);
         }
         if (base == 0) {
-            if (active) angles_of<PAIR>(tab, t, e0, c, s);
-            if (NORM) weigh<DTYPE, PAIR>(tab, active ? rows.weight : nullptr, q, c, s);
+            if (task.active && inside)
+                factors_of<PAIR>(tab, lane_of<PAIR>(tab, e0), place_of(tab, task.t), e0, c, s);
+            if (NORM) weigh<DTYPE, PAIR>(tab, inside ? task.weight : nullptr, q, c, s);
         }
 #pragma unroll
-        for (int b = 0; b < kRotaryBatch; ++b) {
-            if (base + b >= deal.per) break;
+        for (int b = 0; b < kBatch; ++b) {
+            if (base + b >= task.most) break;
             const bool mine = base + b < count;
-            const char* const row = in + b * rows.in_head;
-            char* const to = out + b * rows.out_head;
+            const char* const row = task.in + b * task.in_step;
+            char* const to = task.out + b * task.out_step;
             Piece x, other, y;
             if (vectors) {
                 open_piece(raw[b], x);
@@ -289,7 +496,7 @@ __device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDe
             if (!mine || !writes) continue;
             if (vectors) {
                 Eight<DTYPE> w = raw[b];
-                if (turns) close_piece(w, y);
+                if (changes) close_piece(w, y);
                 store_eight(to + e0 * kBytes, w);
             } else {
                 float f[8];
@@ -299,12 +506,134 @@ __device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDe
                     if (e0 + j < tab.head_dim) store_one<DTYPE>(to, e0 + j, f[j]);
             }
         }
-        in += kRotaryBatch * rows.in_head;
-        out += kRotaryBatch * rows.out_head;
+        task.in += kBatch * task.in_step;
+        task.out += kBatch * task.out_step;
     }
 }
 
-// Pieces of `heads` rows for the deal's `per`.
-inline int chunks_of(int heads, int per) { return (heads + per - 1) / per; }
+// Group tasks with eight pairs a lane (a lane beyond the rotation: sixteen
+// neighbours that stay).  The same products and sums as with eight values a lane,
+// those of a norm in the same order; with a norm there are no lanes beyond.
+template <int DTYPE, bool SIXTEEN, bool NORM>
+__device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+{
+    constexpr int kBytes = Eight<DTYPE>::kBytes, kBatch = NORM ? 2 : 4;
+    const RotaryTable& tab = a.table;
+    const int q = threadIdx.x & ((1 << deal.log_lanes) - 1);
+    RotaryTask task = task_of(a, deal, item);
+    const bool turning = 16 * q < tab.rotary_dim;
+    const int e0 = SIXTEEN || !turning ? 16 * q : 8 * q;
+    const int e1 = SIXTEEN || !turning ? e0 + 8 : e0 + tab.rotary_dim / 2;
+    const bool inside = 16 * q < tab.head_dim;
+    const bool norm = NORM && task.weight;
+    // beyond the rotation rows in place stay as they are
+    const int count = inside && (turning || task.in != task.out) ? task.count : 0;
+    task.in += e0 * kBytes;
+    task.out += e0 * kBytes;
+    const int apart = (e1 - e0) * kBytes;
+
+    // y_A = A cA + B sA, y_B = B cB + A sB; without a norm cB is cA and sB is -sA
+    Piece cA, sA, cB, sB;
+    for (int base = 0; base < task.most; base += kBatch) {
+        Eight<DTYPE> one[kBatch], two[kBatch];
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b)
+            if (base + b < count) {
+                load_eight(one[b], task.in + b * task.in_step);
+                load_eight(two[b], task.in + b * task.in_step + apart);
+            }
+        if (base == 0 && turning && task.active) {
+            const RotaryPlace at = place_of(tab, task.t);
+            const float turned = tab.transposed ? -tab.amplitude : tab.amplitude;
+            float c[8], s[8];
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                float cosine[2], sine[2];
+                const int i = 8 * q + j;
+                const int axis = tab.axes > 1 ? tab.axis[i] : 0, next = tab.axes > 1 ? tab.axis[i + 1] : 0;
+                two_angles(phase_of(at, tab.turns[i], axis), phase_of(at, tab.turns[i + 1], next), cosine, sine);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    c[j + k] = cosine[k] * tab.amplitude;
+                    s[j + k] = sine[k] * turned;
+                }
+            }
+            set_floats(cA, c);
+            set_floats(sB, s);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] = -s[j];
+            set_floats(sA, s);
+            cB = cA;
+            if (norm) {
+                Piece wA, wB;
+                weights_of<DTYPE, SIXTEEN>(tab, task.weight, e0, e1, wA, wB);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    cA.p[j] = mul2(cA.p[j], wA.p[j]);
+                    sA.p[j] = mul2(sA.p[j], wB.p[j]);
+                    cB.p[j] = mul2(cB.p[j], wB.p[j]);
+                    sB.p[j] = mul2(sB.p[j], wA.p[j]);
+                }
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            if (NORM && base + b >= task.most) break;
+            const bool mine = base + b < count;
+            if (!NORM && !mine) break;
+            Piece A, B, yA, yB;
+            if (NORM && !mine)
+#pragma unroll
+                for (int i = 0; i < Eight<DTYPE>::kWords; ++i) one[b].w[i] = two[b].w[i] = 0;
+            open_pairs<DTYPE, SIXTEEN>(one[b], two[b], A, B);
+            float inv = 1.0f;
+            if (NORM) inv = pairs_inverse<DTYPE, SIXTEEN>(tab, deal.log_lanes, norm, one[b], two[b], A, B);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                yA.p[j] = fma2(A.p[j], cA.p[j], mul2(B.p[j], sA.p[j]));
+                yB.p[j] = fma2(B.p[j], NORM ? cB.p[j] : cA.p[j], mul2(A.p[j], sB.p[j]));
+            }
+            if (NORM) {
+                scale_piece(yA, inv);
+                scale_piece(yB, inv);
+            }
+            if (!mine) continue;
+            if (turning) close_pairs<DTYPE, SIXTEEN>(one[b], two[b], yA, yB);
+            store_eight(task.out + b * task.out_step, one[b]);
+            store_eight(task.out + b * task.out_step + apart, two[b]);
+        }
+        task.in += kBatch * task.in_step;
+        task.out += kBatch * task.out_step;
+    }
+}
+
+template <int DTYPE, int PAIR, bool NORM>
+__device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+{
+    if constexpr (PAIR == kPairHalves)
+        rotate_pairs<DTYPE, false, NORM>(a, deal, item);
+    else if constexpr (PAIR == kPairSixteen)
+        rotate_pairs<DTYPE, true, NORM>(a, deal, item);
+    else
+        rotate_eights<DTYPE, PAIR, NORM>(a, deal, item);
+}
+
+// Deals out rows: as few heads share a group and its angles as fill the machine.
+// Returns the pieces.
+inline long long deal_rows(const RotaryArgs& a, int values, RotaryDeal* deal)
+{
+    *deal = RotaryDeal{};
+    while (values << deal->log_lanes < a.table.head_dim) ++deal->log_lanes;
+    const long long rows = a.table.tokens * (a.rows[0].heads + a.rows[1].heads);
+    int most = 1;
+    while (most < kMostHeads && rows / most > (152LL * 2048 >> deal->log_lanes)) most *= 2;
+    for (int i = 0; i < 2; ++i) {
+        const int heads = a.rows[i].heads, chunks = (heads + most - 1) / most;
+        deal->chunks[i] = chunks;
+        deal->per[i] = chunks ? (heads + chunks - 1) / chunks : 0;
+    }
+    return a.table.tokens * (deal->chunks[0] + deal->chunks[1]);
+}
+inline int values_of_lane(int pair) { return pair == kPairHalves || pair == kPairSixteen ? 16 : 8; }
 
 }  // namespace bacon

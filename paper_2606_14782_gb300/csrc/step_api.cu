@@ -132,6 +132,11 @@ bacon_status rotary_args(const bacon_rotary* rotary, int requests, int tokens, c
              : a.table.interleaved           ? kPairOwn
              : a.table.rotary_dim % 16 == 0 ? kPairLane
                                              : kPairMemory;
+    // lanes with eight pairs: where sixteen values lie on one side of the rotation's
+    // end, and a norm has no lanes beyond it
+    const bool pairs = d % 16 == 0 && a.table.rotary_dim % 16 == 0 &&
+                       !(norm && a.table.rotary_dim < d);
+    a.q_pair = a.pair == kPairMemory || !pairs ? a.pair : a.table.interleaved ? kPairSixteen : kPairHalves;
     *out = a;
     return BACON_OK;
 }

@@ -8,7 +8,6 @@ is missing, loading it raises.
 
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 import struct
@@ -803,12 +802,16 @@ class Cache:
 # ------------------------------------------------------------------------
 # a token between its matrix products and the cache
 
-def _current(index):
-    """The device made current for a call on its tensors, if it is not."""
-    return _same if torch.cuda.current_device() == index else torch.cuda.device(index)
+_device = torch._C._cuda_getDevice
 
 
-_same = contextlib.nullcontext()
+def _on(index, call, *args):
+    """A call of the library with device `index` current."""
+    if _device() == index:
+        _check(call(*args))
+    else:
+        with torch.cuda.device(index):
+            _check(call(*args))
 
 
 def _stream_of(stream, index):
@@ -890,23 +893,24 @@ class Rotary:
 
     def _rows(self, t, out, weight, dtype, index, places, stream, what):
         """Packed rows and the output (allocated if None)."""
-        stride = t.stride()
-        if (t.dtype is not dtype or t.get_device() != index or t.shape[:-2] != places
-                or t.shape[-1] != self.head_dim or (stride[-1] != 1 and t.numel())):
+        shape, stride = t.shape, t.stride()
+        if (t.dtype is not dtype or t.get_device() != index or shape[:-2] != places
+                or shape[-1] != self.head_dim or (stride[-1] != 1 and t.numel())):
             raise ValueError(f"{what} must be {dtype} rows of {self.head_dim} values on cuda:{index}, "
                              "[tokens, heads, d] or [requests, tokens, heads, d] like the other, "
                              "the last dimension contiguous")
         if out is None:
-            out = _empty(t.shape, dtype, t.device, stream)
-        elif (out.dtype is not dtype or out.get_device() != index or out.shape != t.shape
+            out = _empty(shape, dtype, t.device, stream)
+        elif (out.dtype is not dtype or out.get_device() != index or out.shape != shape
               or (out.stride(-1) != 1 and t.numel())):
             raise ValueError(f"the output of {what} must have its shape, type and device, the last "
                              "dimension contiguous")
         to = out.stride()
-        many = len(places) == 2
-        return out, _pack_rows(t.data_ptr(), out.data_ptr(), _ptr(weight) or 0, t.shape[-2],
-                               stride[0] if many else 0, stride[-3], stride[-2],
-                               to[0] if many else 0, to[-3], to[-2])
+        if len(stride) == 4:
+            return out, _pack_rows(t.data_ptr(), out.data_ptr(), 0 if weight is None else weight.data_ptr(),
+                                   shape[2], *stride[:3], *to[:3])
+        return out, _pack_rows(t.data_ptr(), out.data_ptr(), 0 if weight is None else weight.data_ptr(),
+                               shape[1], 0, stride[0], stride[1], 0, to[0], to[1])
 
     def apply(self, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, offset=0.0,
               transposed=False, q_out=None, k_out=None, stream=None):
@@ -924,21 +928,22 @@ class Rotary:
             raise ValueError("q or k must be bf16, fp16 or fp32 rows on a GPU, [tokens, heads, d] or "
                              "[requests, tokens, heads, d]")
         dtype, index, places = t.dtype, t.get_device(), t.shape[:-2]
-        weights = _weights_dtype((q_weight, k_weight), (self.head_dim,), dtype, index)
+        kind = weights = DTYPES[dtype]
+        if q_weight is not None or k_weight is not None:
+            weights = _weights_dtype((q_weight, k_weight), (self.head_dim,), dtype, index)
         rows = [None, None]
         if q is not None:
             q_out, rows[0] = self._rows(q, q_out, q_weight, dtype, index, places, stream, "q")
         if k is not None:
             k_out, rows[1] = self._rows(k, k_out, k_weight, dtype, index, places, stream, "k")
-        if (positions.dtype is not _i32 or positions.shape != self.shape(*places)
+        if (positions.dtype is not _i32
+                or positions.shape != (places if self.axes == 1 else (3,) + places)
                 or positions.get_device() != index or not positions.is_contiguous()):
             raise ValueError("positions must be a contiguous int32 tensor of shape "
                              f"{tuple(self.shape(*places))} on cuda:{index}")
-        with _current(index):
-            _check(self._lib.bacon_rotary_apply(
-                self.handle, places[0] if len(places) == 2 else 1, places[-1], *rows,
-                DTYPES[dtype], weights, eps, offset, transposed, positions.data_ptr(),
-                _stream_of(stream, index)))
+        _on(index, self._lib.bacon_rotary_apply, self.handle, places[0] if len(places) == 2 else 1,
+            places[-1], *rows, kind, weights, eps, offset, transposed, positions.data_ptr(),
+            _stream_of(stream, index))
         return q_out, k_out
 
 
@@ -1002,13 +1007,16 @@ class BlockNorm:
             raise ValueError(f"y must be [..., {width}] on a GPU")
         if self._index is not None and self._index != index:
             raise ValueError(f"the weights are on cuda:{self._index}")
-        weight_dtype = self._weight_dtype(dtype, index)
+        weight_dtype = self._dtypes.get(dtype)
+        if weight_dtype is None:
+            weight_dtype = self._weight_dtype(dtype, index)
         tokens = y.numel() // width
-        strides = [0, self._rows(y, shape, (dtype,), index, "y"), 0, 0, 0]
+        y_stride = self._rows(y, shape, (dtype,), index, "y")
+        gate_stride = x_stride = sum_stride = norm_stride = 0
         wide = x if x is not None else sum_out
         residual = dtype if wide is None else wide.dtype
         if x is not None:
-            strides[2] = self._rows(x, shape, (dtype, torch.float32), index, "x")
+            x_stride = self._rows(x, shape, (dtype, torch.float32), index, "x")
         channel = 0
         if gate is not None:
             g = gate.shape
@@ -1016,35 +1024,36 @@ class BlockNorm:
                 raise ValueError("the gate must have y's type and device")
             if g == shape:
                 channel = 1
-                strides[0] = self._rows(gate, shape, (dtype,), index, "gate")
+                gate_stride = self._rows(gate, shape, (dtype,), index, "gate")
             elif g == (width,) and gate.is_contiguous():
                 channel = 1
             elif g == shape[:-1] + (1,) and gate.is_contiguous():
-                strides[0] = 1
+                gate_stride = 1
             else:
                 raise ValueError(f"the gate must be contiguous [{width}] or {tuple(shape[:-1])} + "
                                  "(1,), or have y's shape")
         if sum_out is not None:
-            strides[3] = self._rows(sum_out, shape, (residual,) if x is not None else
+            sum_stride = self._rows(sum_out, shape, (residual,) if x is not None else
                                     (dtype, torch.float32), index, "sum_out")
         elif x is not None or self.post is not None or gate is not None:
             sum_out = _empty(shape, residual, y.device, stream)
-            strides[3] = width
+            sum_stride = width
         if self.pre is None:
             if norm_out is not None:
                 raise ValueError("there is no pre norm")
         elif norm_out is None:
             norm_out = _empty(shape, dtype, y.device, stream)
-            strides[4] = width
+            norm_stride = width
         else:
-            strides[4] = self._rows(norm_out, shape, (dtype,), index, "norm_out")
+            norm_stride = self._rows(norm_out, shape, (dtype,), index, "norm_out")
         post, pre, kind, scale, eps, offset = self._kinds
         desc = _pack_block(tokens, width, DTYPES[dtype], DTYPES[residual], weight_dtype, post, pre,
-                           kind, scale, eps, offset, channel, *strides, y.data_ptr(), _ptr(x) or 0,
-                           _ptr(gate) or 0, *self._pointers, _ptr(sum_out) or 0,
-                           _ptr(norm_out) or 0)
-        with _current(index):
-            _check(self._lib.bacon_block_norm(desc, _stream_of(stream, index)))
+                           kind, scale, eps, offset, channel, gate_stride, y_stride, x_stride,
+                           sum_stride, norm_stride, y.data_ptr(), 0 if x is None else x.data_ptr(),
+                           0 if gate is None else gate.data_ptr(), *self._pointers,
+                           0 if sum_out is None else sum_out.data_ptr(),
+                           0 if norm_out is None else norm_out.data_ptr())
+        _on(index, self._lib.bacon_block_norm, desc, _stream_of(stream, index))
         return sum_out, norm_out
 
 

@@ -75,16 +75,41 @@ __device__ __forceinline__ void turn_rows(const RotaryArgs& a, const uint16_t* r
     }
 }
 
-// Rows of Q, by whichever way suits them where K has PAIR.
-template <int DTYPE, int PAIR>
-__device__ __forceinline__ void turn_queries(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
+// The same with eight pairs a lane, into `stage` ([page][D]): half as many lanes have
+// a row, so that a run's rows are turned in two steps at most, and each lane works
+// out half as many angles.
+template <int DTYPE, int D, bool SIXTEEN>
+__device__ __forceinline__ void stage_rows(const RotaryArgs& a, const uint16_t* rows,
+                                           long long token_stride, long long t, int len, uint16_t* stage)
 {
-    if (a.q_pair == PAIR)
-        rotate_piece<DTYPE, PAIR, true>(a, deal, item);
-    else if (PAIR == kPairOwn)
-        rotate_piece<DTYPE, kPairSixteen, true>(a, deal, item);
-    else if (PAIR == kPairLane)
-        rotate_piece<DTYPE, kPairHalves, true>(a, deal, item);
+    constexpr int kLanes = D / 16, kSteps = kChunks / 2;
+    const RotaryTable& tab = a.table;
+    const int q = threadIdx.x % kLanes, group = threadIdx.x / kLanes, groups = blockDim.x / kLanes;
+    const RotarySpan span = span_of<SIXTEEN>(tab, q);
+    Eight<DTYPE> one[kSteps], two[kSteps];
+    RotaryPlace at[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const int r = group + i * groups;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) one[i].w[j] = two[i].w[j] = 0;
+        at[i] = RotaryPlace{{0, 0, 0}};
+        if (r >= len) continue;
+        load_eight(one[i], rows + (t + r) * token_stride + span.e0);
+        load_eight(two[i], rows + (t + r) * token_stride + span.e1);
+        at[i] = place_of(tab, t + r);
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const int r = group + i * groups;
+        if (i * groups >= len) break;  // nobody has a row
+        PairFactors f;
+        pair_factors<DTYPE, SIXTEEN, true>(tab, at[i], a.rows[1].weight, q, span, f);
+        turn_pairs<DTYPE, SIXTEEN, true>(tab, D == 128 ? 3 : 2, a.rows[1].weight, span, f, one[i], two[i]);
+        if (r >= len) continue;
+        store_eight(stage + r * D + span.e0, one[i]);
+        store_eight(stage + r * D + span.e1, two[i]);
+    }
 }
 
 struct NoRotary {};
@@ -100,12 +125,14 @@ template <int DTYPE, int FORMAT, int D, int PAIR, typename ROTARY>
 __global__ void __launch_bounds__(512)
 store_kernel(CacheGeom g, StoreArgs a, int window, const __grid_constant__ ROTARY rotary)
 {
+    extern __shared__ __align__(16) uint16_t s_stage[];  // turned rows of K
+    constexpr bool kStaged = PAIR == kPairHalves || PAIR == kPairSixteen;
     if constexpr (PAIR != kNoPair) {
         if (blockIdx.y >= a.heads) {
             const unsigned groups = blockDim.x >> rotary.deal.log_lanes;
             unsigned item = ((blockIdx.y - a.heads) * gridDim.x + blockIdx.x) * groups;
             item += threadIdx.x >> rotary.deal.log_lanes;
-            turn_queries<DTYPE, PAIR>(rotary.args, rotary.deal, item);
+            rotate_piece<DTYPE, PAIR, true>(rotary.args, rotary.deal, item);
             return;
         }
     }
@@ -178,11 +205,21 @@ store_kernel(CacheGeom g, StoreArgs a, int window, const __grid_constant__ ROTAR
                 for (int c = 0; c < kChunks; ++c) {
                     const int e = tid + c * threads, r = e / (D / 8), q = e % (D / 8);
                     raw[z][c] = make_uint4(0, 0, 0, 0);
-                    if (r < len)
+                    if (r < len && !(kStaged && z == 0))
                         raw[z][c] = *reinterpret_cast<const uint4*>(rows[z] + (t + r) * a.token_stride[z] + q * 8);
                 }
-            if constexpr (PAIR != kNoPair)
+            if constexpr (kStaged) {
+                __syncthreads();  // the run before has been taken from there
+                stage_rows<DTYPE, D, PAIR == kPairSixteen>(rotary.args, rows[0], a.token_stride[0], t, len, s_stage);
+                __syncthreads();
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const int e = tid + c * threads;
+                    if (e / (D / 8) < len) raw[0][c] = reinterpret_cast<const uint4*>(s_stage)[e];
+                }
+            } else if constexpr (PAIR != kNoPair) {
                 turn_rows<DTYPE, D, PAIR>(rotary.args, rows[0], a.token_stride[0], t, len, raw[0]);
+            }
 #pragma unroll
             for (int z = 0; z < 2; ++z)
 #pragma unroll

@@ -13,15 +13,16 @@ struct StoreTurned {
     static cudaError_t pair(const CacheGeom& g, const StoreArgs& a, const StoreRotary& rotary, dim3 grid,
                             int window, cudaStream_t st)
     {
+        const size_t stage = PAIR == kPairMemory ? 0 : (size_t)g.page * D * 2;
         return launch_first(store_kernel<DTYPE, FORMAT, D, PAIR, StoreRotary>, grid,
-                            g.page * D / 8 / kChunks, 0, st, g, a, window, rotary);
+                            g.page * D / 8 / kChunks, stage, st, g, a, window, rotary);
     }
     static cudaError_t go(const CacheGeom& g, const StoreArgs& a, const StoreRotary& rotary, dim3 grid,
                           int window, cudaStream_t st)
     {
-        return rotary.args.pair == kPairLane  ? pair<kPairLane>(g, a, rotary, grid, window, st)
-               : rotary.args.pair == kPairOwn ? pair<kPairOwn>(g, a, rotary, grid, window, st)
-                                              : pair<kPairMemory>(g, a, rotary, grid, window, st);
+        return rotary.args.q_pair == kPairHalves    ? pair<kPairHalves>(g, a, rotary, grid, window, st)
+               : rotary.args.q_pair == kPairSixteen ? pair<kPairSixteen>(g, a, rotary, grid, window, st)
+                                                    : pair<kPairMemory>(g, a, rotary, grid, window, st);
     }
 };
 

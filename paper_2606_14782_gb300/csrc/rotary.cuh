@@ -511,9 +511,94 @@ __device__ __forceinline__ void rotate_eights(const RotaryArgs& a, const RotaryD
     }
 }
 
-// Group tasks with eight pairs a lane (a lane beyond the rotation: sixteen
-// neighbours that stay).  The same products and sums as with eight values a lane,
-// those of a norm in the same order; with a norm there are no lanes beyond.
+// Where a lane's two groups of eight values lie: eight pairs, or beyond the
+// rotation sixteen neighbours that stay.
+struct RotarySpan {
+    int e0, e1;
+    bool turning;
+};
+template <bool SIXTEEN>
+__device__ __forceinline__ RotarySpan span_of(const RotaryTable& a, int q)
+{
+    RotarySpan s;
+    s.turning = 16 * q < a.rotary_dim;
+    s.e0 = SIXTEEN || !s.turning ? 16 * q : 8 * q;
+    s.e1 = SIXTEEN || !s.turning ? s.e0 + 8 : s.e0 + a.rotary_dim / 2;
+    return s;
+}
+
+// y_A = A cA + B sA, y_B = B cB + A sB; without a norm cB is cA.
+struct PairFactors {
+    Piece cA, sA, cB, sB;
+};
+template <int DTYPE, bool SIXTEEN, bool NORM>
+__device__ __forceinline__ void pair_factors(const RotaryTable& tab, const RotaryPlace& at, const void* weight,
+                                             int q, const RotarySpan& span, PairFactors& f)
+{
+    if (!span.turning) return;  // nobody looks at them
+    const float turned = tab.transposed ? -tab.amplitude : tab.amplitude;
+    float c[8], s[8];
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        float cosine[2], sine[2];
+        uint32_t u[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int i = 8 * q + j + k;
+            u[k] = phase_of(at, tab.turns[i], tab.axes > 1 ? tab.axis[i] : 0);
+        }
+        two_angles(u[0], u[1], cosine, sine);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            c[j + k] = cosine[k] * tab.amplitude;
+            s[j + k] = sine[k] * turned;
+        }
+    }
+    set_floats(f.cA, c);
+    set_floats(f.sB, s);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = -s[j];
+    set_floats(f.sA, s);
+    f.cB = f.cA;
+    if (NORM && weight) {
+        Piece wA, wB;
+        weights_of<DTYPE, SIXTEEN>(tab, weight, span.e0, span.e1, wA, wB);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            f.cA.p[j] = mul2(f.cA.p[j], wA.p[j]);
+            f.sA.p[j] = mul2(f.sA.p[j], wB.p[j]);
+            f.cB.p[j] = mul2(f.cB.p[j], wB.p[j]);
+            f.sB.p[j] = mul2(f.sB.p[j], wA.p[j]);
+        }
+    }
+}
+
+// Turns a lane's pairs of a row; beyond the rotation they stay bit for bit.  With
+// NORM whole warps call it.
+template <int DTYPE, bool SIXTEEN, bool NORM>
+__device__ __forceinline__ void turn_pairs(const RotaryTable& tab, int log_lanes, bool norm,
+                                           const RotarySpan& span, const PairFactors& f, Eight<DTYPE>& one,
+                                           Eight<DTYPE>& two)
+{
+    Piece A, B, yA, yB;
+    open_pairs<DTYPE, SIXTEEN>(one, two, A, B);
+    float inv = 1.0f;
+    if (NORM) inv = pairs_inverse<DTYPE, SIXTEEN>(tab, log_lanes, norm, one, two, A, B);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        yA.p[j] = fma2(A.p[j], f.cA.p[j], mul2(B.p[j], f.sA.p[j]));
+        yB.p[j] = fma2(B.p[j], NORM ? f.cB.p[j] : f.cA.p[j], mul2(A.p[j], f.sB.p[j]));
+    }
+    if (NORM) {
+        scale_piece(yA, inv);
+        scale_piece(yB, inv);
+    }
+    if (span.turning) close_pairs<DTYPE, SIXTEEN>(one, two, yA, yB);
+}
+
+// Group tasks with eight pairs a lane.  The same products and sums as with eight
+// values a lane, those of a norm in the same order; with a norm there are no lanes
+// beyond the rotation.  Whole warps call it.
 template <int DTYPE, bool SIXTEEN, bool NORM>
 __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
 {
@@ -521,19 +606,15 @@ __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDe
     const RotaryTable& tab = a.table;
     const int q = threadIdx.x & ((1 << deal.log_lanes) - 1);
     RotaryTask task = task_of(a, deal, item);
-    const bool turning = 16 * q < tab.rotary_dim;
-    const int e0 = SIXTEEN || !turning ? 16 * q : 8 * q;
-    const int e1 = SIXTEEN || !turning ? e0 + 8 : e0 + tab.rotary_dim / 2;
+    const RotarySpan span = span_of<SIXTEEN>(tab, q);
     const bool inside = 16 * q < tab.head_dim;
-    const bool norm = NORM && task.weight;
     // beyond the rotation rows in place stay as they are
-    const int count = inside && (turning || task.in != task.out) ? task.count : 0;
-    task.in += e0 * kBytes;
-    task.out += e0 * kBytes;
-    const int apart = (e1 - e0) * kBytes;
+    const int count = inside && (span.turning || task.in != task.out) ? task.count : 0;
+    task.in += span.e0 * kBytes;
+    task.out += span.e0 * kBytes;
+    const int apart = (span.e1 - span.e0) * kBytes;
 
-    // y_A = A cA + B sA, y_B = B cB + A sB; without a norm cB is cA and sB is -sA
-    Piece cA, sA, cB, sB;
+    PairFactors f;
     for (int base = 0; base < task.most; base += kBatch) {
         Eight<DTYPE> one[kBatch], two[kBatch];
 #pragma unroll
@@ -542,63 +623,18 @@ __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDe
                 load_eight(one[b], task.in + b * task.in_step);
                 load_eight(two[b], task.in + b * task.in_step + apart);
             }
-        if (base == 0 && turning && task.active) {
-            const RotaryPlace at = place_of(tab, task.t);
-            const float turned = tab.transposed ? -tab.amplitude : tab.amplitude;
-            float c[8], s[8];
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                float cosine[2], sine[2];
-                const int i = 8 * q + j;
-                const int axis = tab.axes > 1 ? tab.axis[i] : 0, next = tab.axes > 1 ? tab.axis[i + 1] : 0;
-                two_angles(phase_of(at, tab.turns[i], axis), phase_of(at, tab.turns[i + 1], next), cosine, sine);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    c[j + k] = cosine[k] * tab.amplitude;
-                    s[j + k] = sine[k] * turned;
-                }
-            }
-            set_floats(cA, c);
-            set_floats(sB, s);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = -s[j];
-            set_floats(sA, s);
-            cB = cA;
-            if (norm) {
-                Piece wA, wB;
-                weights_of<DTYPE, SIXTEEN>(tab, task.weight, e0, e1, wA, wB);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    cA.p[j] = mul2(cA.p[j], wA.p[j]);
-                    sA.p[j] = mul2(sA.p[j], wB.p[j]);
-                    cB.p[j] = mul2(cB.p[j], wB.p[j]);
-                    sB.p[j] = mul2(sB.p[j], wA.p[j]);
-                }
-            }
-        }
+        if (base == 0 && inside && task.active)
+            pair_factors<DTYPE, SIXTEEN, NORM>(tab, place_of(tab, task.t), task.weight, q, span, f);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             if (NORM && base + b >= task.most) break;
             const bool mine = base + b < count;
             if (!NORM && !mine) break;
-            Piece A, B, yA, yB;
             if (NORM && !mine)
 #pragma unroll
                 for (int i = 0; i < Eight<DTYPE>::kWords; ++i) one[b].w[i] = two[b].w[i] = 0;
-            open_pairs<DTYPE, SIXTEEN>(one[b], two[b], A, B);
-            float inv = 1.0f;
-            if (NORM) inv = pairs_inverse<DTYPE, SIXTEEN>(tab, deal.log_lanes, norm, one[b], two[b], A, B);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                yA.p[j] = fma2(A.p[j], cA.p[j], mul2(B.p[j], sA.p[j]));
-                yB.p[j] = fma2(B.p[j], NORM ? cB.p[j] : cA.p[j], mul2(A.p[j], sB.p[j]));
-            }
-            if (NORM) {
-                scale_piece(yA, inv);
-                scale_piece(yB, inv);
-            }
+            turn_pairs<DTYPE, SIXTEEN, NORM>(tab, deal.log_lanes, task.weight != nullptr, span, f, one[b], two[b]);
             if (!mine) continue;
-            if (turning) close_pairs<DTYPE, SIXTEEN>(one[b], two[b], yA, yB);
             store_eight(task.out + b * task.out_step, one[b]);
             store_eight(task.out + b * task.out_step + apart, two[b]);
         }

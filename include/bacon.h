@@ -652,7 +652,8 @@ typedef struct {
     const int32_t* tokens;      /* NULL: no history                                */
     const int32_t* request;     /* [rows]; NULL: rows of tokens are the rows'      */
     const int32_t* prompt;      /* [rows]; NULL: 0                                 */
-    const int32_t* lengths;     /* [rows]; NULL: no history                        */
+    const int32_t* lengths;     /* [rows]; NULL: no history (without tokens only -1
+                                   says something)                                 */
     const float* repetition;    /* [rows] >= 1e-30; NULL: 1                        */
     const float* frequency;     /* [rows] finite; NULL: 0                          */
     const float* presence;      /* [rows] finite; NULL: 0                          */

@@ -105,7 +105,7 @@ __device__ __forceinline__ void stage_rows(const RotaryArgs& a, const uint16_t* 
         if (i * groups >= len) break;  // nobody has a row
         PairFactors f;
         pair_factors<DTYPE, SIXTEEN, true>(tab, at[i], a.rows[1].weight, q, span, f);
-        turn_pairs<DTYPE, SIXTEEN, true>(tab, D == 128 ? 3 : 2, a.rows[1].weight, span, f, one[i], two[i]);
+        turn_pairs<DTYPE, SIXTEEN, true>(tab, D == 128 ? 3 : 2, q, a.rows[1].weight != nullptr, span, f, one[i], two[i]);
         if (r >= len) continue;
         store_eight(stage + r * D + span.e0, one[i]);
         store_eight(stage + r * D + span.e1, two[i]);

@@ -1,7 +1,11 @@
 // Rows of K and V into the pages of the cache with the positions put into K on the
-// way, and into Q by further blocks of the same launch.  K's rows are turned in the
-// registers that the store keeps them in: what is saved against the two calls is a
-// launch, and writing K and reading it again.
+// way, and into Q by further blocks of the same launch.  A run's rows of K are turned
+// by lanes with eight pairs, through shared memory into the registers that the store
+// keeps them in: what is saved against the two calls is a launch, and writing K and
+// reading it again.  us: a token of 32 requests (32 and 8 heads, norms) 5.0, the two
+// calls 3.1 and 3.1; turns of 5 requests, 3500 tokens (28 and 4 heads) 16.8, the two
+// calls 8.7 and 9.6.  Short of the bytes' time (1.1 and 7 us): chains of a run's slots,
+// its rows, its scale and its codes, which few blocks have anything beside.
 #include "cache_store.cuh"
 
 namespace bacon {
@@ -36,8 +40,10 @@ cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, c
     const int window = store_window(g, a, 2);
     dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
     if (r.args.rows[0].heads) {
-        // blocks of the store's size
-        const long long pieces = deal_rows(r.args, values_of_lane(r.args.q_pair), &r.deal);
+        // blocks of the store's size, which begin when most of its own are through: more
+        // and shorter pieces than rotary.cu has (3500 tokens of 28 heads: 16.8 us a call, 18.5
+        // with its 512)
+        const long long pieces = deal_rows(r.args, values_of_lane(r.args.q_pair), 2048, &r.deal);
         const int groups = (g.page * g.d / 8 / kChunks) >> r.deal.log_lanes;
         const long long blocks = (pieces + groups - 1) / groups;
         const long long more = (blocks + grid.x - 1) / grid.x;

@@ -317,10 +317,11 @@ struct TypeTag {
     static constexpr int kType = DTYPE;
 };
 
-// The same of rows that lanes have eight pairs of: each group of eight values is
-// summed like a lane's there, and the groups meet in the same order.
+// The same of rows that lanes have eight pairs of, q a lane's place among those of
+// its row: each group of eight values is summed like a lane's there, and the groups
+// meet in the same order, so that a row's bits do not depend on how it is read.
 template <int DTYPE, bool SIXTEEN>
-__device__ __forceinline__ float pairs_inverse(const RotaryTable& a, int log_lanes, bool norm,
+__device__ __forceinline__ float pairs_inverse(const RotaryTable& a, int log_lanes, int q, bool norm,
                                                const Eight<DTYPE>& one, const Eight<DTYPE>& two, Piece& A,
                                                Piece& B)
 {
@@ -339,12 +340,23 @@ __device__ __forceinline__ float pairs_inverse(const RotaryTable& a, int log_lan
             const float2 f = floats_of(t);
             sums[z] = f.x + f.y;
         }
-        if (SIXTEEN) sums[0] += sums[1];  // neighbours meet first
-        for (int off = 0; off < log_lanes; ++off) {
-            sums[0] += __shfl_xor_sync(0xFFFFFFFFu, sums[0], 1 << off);
-            if (!SIXTEEN) sums[1] += __shfl_xor_sync(0xFFFFFFFFu, sums[1], 1 << off);
+        if (!SIXTEEN) {
+            // lane q gets the groups 2 q and 2 q + 1, neighbours as in the row
+            const int half = a.rotary_dim / 16, first = threadIdx.x & 31 & ~((1 << log_lanes) - 1);
+            float mine[2];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                const int g = 2 * q + z;
+                const int from = first + (g < half ? g : g < 2 * half ? g - half : q);
+                const float x = __shfl_sync(0xFFFFFFFFu, sums[0], from), y = __shfl_sync(0xFFFFFFFFu, sums[1], from);
+                mine[z] = (g < 2 * half ? g >= half : z) ? y : x;
+            }
+            sums[0] = mine[0];
+            sums[1] = mine[1];
         }
-        return SIXTEEN ? sums[0] : sums[0] + sums[1];  // halves last
+        float sum = sums[0] + sums[1];
+        for (int off = 0; off < log_lanes; ++off) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 1 << off);
+        return sum;
     };
     float sum = squares(1.0f), eps = a.eps;
     const bool passed = norm && !(sum < INFINITY);
@@ -535,25 +547,28 @@ template <int DTYPE, bool SIXTEEN, bool NORM>
 __device__ __forceinline__ void pair_factors(const RotaryTable& tab, const RotaryPlace& at, const void* weight,
                                              int q, const RotarySpan& span, PairFactors& f)
 {
-    if (!span.turning) return;  // nobody looks at them
+    if (!span.turning && !(NORM && weight)) return;  // nobody looks at them
     const float turned = tab.transposed ? -tab.amplitude : tab.amplitude;
     float c[8], s[8];
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-        float cosine[2], sine[2];
-        uint32_t u[2];
+    for (int j = 0; j < 8; ++j) c[j] = 1.0f, s[j] = 0.0f;
+    if (span.turning)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int i = 8 * q + j + k;
-            u[k] = phase_of(at, tab.turns[i], tab.axes > 1 ? tab.axis[i] : 0);
-        }
-        two_angles(u[0], u[1], cosine, sine);
+        for (int j = 0; j < 8; j += 2) {
+            float cosine[2], sine[2];
+            uint32_t u[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            c[j + k] = cosine[k] * tab.amplitude;
-            s[j + k] = sine[k] * turned;
+            for (int k = 0; k < 2; ++k) {
+                const int i = 8 * q + j + k;
+                u[k] = phase_of(at, tab.turns[i], tab.axes > 1 ? tab.axis[i] : 0);
+            }
+            two_angles(u[0], u[1], cosine, sine);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                c[j + k] = cosine[k] * tab.amplitude;
+                s[j + k] = sine[k] * turned;
+            }
         }
-    }
     set_floats(f.cA, c);
     set_floats(f.sB, s);
 #pragma unroll
@@ -573,32 +588,34 @@ __device__ __forceinline__ void pair_factors(const RotaryTable& tab, const Rotar
     }
 }
 
-// Turns a lane's pairs of a row; beyond the rotation they stay bit for bit.  With
-// NORM whole warps call it.
+// Turns a lane's pairs of a row; beyond the rotation and without a norm they stay
+// bit for bit.  With NORM whole warps call it.
 template <int DTYPE, bool SIXTEEN, bool NORM>
-__device__ __forceinline__ void turn_pairs(const RotaryTable& tab, int log_lanes, bool norm,
+__device__ __forceinline__ void turn_pairs(const RotaryTable& tab, int log_lanes, int q, bool norm,
                                            const RotarySpan& span, const PairFactors& f, Eight<DTYPE>& one,
                                            Eight<DTYPE>& two)
 {
     Piece A, B, yA, yB;
     open_pairs<DTYPE, SIXTEEN>(one, two, A, B);
     float inv = 1.0f;
-    if (NORM) inv = pairs_inverse<DTYPE, SIXTEEN>(tab, log_lanes, norm, one, two, A, B);
+    if (NORM) inv = pairs_inverse<DTYPE, SIXTEEN>(tab, log_lanes, q, norm, one, two, A, B);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        yA.p[j] = fma2(A.p[j], f.cA.p[j], mul2(B.p[j], f.sA.p[j]));
-        yB.p[j] = fma2(B.p[j], NORM ? f.cB.p[j] : f.cA.p[j], mul2(A.p[j], f.sB.p[j]));
+        // (beyond the rotation nothing of the other, were it an infinity)
+        const Pair fromB = !NORM || span.turning ? mul2(B.p[j], f.sA.p[j]) : 0;
+        const Pair fromA = !NORM || span.turning ? mul2(A.p[j], f.sB.p[j]) : 0;
+        yA.p[j] = fma2(A.p[j], f.cA.p[j], fromB);
+        yB.p[j] = fma2(B.p[j], NORM ? f.cB.p[j] : f.cA.p[j], fromA);
     }
     if (NORM) {
         scale_piece(yA, inv);
         scale_piece(yB, inv);
     }
-    if (span.turning) close_pairs<DTYPE, SIXTEEN>(one, two, yA, yB);
+    if (span.turning || (NORM && norm)) close_pairs<DTYPE, SIXTEEN>(one, two, yA, yB);
 }
 
-// Group tasks with eight pairs a lane.  The same products and sums as with eight
-// values a lane, those of a norm in the same order; with a norm there are no lanes
-// beyond the rotation.  Whole warps call it.
+// Group tasks with eight pairs a lane, with the same products and sums as with eight
+// values a lane.  Whole warps call it.
 template <int DTYPE, bool SIXTEEN, bool NORM>
 __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDeal& deal, unsigned item)
 {
@@ -609,7 +626,7 @@ __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDe
     const RotarySpan span = span_of<SIXTEEN>(tab, q);
     const bool inside = 16 * q < tab.head_dim;
     // beyond the rotation rows in place stay as they are
-    const int count = inside && (span.turning || task.in != task.out) ? task.count : 0;
+    const int count = inside && (span.turning || (NORM && task.weight) || task.in != task.out) ? task.count : 0;
     task.in += span.e0 * kBytes;
     task.out += span.e0 * kBytes;
     const int apart = (span.e1 - span.e0) * kBytes;
@@ -633,7 +650,7 @@ __device__ __forceinline__ void rotate_pairs(const RotaryArgs& a, const RotaryDe
             if (NORM && !mine)
 #pragma unroll
                 for (int i = 0; i < Eight<DTYPE>::kWords; ++i) one[b].w[i] = two[b].w[i] = 0;
-            turn_pairs<DTYPE, SIXTEEN, NORM>(tab, deal.log_lanes, task.weight != nullptr, span, f, one[b], two[b]);
+            turn_pairs<DTYPE, SIXTEEN, NORM>(tab, deal.log_lanes, q, task.weight != nullptr, span, f, one[b], two[b]);
             if (!mine) continue;
             store_eight(task.out + b * task.out_step, one[b]);
             store_eight(task.out + b * task.out_step + apart, two[b]);
@@ -654,15 +671,15 @@ __device__ __forceinline__ void rotate_piece(const RotaryArgs& a, const RotaryDe
         rotate_eights<DTYPE, PAIR, NORM>(a, deal, item);
 }
 
-// Deals out rows: as few heads share a group and its angles as fill the machine.
-// Returns the pieces.
-inline long long deal_rows(const RotaryArgs& a, int values, RotaryDeal* deal)
+// Deals out rows: as few heads share a group and its angles as give every SM
+// `threads` threads.  Returns the pieces.
+inline long long deal_rows(const RotaryArgs& a, int values, int threads, RotaryDeal* deal)
 {
     *deal = RotaryDeal{};
     while (values << deal->log_lanes < a.table.head_dim) ++deal->log_lanes;
     const long long rows = a.table.tokens * (a.rows[0].heads + a.rows[1].heads);
     int most = 1;
-    while (most < kMostHeads && rows / most > (152LL * 2048 >> deal->log_lanes)) most *= 2;
+    while (most < kMostHeads && rows / most > (152LL * threads >> deal->log_lanes)) most *= 2;
     for (int i = 0; i < 2; ++i) {
         const int heads = a.rows[i].heads, chunks = (heads + most - 1) / most;
         deal->chunks[i] = chunks;

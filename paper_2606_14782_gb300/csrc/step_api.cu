@@ -132,10 +132,8 @@ bacon_status rotary_args(const bacon_rotary* rotary, int requests, int tokens, c
              : a.table.interleaved           ? kPairOwn
              : a.table.rotary_dim % 16 == 0 ? kPairLane
                                              : kPairMemory;
-    // lanes with eight pairs: where sixteen values lie on one side of the rotation's
-    // end, and a norm has no lanes beyond it
-    const bool pairs = d % 16 == 0 && a.table.rotary_dim % 16 == 0 &&
-                       !(norm && a.table.rotary_dim < d);
+    // lanes with eight pairs: where sixteen values lie on one side of the rotation's end
+    const bool pairs = d % 16 == 0 && a.table.rotary_dim % 16 == 0;
     a.q_pair = a.pair == kPairMemory || !pairs ? a.pair : a.table.interleaved ? kPairSixteen : kPairHalves;
     *out = a;
     return BACON_OK;
@@ -330,8 +328,7 @@ bacon_status bacon_logits_process(bacon_logits* logits, const bacon_logits_rows*
     if (r.tokens && r.lengths &&
         (r.requests < 1 || r.capacity < 0 || r.capacity > BACON_MAX_HISTORY || r.token_stride < 0))
         return fail(BACON_EINVAL, "requests must be positive, capacity in [0, %d]", BACON_MAX_HISTORY);
-    if ((r.tokens == nullptr) != (r.lengths == nullptr))
-        return fail(BACON_EINVAL, "tokens and lengths come together");
+    if (r.tokens && !r.lengths) return fail(BACON_EINVAL, "tokens need lengths");
     if (r.biases && (!r.bias_tokens || !r.bias_values))
         return fail(BACON_EINVAL, "null list of biases");
     if (!r.logits) return fail(BACON_EINVAL, "null logits");

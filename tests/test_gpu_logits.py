@@ -180,6 +180,52 @@ def test_long_histories_and_the_largest_vocabulary():
     h.sync()
 
 
+def test_the_largest_vocabulary_in_many_rows():
+    """Eight blocks of a row: the most shared memory."""
+    V = 458752
+    x = draw(20, V, "fp16", 1)
+    tokens = torch.randint(0, V, (20, 50), generator=torch.Generator().manual_seed(2)).int()
+    want = [ref.rules(x[r].cpu(), tokens[r].tolist(), 25, 2.0, 0.25, 0.5) for r in range(20)]
+    h = bacon.Logits(V)
+    got = h.process(x, tokens=tokens.cuda(), lengths=ints([50] * 20), prompt=ints([25] * 20),
+                    repetition=floats([2.0] * 20), frequency=floats([0.25] * 20), presence=floats([0.5] * 20))
+    verify(*got, want)
+    h.sync()
+
+
+def test_a_prompt_of_one_token_many_times():
+    """An image's places: one number over and over, then a few words."""
+    V = 2000
+    x = draw(2, V, "fp32", 5)
+    history = [7] * 30000 + [8, 7, 9, 9]
+    tokens = ints([history, history])
+    h = bacon.Logits(V)
+    for start in (0, 1, 2, 3):  # lines that start anywhere
+        room = torch.zeros(2, len(history) + 5, dtype=torch.int32, device="cuda")
+        room[:, start:start + len(history)] = tokens
+        line = room[:, start:start + len(history)]
+        got = h.process(x, tokens=line, lengths=ints([30004, 17]), prompt=ints([30000, 17]), repetition=floats([1.5] * 2),
+                        frequency=floats([0.5] * 2), presence=floats([0.25] * 2))
+        want = [ref.rules(x[0].cpu(), history, 30000, 1.5, 0.5, 0.25), ref.rules(x[1].cpu(), [7] * 17, 17, 1.5, 0.5, 0.25)]
+        verify(*got, want)
+    h.sync()
+
+
+def test_no_history_and_no_list():
+    V = 300
+    x = draw(3, V, "bf16", 6)
+    h = bacon.Logits(V)
+    none = torch.empty(3, 0, dtype=torch.int32, device="cuda")
+    empty = h.process(x, tokens=none, lengths=ints([0, 0, 0]), bias_tokens=none, bias_values=none.float())
+    verify(*empty, [x[r].cpu().float() for r in range(3)])
+    some = h.process(x, tokens=ints([[1, 2]] * 3), lengths=ints([0, 0, 0]), repetition=floats([3.0] * 3))
+    verify(*some, [x[r].cpu().float() for r in range(3)])
+    out = torch.full((3, V), 4.0, device="cuda")
+    h.process(x, lengths=ints([0, -1, 0]), out=out)
+    assert bool((out[1] == 4).all()) and torch.equal(out[2], x[2].float())
+    h.sync()
+
+
 def test_many_rows():
     x, kw, want = everything(300, 777, "bf16", 5)
     h = bacon.Logits(777)

@@ -150,6 +150,22 @@ def test_rows_that_start_anywhere(d, D, interleaved):
     assert bool((room[~touched] == 9).all())
 
 
+@pytest.mark.parametrize("d,D,interleaved", [(64, 64, False), (128, 32, False), (128, 128, True), (64, 16, True),
+                                             (80, 48, False), (80, 40, True), (40, 16, False), (256, 96, False)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_a_rows_bits_do_not_depend_on_how_it_is_read(d, D, interleaved, norm):
+    """Rows one value off a multiple of 16 bytes are turned by other lanes."""
+    r = rotary(d, D, interleaved=interleaved)
+    x, p = draw((37, 3, d), "bf16", 1), places((37,), 2)
+    w = draw((d,), "bf16", 3) if norm else None
+    want = r.apply(x, None, p, q_weight=w)[0]
+    room = torch.empty(37 * 3 * d + 1, dtype=torch.bfloat16, device="cuda")
+    other = room[1:].view(37, 3, d)
+    other.copy_(x)
+    assert torch.equal(r.apply(other, None, p, q_weight=w)[0], want)
+    assert torch.equal(r.apply(x[20:21], None, p[20:21], q_weight=w)[0], want[20:21])  # alone as among others
+
+
 def test_what_does_not_turn_stays_bit_for_bit():
     for inter in (False, True):
         r = rotary(64, 32, interleaved=inter)
@@ -308,9 +324,8 @@ def test_rotated_store_is_the_two_calls(format, dtype, d, D, interleaved, page, 
     one.sync()
     two.sync()
     assert torch.equal(got, qr)
-    mine = (lengths > 0).sum() * 0  # every page that the tables name
     used = table[table >= 0].long()
-    assert used.numel() and int(mine) == 0
+    assert used.numel()
     for a, b in ((one.k_scale, two.k_scale), (one.v_scale, two.v_scale)):
         assert torch.equal(a[used], b[used])
     rows = slots[0].reshape(-1).long()

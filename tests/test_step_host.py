@@ -190,7 +190,7 @@ def handle(tmp_path_factory):
     (dict(out=0, best=0, logprob=0, lse=0), "wanted"), (dict(biases=-1), "biases"),
     (dict(biases=2048), "biases"), (dict(bias_values=0), "null"), (dict(requests=0), "requests"),
     (dict(capacity=1 << 20), "capacity"), (dict(capacity=-1), "capacity"), (dict(token_stride=-1), "capacity"),
-    (dict(lengths=0), "together"), (dict(tokens=0), "together"), (dict(logits=0), "null"),
+    (dict(lengths=0), "lengths"), (dict(logits=0), "null"),
     (dict(logits=A + 2), "aligned"), (dict(mask=A + 1), "aligned"), (dict(best=A + 2), "aligned"),
     (dict(row_stride=-1), "stride"), (dict(mask_stride=-1), "stride"), (dict(out_stride=99), "overlap"),
     (dict(row_stride=104), "in place"), (dict(dtype=0), "in place")])

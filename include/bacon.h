@@ -515,7 +515,7 @@ bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream);
  * axis_i,
  *   (x_a, x_b) -> A (x_a cos - x_b sin, x_b cos + x_a sin),
  * with (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) interleaved; values
- * from rotary_dim on stay.  Angles are exact to 2^-32 of a turn at every int32
+ * from rotary_dim on stay.  Angles are right to 2^-24 of a turn at every int32
  * position, negative ones too.  A row moves from position p to p' by a
  * turn of p' - p. */
 typedef struct bacon_rotary bacon_rotary;
@@ -633,7 +633,7 @@ bacon_status bacon_block_norm(const bacon_block* block, bacon_stream stream);
  * line request[row] of `tokens`, the first prompt[row] of them the prompt, the
  * others the answer; entries outside [0, vocab) count for nothing.  A token that
  * a list has twice has the last of its biases.  A row whose length is -1 is left
- * out: nothing of it is read or written. */
+ * out: its outputs stay as they are, and nothing of it is reported. */
 typedef struct bacon_logits bacon_logits;
 #define BACON_MAX_VOCAB 458752
 #define BACON_MAX_BIASES 2047

@@ -4,10 +4,10 @@
 // in registers between the statistics and their use.
 //
 // Here are rows of whole pieces of eight channels that start at multiples of 16
-// bytes (others: block_norm_ragged.cu).  A row belongs to a warp when it is narrow
-// and to a block otherwise, a thread has CHUNKS pieces of it as pairs of floats:
-// products and sums are the two-float instructions, since what is left of the bound
-// after the bytes is issuing instructions.  Blocks stay and go from row to row, and
+// bytes (others: block_norm_ragged.cu).  A row belongs to some or all lanes of a warp
+// when it is narrow and to a block otherwise, a thread has CHUNKS pieces of it as
+// pairs of floats: products and sums are the two-float instructions, since what is
+// left of the bound after the bytes is issuing instructions.  Blocks stay and go from row to row, and
 // the next row is on its way while one is worked on.
 #include "block_norm.cuh"
 
@@ -103,10 +103,13 @@ __device__ __forceinline__ void normalise(const bacon_block& b, float per_channe
         const float2 f = floats_of(s);
         const float squares = sum(f.x + f.y);
         inverse = rsqrtf(fmaf(squares, per_channel, eps));
-        if (squares < INFINITY || pass) break;
-        // once more with the row far smaller; eps is nothing beside its squares
-        eps = 0.0f;
-        const Pair small = pair_of(0x1p-100f, 0x1p-100f);
+        // once more with the row far smaller; eps is nothing beside its squares.  The
+        // rows of a warp go together, and the others find again what they had
+        const bool again = !(squares < INFINITY) && !pass;
+        if (TIGHT ? !again : !__any_sync(0xFFFFFFFFu, again)) break;
+        if (again) eps = 0.0f;
+        const float by = again ? 0x1p-100f : 1.0f;
+        const Pair small = pair_of(by, by);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
@@ -131,22 +134,25 @@ constexpr int most_threads(int chunks, bool warp) { return warp ? 128 : chunks =
 
 template <int DTYPE, int RESIDUAL, int CHUNKS, bool WARP>
 __global__ void __launch_bounds__(most_threads(CHUNKS, WARP))
-block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
+block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel, int lanes)
 {
     __shared__ __align__(16) float s_scratch[64];
     if (!WARP) {
         if (threadIdx.x < 64) s_scratch[threadIdx.x] = 0.0f;
         __syncthreads();
     }
-    RowSum<WARP> sum{s_scratch};
+    RowSum<WARP> sum{s_scratch, lanes};
     constexpr int kBytes = Eight<DTYPE>::kBytes, kWide = Eight<RESIDUAL>::kBytes;
     Pieces<CHUNKS, !WARP> p;
     p.width = b.width;
-    p.first = WARP ? threadIdx.x & 31 : threadIdx.x;
-    p.step = WARP ? 32 : blockDim.x;
-    const int rows = WARP ? blockDim.x / 32 : 1;
+    p.first = WARP ? threadIdx.x & (lanes - 1) : threadIdx.x;
+    p.step = WARP ? lanes : blockDim.x;
+    const int rows = WARP ? blockDim.x / lanes : 1;
     const long long apart = (long long)gridDim.x * rows;
-    long long t = (long long)blockIdx.x * rows + (WARP ? threadIdx.x >> 5 : 0);
+    long long t = (long long)blockIdx.x * rows + (WARP ? threadIdx.x / lanes : 0);
+    // the first row of the warp: all of its rows go round together, those that are
+    // not there as rows of no channels
+    long long first = WARP ? t - (threadIdx.x & 31) / lanes : t;
 
     // a row ahead, where rows leave registers for it
     constexpr bool kAhead = CHUNKS <= 4;
@@ -155,6 +161,7 @@ block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
     auto fetch = [&](long long row) {
         const char* const y = static_cast<const char*>(b.y) + row * b.y_token * kBytes;
         const char* const x = static_cast<const char*>(b.x) + row * b.x_token * kWide;
+        p.width = !WARP || row < b.tokens ? b.width : 0;
 #pragma unroll
         for (int i = 0; i < (kAhead ? CHUNKS : 1); ++i)
             if (p.some(i)) {
@@ -170,9 +177,9 @@ block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
 #pragma unroll
             for (int j = 0; j < Eight<RESIDUAL>::kWords; ++j) x_next[i].w[j] = 0;
         }
-        if (t < b.tokens) fetch(t);
+        if (first < b.tokens) fetch(t);
     }
-    for (; t < b.tokens; t += apart) {
+    for (; first < b.tokens; t += apart, first += apart) {
         Piece v[CHUNKS], x[CHUNKS];
         const char* const y = static_cast<const char*>(b.y) + t * b.y_token * kBytes;
         const char* const x_row = static_cast<const char*>(b.x) + t * b.x_token * kWide;
@@ -182,7 +189,8 @@ block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
                 open_piece(y_next[i], v[i]);
                 open_piece(x_next[i], x[i]);
             }
-            if (t + apart < b.tokens) fetch(t + apart);
+            if (first + apart < b.tokens) fetch(t + apart);
+            p.width = !WARP || t < b.tokens ? b.width : 0;
         } else {
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i) {
@@ -195,7 +203,7 @@ block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
             normalise<DTYPE>(b, per_channel, Norm{b.post, b.post_weight, b.post_bias}, p, sum, v);
         const char* const gate = static_cast<const char*>(b.gate) + t * b.gate_token * kBytes;
         if (b.gate && !b.gate_channel) {
-            const float g = load_one<DTYPE>(gate, 0);
+            const float g = p.width ? load_one<DTYPE>(gate, 0) : 0.0f;
             const float a = b.activation == BACON_GATE_LINEAR ? g : activate(g, b.activation);
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i)
@@ -247,13 +255,15 @@ block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
 template <int DTYPE, int RESIDUAL, int CHUNKS, bool WARP>
 cudaError_t launch_rows(const bacon_block& b, int pieces, cudaStream_t st)
 {
+    int lanes = 32;  // of a narrow row: several rows a warp
+    while (WARP && CHUNKS == 1 && lanes / 2 >= pieces) lanes /= 2;
     const int threads = WARP ? 128 : ((pieces + CHUNKS - 1) / CHUNKS + 31) / 32 * 32;
-    const long long rows = WARP ? 4 : 1, wanted = (b.tokens + rows - 1) / rows;
+    const long long rows = WARP ? 128 / lanes : 1, wanted = (b.tokens + rows - 1) / rows;
     // as many blocks as the registers leave room for, or half as many rows
     const long long most = 152LL * (CHUNKS == 1 ? 1024 : WARP ? 384 : 512) / threads;
     const long long blocks = wanted < most || CHUNKS > 4 ? wanted : most;
     return launch_first(block_norm_kernel<DTYPE, RESIDUAL, CHUNKS, WARP>, (unsigned)blocks, threads, 0, st, b,
-                        1.0f / (float)b.width);
+                        1.0f / (float)b.width, lanes);
 }
 
 template <int DTYPE, int RESIDUAL>

@@ -12,11 +12,11 @@ namespace {
 template <bool WARP>
 struct RowSum {
     float* scratch;  // [2][32], zeros beyond the block's warps
+    int lanes;       // of a row that has a warp's, a power of two
     int turn = 0;
     __device__ __forceinline__ float operator()(float v)
     {
-#pragma unroll
-        for (int off = 16; off; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+        for (int off = (WARP ? lanes : 32) / 2; off; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
         if (WARP) return v;
         // two buffers in turn: who writes one again has been past the barrier
         // of the other, which everyone has left the first behind for
@@ -50,7 +50,6 @@ struct Norm {
     const void* weight;
     const void* bias;
 };
-
 
 }  // namespace
 }  // namespace bacon

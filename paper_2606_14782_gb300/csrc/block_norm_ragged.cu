@@ -63,7 +63,7 @@ ragged_norm_kernel(const __grid_constant__ bacon_block b, float per_channel)
         if (threadIdx.x < 64) s_scratch[threadIdx.x] = 0.0f;
         __syncthreads();
     }
-    RowSum<WARP> sum{s_scratch};
+    RowSum<WARP> sum{s_scratch, 32};
     const long long t = WARP ? blockIdx.x * 4LL + (threadIdx.x >> 5) : blockIdx.x;
     if (WARP && t >= b.tokens) return;
     constexpr int kBytes = Eight<DTYPE>::kBytes, kWide = Eight<RESIDUAL>::kBytes;

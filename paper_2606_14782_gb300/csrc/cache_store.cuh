@@ -8,7 +8,6 @@
 #include "common.cuh"
 #include "rotary.cuh"
 
-
 namespace bacon {
 namespace {
 

@@ -167,6 +167,33 @@ def test_extreme_rows(width, pre):
     assert bool((total == 0).all())  # silu at minus infinity
 
 
+@pytest.mark.parametrize("width", [8, 16, 24, 40, 64, 128, 200])
+@pytest.mark.parametrize("pre", ["rms", "layer"])
+def test_extreme_rows_beside_others(width, pre):
+    """Rows that share a warp: one that is gone through again, one of NaN, one of
+    infinities, and those beside them as if they were alone."""
+    for T in (1, 3, 13, 1000):
+        y = draw((T, width), "bf16", T)
+        x, g = draw((T, width), "fp32", 2), draw((T, 1), "bf16", 3)
+        for r, v in ((1, 3e38), (4, float("nan")), (6, float("inf"))):
+            if r < T:
+                y[r] = v
+                y[r, 0] = -1
+        layer = bacon.BlockNorm(width, pre=pre)
+        _, n = layer(y)
+        total, m = layer(y, x, g)
+        for r in (0, 2, 5, 7, T - 1):
+            if r < T and r not in (1, 4, 6):
+                assert torch.equal(layer(y[r:r + 1])[1], n[r:r + 1])
+                assert all(torch.equal(a, b[r:r + 1]) for a, b in
+                           zip(layer(y[r:r + 1], x[r:r + 1], g[r:r + 1]), (total, m)))
+        if T > 6:
+            want = ref.normed(y[1].double(), pre, None, None, 1e-6, 0.0)
+            # 3e38 in all but one place: the mean is off by 2^-18 of it, the root by 2^-18
+            assert bool(((n[1].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -12).all())
+            assert bool(n[4].isnan().all()) and bool(n[6].isnan().any())
+
+
 def test_large_means():
     """Values of 1000 +- 1: the mean is taken off before squares are summed."""
     for width in (512, 8192):

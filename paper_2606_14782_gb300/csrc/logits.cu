@@ -3,14 +3,20 @@
 // if wanted, written once.
 //
 // A row belongs to a cluster of blocks, which have groups of 256 neighbouring tokens
-// in turn, so that the many uses of a few low numbers are spread.  A block goes through the row's whole history and counts its own tokens by
-// atomics on a word a token in its shared memory: the number of times in the
-// answer, whether the prompt has it, and the last place of the row's bias list that
-// names it.  Whole numbers only, so that no order changes a result.  (Each entry
-// read by one block and counted in the block that has its token, by atomics on
-// distributed shared memory, took 42 us for 100000 entries on 16 blocks: about
-// eight cycles an entry.)  The pass over the logits then looks at these words, and
-// the maxima and sums of the parts meet in the first block.
+// in turn, so that the many uses of a few low numbers are spread.  A block goes
+// through the row's whole history and counts its own tokens by atomics on a word a
+// token in its shared memory: the number of times in the answer, whether the prompt
+// has it, and the last place of the row's bias list that names it.  Whole numbers
+// only, so that no order changes a result.  (Each entry read by one block and counted
+// in the block that has its token, by atomics on distributed shared memory, took
+// about eight cycles an entry.)  Of long prompts, where one bit a token is enough,
+// the blocks read a part each and exchange the bits: 4 rows with histories of 100000
+// tokens 18.5 us, 31 without.  The pass over the logits then looks at these words, and
+// the maxima and sums of the parts meet in the first block.  256 rows of 131072 fp32
+// logits with all rules 95 us, 43 % of the measured copy bandwidth; without history
+// and mask 53 us: counting and the rules take as many instructions as the pass, and
+// a block's steps wait for one another.  One row of 32000: 5.7 us, a chain of its
+// parameters, its history, its logits and the cluster's meeting.
 #include "logits.h"
 
 #include "common.cuh"
@@ -21,6 +27,8 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kGroup = 256;              // tokens that a warp takes together
+constexpr int kSplit = 16384;           // tokens of a prompt that a row's blocks share
+constexpr int kMostOfThree = 70;         // groups of a block of which three fit an SM's shared memory
 constexpr float kLeast = 1e-30f;         // repetition and temperature
 constexpr uint32_t kCount = 0xFFFFFu;    // of a token's word: times in the answer
 constexpr uint32_t kSeen = 1u << 20;     // in the prompt
@@ -73,6 +81,13 @@ __device__ __forceinline__ void or_where(uint32_t address, uint32_t bits, bool o
     asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p red.shared.or.b32 [%0], %1;\n}\n" ::"r"(address),
                  "r"(bits), "r"((uint32_t)on)
                  : "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_load(uint32_t address)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(address) : "memory");
+    return v;
 }
 
 struct Rules {
@@ -131,9 +146,6 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
     const float temperature = a.temperature ? a.temperature[row] : 1.0f;
     const int32_t* const bias_tokens = a.bias_tokens ? a.bias_tokens + (long long)row * a.biases : nullptr;
     const int first_bias = bias_tokens && tid < a.biases ? bias_tokens[tid] : -1;
-    if (words)
-        for (int i = tid; i < groups * kGroup / 4; i += kThreads)
-            reinterpret_cast<uint4*>(s_word)[i] = make_uint4(0, 0, 0, 0);
     if (a.lengths && length_in == -1) return;  // all blocks of the row
     Rules rules;
     rules.repetition = checked(repetition, 1.0f, true, err);
@@ -147,6 +159,8 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
     const bool greedy = a.best || a.logprob || a.lse;
     // the row's blocks have all begun before one writes into another
     if (greedy) cluster_arrive();
+    uint32_t* const s_seen = s_word + (((vocab + kGroup - 1) / kGroup + blocks - 1) >> log_blocks) * kGroup;
+    bool split = false;  // what the prompt has is in s_seen, a bit a token
     if (words) {
         int length = a.tokens && a.lengths ? length_in : 0;
         if (length && (length < 0 || length > a.capacity || prompt_in < 0 || prompt_in > length || line < 0 ||
@@ -156,47 +170,80 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
         }
         const int prompt = length ? prompt_in : 0;
         const int32_t* const history = a.tokens + (length ? line * a.token_stride : 0);
-        // four entries a load, from the last multiple of 16 bytes before the line
-        const int lead = (int)(reinterpret_cast<uintptr_t>(history) >> 2) & 3;
-        const int loads = (length + lead + 3) / 4;
         const uint32_t words_at = smem_u32(s_word);
         constexpr int kFlight = 4;  // loads of a thread that are on their way together
         int4 token[kFlight];
-        const auto fetch = [&](int g0) {
+        // entries from .. to of the history: four a load, from the last multiple of 16
+        // bytes before them; use(entry's number, token, whether the one before is the same)
+        const auto entries = [&](int from, int to, const auto& meanwhile, const auto& use) {
+            const int lead = (int)(reinterpret_cast<uintptr_t>(history + from) >> 2) & 3;
+            const int loads = (to - from + lead + 3) / 4;
+            const auto fetch = [&](int g0) {
 #pragma unroll
-            for (int k = 0; k < kFlight; ++k) {
-                const int g = g0 + k * kThreads, i = 4 * g - lead;
-                token[k] = make_int4(-1, -1, -1, -1);
-                if (g >= loads) continue;
-                if (i >= 0 && i + 4 <= length) {
-                    token[k] = *reinterpret_cast<const int4*>(history + i);
-                } else {
-                    if (i >= 0) token[k].x = history[i];
-                    if (i + 1 >= 0 && i + 1 < length) token[k].y = history[i + 1];
-                    if (i + 2 >= 0 && i + 2 < length) token[k].z = history[i + 2];
-                    if (i + 3 < length) token[k].w = history[i + 3];
+                for (int k = 0; k < kFlight; ++k) {
+                    const int g = g0 + k * kThreads, i = from + 4 * g - lead;
+                    token[k] = make_int4(-1, -1, -1, -1);
+                    if (g >= loads) continue;
+                    if (i >= from && i + 4 <= to) {
+                        token[k] = *reinterpret_cast<const int4*>(history + i);
+                    } else {
+                        if (i >= from) token[k].x = history[i];
+                        if (i + 1 >= from && i + 1 < to) token[k].y = history[i + 1];
+                        if (i + 2 >= from && i + 2 < to) token[k].z = history[i + 2];
+                        if (i + 3 < to) token[k].w = history[i + 3];
+                    }
+                }
+            };
+            if (tid < loads) fetch(tid);
+            meanwhile();
+            for (int g0 = tid; g0 < loads; g0 += kFlight * kThreads) {
+                if (g0 != tid) fetch(g0);
+#pragma unroll
+                for (int k = 0; k < kFlight; ++k) {
+                    const int i = from + 4 * (g0 + k * kThreads) - lead;
+                    use(i, token[k].x, false);
+                    use(i + 1, token[k].y, token[k].y == token[k].x);
+                    use(i + 2, token[k].z, token[k].z == token[k].y);
+                    use(i + 3, token[k].w, token[k].w == token[k].z);
                 }
             }
         };
-        fetch(tid);
-        __syncthreads();  // the words are 0
-        for (int g0 = tid; g0 < loads; g0 += kFlight * kThreads) {
-            if (g0 != tid) fetch(g0);
-#pragma unroll
-            for (int k = 0; k < kFlight; ++k) {
-                const int i = 4 * (g0 + k * kThreads) - lead;
-                const int entry[4] = {token[k].x, token[k].y, token[k].z, token[k].w};
-#pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                    const bool own = mine(entry[z]), said = i + z >= prompt;
-                    const uint32_t at = word_of(entry[z]);
-                    // a prompt may have one token many times on end
-                    const bool anew = own && (z == 0 || entry[z] != entry[z ? z - 1 : 0]);
-                    add_where(words_at + 4 * at, own && said);
-                    or_where(words_at + 4 * at, kSeen, anew && !said);
-                }
+        const auto clear = [&](int count) {
+            for (int i = tid; i < (count + 3) / 4; i += kThreads)
+                reinterpret_cast<uint4*>(s_word)[i] = make_uint4(0, 0, 0, 0);
+            __syncthreads();
+        };
+        split = prompt >= kSplit && blocks > 1;
+        if (split) {
+            // whether the prompt has a token is one bit: each block goes through a part
+            // of a long prompt into a map of the whole vocabulary, and then takes its own
+            // tokens' words from everybody's
+            const int part = (prompt + blocks - 1) >> log_blocks, from = min(prompt, rank * part);
+            entries(from, min(prompt, from + part), [&] { clear((vocab + kGroup - 1) / kGroup * (kGroup / 32)); },
+                    [&](int, int t, bool same) {
+                        or_where(words_at + ((uint32_t)t / 32) * 4, 1u << (t & 31),
+                                 (uint32_t)t < (uint32_t)vocab && !same);
+                    });
+            if (greedy) cluster_wait();
+            cluster_arrive();
+            cluster_wait();
+            for (int i = tid; i < groups * (kGroup / 32); i += kThreads) {
+                const uint32_t at = words_at + (((i >> 3) << log_blocks) + rank) * kGroup / 8 + (i & 7) * 4;
+                uint32_t bits = 0;
+                for (int r = 0; r < blocks; ++r) bits |= cluster_load(cluster_address(at, r));
+                s_seen[i] = bits;
             }
+            cluster_arrive();
+            cluster_wait();
         }
+        entries(split ? prompt : 0, length, [&] { clear(groups * kGroup); },
+                [&](int i, int t, bool same) {
+                    const bool own = mine(t), said = i >= prompt;
+                    const uint32_t to = words_at + 4 * word_of(t);
+                    add_where(to, own && said);
+                    // a prompt may have one token many times on end
+                    or_where(to, kSeen, own && !said && !same);
+                });
         __syncthreads();
         // the other fields of a word are settled: the largest word has the last place
         if (bias_tokens) {
@@ -255,6 +302,15 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
             read();
 #pragma unroll
             for (int j = 0; j < 8; ++j) some |= (w[j] != 0) << j;
+            uint32_t seen = 0;
+            if (split) {
+                if (kStep == 8)
+                    seen = reinterpret_cast<const uint8_t*>(s_seen)[k * (kGroup / 8) + lane];
+                else
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) seen |= (s_seen[k * 8 + j] >> lane & 1) << j;
+                some |= seen;
+            }
             if (some) {
                 // few of the eight, so each in its turn: its word becomes the logit that
                 // the rules make of it (eight at once: 103 us for 94 of the largest case)
@@ -263,7 +319,7 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
                 for (uint32_t left = some; left; left &= left - 1) {
                     const int j = __ffs(left) - 1;
                     const float raw = load_one<DTYPE>(in, v0 + j * kGap);
-                    words_here[j * kGap] = __float_as_uint(ruled(raw, words_here[j * kGap], rules));
+                    words_here[j * kGap] = __float_as_uint(ruled(raw, words_here[j * kGap] | (seen >> j & 1 ? kSeen : 0), rules));
                 }
                 read();
 #pragma unroll
@@ -335,7 +391,7 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
     }
     if (!greedy) return;
 
-    cluster_wait();
+    if (!split) cluster_wait();
     p = join_warp(p, rate);
     if (lane == 0) s_part[tid >> 5] = p;
     __syncthreads();
@@ -371,7 +427,7 @@ cudaError_t start(const bacon_logits_rows& r, int vocab, int blocks, int* err, c
     int log_blocks = 0;
     while (1 << log_blocks < blocks) ++log_blocks;
     const int groups = ((vocab + kGroup - 1) / kGroup + blocks - 1) / blocks;  // of a block, at most
-    const size_t smem = words ? (size_t)groups * kGroup * 4 : 0;
+    const size_t smem = words ? (size_t)groups * (kGroup + kGroup / 32) * 4 : 0;
     auto* const kernel = logits_kernel<DTYPE, OUT, kStep, kResident>;
     if (smem > 32 * 1024) {
         const cudaError_t e =
@@ -405,8 +461,12 @@ cudaError_t go(const bacon_logits_rows& r, int vocab, int* err, cudaStream_t st)
     while (blocks > 1 && vocab <= blocks / 2 * kThreads * 8 && vocab <= BACON_MAX_VOCAB / 16 &&
            r.capacity <= blocks * kThreads)
         blocks /= 2;
-    return (long long)r.rows * blocks > 152 * 2 ? start<DTYPE, OUT, kStep, 3>(r, vocab, blocks, err, st)
-                                                : start<DTYPE, OUT, kStep, 2>(r, vocab, blocks, err, st);
+    // so many words that three blocks would not fit an SM (34 rows of 255141 logits:
+    // 47 us with eight, 30 with sixteen)
+    if (vocab > kGroup * kMostOfThree * blocks) blocks = 16;
+    const bool three = (long long)r.rows * blocks > 152 * 2 && vocab <= kGroup * kMostOfThree * blocks;
+    return three ? start<DTYPE, OUT, kStep, 3>(r, vocab, blocks, err, st)
+                 : start<DTYPE, OUT, kStep, 2>(r, vocab, blocks, err, st);
 }
 
 template <int DTYPE, int OUT>

@@ -211,6 +211,31 @@ def test_a_prompt_of_one_token_many_times():
     h.sync()
 
 
+@pytest.mark.parametrize("V", [33, 777, 4096, 50021, 131072])
+@pytest.mark.parametrize("rows", [1, 3, 25])
+def test_prompts_that_a_rows_blocks_share(V, rows):
+    """Long prompts beside short ones, and rows left out, in one call."""
+    gen = torch.Generator().manual_seed(V)
+    tokens = (V * torch.rand(rows, 40001, generator=gen) ** 4).int()
+    tokens[:, 5000:9000] = V + 7
+    x = draw(rows, V, "bf16", 2)
+    prompt = [20000 if r % 3 == 0 else 50 if r % 3 == 1 else 16383 + r % 2 for r in range(rows)]
+    lengths = [p + 300 + r for r, p in enumerate(prompt)]
+    want = [ref.rules(x[r].cpu(), tokens[r, :n].tolist(), p, 1.25, 0.01, 0.3) for r, (n, p) in enumerate(zip(lengths, prompt))]
+    kw = dict(tokens=tokens.cuda(), prompt=ints(prompt), repetition=floats([1.25] * rows),
+              frequency=floats([0.01] * rows), presence=floats([0.3] * rows))
+    h = bacon.Logits(V)
+    verify(*h.process(x, lengths=ints(lengths), **kw), want)
+    out, best, _, _ = h.process(x, lengths=ints(lengths), greedy=False, **kw)
+    verify(out, None, None, None, want)
+    lengths[0] = -1
+    out = torch.full((rows, V), 6.0, device="cuda")
+    got = h.process(x, lengths=ints(lengths), out=out, **kw)
+    assert bool((out[0] == 6).all())
+    verify(*got, want, rows=range(1, rows))
+    h.sync()
+
+
 def test_no_history_and_no_list():
     V = 300
     x = draw(3, V, "bf16", 6)

@@ -11,9 +11,9 @@
 // in the block that has its token, by atomics on distributed shared memory, took
 // about eight cycles an entry.)  Of long prompts, where one bit a token is enough,
 // the blocks read a part each and exchange the bits: 4 rows with histories of 100000
-// tokens 18.5 us, 31 without.  The pass over the logits then looks at these words, and
+// tokens 17 us, 31 without.  The pass over the logits then looks at these words, and
 // the maxima and sums of the parts meet in the first block.  256 rows of 131072 fp32
-// logits with all rules 95 us, 43 % of the measured copy bandwidth; without history
+// logits with all rules 92 us, 45 % of the measured copy bandwidth; without history
 // and mask 53 us: counting and the rules take as many instructions as the pass, and
 // a block's steps wait for one another.  One row of 32000: 5.7 us, a chain of its
 // parameters, its history, its logits and the cluster's meeting.
@@ -69,18 +69,44 @@ __device__ __forceinline__ Part join_warp(const Part& p, float rate)
     return all;
 }
 
-// Counts in shared memory where `on`, without a branch.
-__device__ __forceinline__ void add_where(uint32_t address, bool on)
+// Whose a token is and where its word lies: the groups of kGroup tokens go to the
+// blocks in turn.
+struct Owner {
+    uint32_t vocab, rank, others, words;  // others: blocks - 1; words: the shared address
+    int log_blocks;
+    __device__ __forceinline__ uint32_t apart(uint32_t t) const { return (t ^ rank * kGroup) & others * kGroup; }
+    __device__ __forceinline__ bool has(uint32_t t) const { return t < vocab && apart(t) == 0; }
+    __device__ __forceinline__ uint32_t place(uint32_t t) const
+    {
+        return (t >> log_blocks & ~(kGroup - 1u)) | (t & (kGroup - 1u));
+    }
+    // without a branch: in nearly every entry some lane has a token of the block
+    __device__ __forceinline__ void said(uint32_t t) const
+    {
+        asm volatile(
+            "{\n.reg .pred p;\nsetp.lt.u32 p, %1, %2;\nsetp.eq.and.u32 p, %3, 0, p;\n"
+            "@p red.shared.add.u32 [%0], 1;\n}\n" ::"r"(words + 4 * place(t)),
+            "r"(t), "r"(vocab), "r"(apart(t))
+            : "memory");
+    }
+    // (a prompt may have one token many times on end)
+    __device__ __forceinline__ void asked(uint32_t t, uint32_t before) const
+    {
+        asm volatile(
+            "{\n.reg .pred p;\nsetp.lt.u32 p, %1, %2;\nsetp.eq.and.u32 p, %3, 0, p;\n"
+            "setp.ne.and.u32 p, %1, %4, p;\n@p red.shared.or.b32 [%0], %5;\n}\n" ::"r"(words + 4 * place(t)),
+            "r"(t), "r"(vocab), "r"(apart(t)), "r"(before), "r"(kSeen)
+            : "memory");
+    }
+};
+// A bit of a map of the whole vocabulary.
+__device__ __forceinline__ void mark(uint32_t map, uint32_t t, uint32_t before, uint32_t vocab)
 {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %1, 0;\n@p red.shared.add.u32 [%0], 1;\n}\n" ::"r"(address),
-                 "r"((uint32_t)on)
-                 : "memory");
-}
-__device__ __forceinline__ void or_where(uint32_t address, uint32_t bits, bool on)
-{
-    asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\n@p red.shared.or.b32 [%0], %1;\n}\n" ::"r"(address),
-                 "r"(bits), "r"((uint32_t)on)
-                 : "memory");
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.lt.u32 p, %1, %2;\nsetp.ne.and.u32 p, %1, %3, p;\n"
+        "@p red.shared.or.b32 [%0], %4;\n}\n" ::"r"(map + t / 32 * 4),
+        "r"(t), "r"(vocab), "r"(before), "r"(1u << (t & 31))
+        : "memory");
 }
 
 __device__ __forceinline__ uint32_t cluster_load(uint32_t address)
@@ -129,14 +155,7 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
     const int tid = threadIdx.x, lane = tid & 31;
     // the block's k-th group is the row's number k blocks + rank
     const int groups = ((vocab + kGroup - 1) / kGroup - rank + blocks - 1) >> log_blocks;
-    const auto mine = [&](int token) {
-        const uint32_t t = token;
-        return t < (uint32_t)vocab && ((t / kGroup ^ rank) & (blocks - 1)) == 0;
-    };
-    const auto word_of = [&](int token) {
-        const uint32_t t = token;
-        return (t / kGroup >> log_blocks) * kGroup + t % kGroup;
-    };
+    const Owner owner{(uint32_t)vocab, (uint32_t)rank, blocks - 1u, smem_u32(s_word), log_blocks};
     // all that the row's parameters say, on its way together
     const int length_in = a.lengths ? a.lengths[row] : 0;
     const int prompt_in = a.prompt ? a.prompt[row] : 0, line = a.request ? a.request[row] : row;
@@ -170,11 +189,10 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
         }
         const int prompt = length ? prompt_in : 0;
         const int32_t* const history = a.tokens + (length ? line * a.token_stride : 0);
-        const uint32_t words_at = smem_u32(s_word);
         constexpr int kFlight = 4;  // loads of a thread that are on their way together
         int4 token[kFlight];
         // entries from .. to of the history: four a load, from the last multiple of 16
-        // bytes before them; use(entry's number, token, whether the one before is the same)
+        // bytes before them; use(the first one's number, the four)
         const auto entries = [&](int from, int to, const auto& meanwhile, const auto& use) {
             const int lead = (int)(reinterpret_cast<uintptr_t>(history + from) >> 2) & 3;
             const int loads = (to - from + lead + 3) / 4;
@@ -200,11 +218,7 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
                 if (g0 != tid) fetch(g0);
 #pragma unroll
                 for (int k = 0; k < kFlight; ++k) {
-                    const int i = from + 4 * (g0 + k * kThreads) - lead;
-                    use(i, token[k].x, false);
-                    use(i + 1, token[k].y, token[k].y == token[k].x);
-                    use(i + 2, token[k].z, token[k].z == token[k].y);
-                    use(i + 3, token[k].w, token[k].w == token[k].z);
+                    use(from + 4 * (g0 + k * kThreads) - lead, token[k]);
                 }
             }
         };
@@ -220,15 +234,17 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
             // tokens' words from everybody's
             const int part = (prompt + blocks - 1) >> log_blocks, from = min(prompt, rank * part);
             entries(from, min(prompt, from + part), [&] { clear((vocab + kGroup - 1) / kGroup * (kGroup / 32)); },
-                    [&](int, int t, bool same) {
-                        or_where(words_at + ((uint32_t)t / 32) * 4, 1u << (t & 31),
-                                 (uint32_t)t < (uint32_t)vocab && !same);
+                    [&](int, const int4& t) {
+                        mark(owner.words, t.x, ~t.x, vocab);
+                        mark(owner.words, t.y, t.x, vocab);
+                        mark(owner.words, t.z, t.y, vocab);
+                        mark(owner.words, t.w, t.z, vocab);
                     });
             if (greedy) cluster_wait();
             cluster_arrive();
             cluster_wait();
             for (int i = tid; i < groups * (kGroup / 32); i += kThreads) {
-                const uint32_t at = words_at + (((i >> 3) << log_blocks) + rank) * kGroup / 8 + (i & 7) * 4;
+                const uint32_t at = owner.words + (((i >> 3) << log_blocks) + rank) * kGroup / 8 + (i & 7) * 4;
                 uint32_t bits = 0;
                 for (int r = 0; r < blocks; ++r) bits |= cluster_load(cluster_address(at, r));
                 s_seen[i] = bits;
@@ -237,20 +253,31 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
             cluster_wait();
         }
         entries(split ? prompt : 0, length, [&] { clear(groups * kGroup); },
-                [&](int i, int t, bool same) {
-                    const bool own = mine(t), said = i >= prompt;
-                    const uint32_t to = words_at + 4 * word_of(t);
-                    add_where(to, own && said);
-                    // a prompt may have one token many times on end
-                    or_where(to, kSeen, own && !said && !same);
+                [&](int i, const int4& t) {
+                    if (i >= prompt) {
+                        owner.said(t.x);
+                        owner.said(t.y);
+                        owner.said(t.z);
+                        owner.said(t.w);
+                    } else if (i + 4 <= prompt) {
+                        owner.asked(t.x, ~t.x);
+                        owner.asked(t.y, t.x);
+                        owner.asked(t.z, t.y);
+                        owner.asked(t.w, t.z);
+                    } else {
+                        owner.asked(t.x, ~t.x);
+                        i + 1 < prompt ? owner.asked(t.y, ~t.y) : owner.said(t.y);
+                        i + 2 < prompt ? owner.asked(t.z, ~t.z) : owner.said(t.z);
+                        owner.said(t.w);
+                    }
                 });
         __syncthreads();
         // the other fields of a word are settled: the largest word has the last place
         if (bias_tokens) {
             for (int i = tid; i < a.biases; i += kThreads) {
                 const int token = i == tid ? first_bias : bias_tokens[i];
-                if (mine(token)) {
-                    const uint32_t at = word_of(token);
+                if (owner.has(token)) {
+                    const uint32_t at = owner.place(token);
                     uint32_t* const w = &s_word[at];
                     const uint32_t fields = *(volatile uint32_t*)w & (kCount | kSeen);
                     atomicMax(w, (uint32_t)(i + 1) << kBiasShift | fields);

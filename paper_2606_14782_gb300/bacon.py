@@ -744,9 +744,11 @@ class Cache:
                 raise ValueError("q must be [tokens, heads, d], of k's tokens")
             if q_out is None:
                 q_out = _empty(q.shape, self.dtype, self.device, stream)
+                op = q_out.data_ptr(), q.shape[1] * self.head_dim, self.head_dim
             elif q_out.shape != q.shape:
                 raise ValueError("q_out must have q's shape")
-            op = self._rows(q_out, "q_out")
+            else:
+                op = self._rows(q_out, "q_out")
             rows = _pack_rows(qp[0], op[0], _ptr(q_weight) or 0, q.shape[1], 0, qp[1], qp[2], 0,
                               op[1], op[2])
         _check(self._lib.bacon_cache_store_rotated(

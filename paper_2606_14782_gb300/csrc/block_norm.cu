@@ -133,10 +133,10 @@ __device__ __forceinline__ void normalise(const bacon_block& b, float per_channe
         weigh<DTYPE>(b, n, p, v);
 }
 
-constexpr int most_threads(int chunks, bool warp) { return warp ? 128 : chunks == 1 ? 1024 : 512; }
+constexpr int most_threads(bool warp) { return warp ? 128 : 512; }
 
 template <int DTYPE, int RESIDUAL, int CHUNKS, bool WARP>
-__global__ void __launch_bounds__(most_threads(CHUNKS, WARP))
+__global__ void __launch_bounds__(most_threads(WARP))
 block_norm_kernel(const __grid_constant__ bacon_block b, float per_channel, int lanes)
 {
     __shared__ __align__(16) float s_scratch[64];
@@ -263,7 +263,7 @@ cudaError_t launch_rows(const bacon_block& b, int pieces, cudaStream_t st)
     const int threads = WARP ? 128 : ((pieces + CHUNKS - 1) / CHUNKS + 31) / 32 * 32;
     const long long rows = WARP ? 128 / lanes : 1, wanted = (b.tokens + rows - 1) / rows;
     // as many blocks as the registers leave room for, if there are as many rows
-    const long long most = 152LL * (CHUNKS == 1 ? 1024 : WARP ? 384 : 512) / threads;
+    const long long most = 152LL * (!WARP ? 512 : CHUNKS == 1 ? 1024 : 384) / threads;
     const long long blocks = wanted < most || CHUNKS > 4 ? wanted : most;
     return launch_first(block_norm_kernel<DTYPE, RESIDUAL, CHUNKS, WARP>, (unsigned)blocks, threads, 0, st, b,
                         1.0f / (float)b.width, lanes);
@@ -275,11 +275,11 @@ cudaError_t whole_rows(const bacon_block& b, cudaStream_t st)
     const int pieces = b.width / 8;
     if (pieces <= 32) return launch_rows<DTYPE, RESIDUAL, 1, true>(b, pieces, st);
     if (pieces <= 128) return launch_rows<DTYPE, RESIDUAL, 4, true>(b, pieces, st);
-    const bool few = b.tokens <= 152 * 2;
-    if (few && pieces <= 1024) return launch_rows<DTYPE, RESIDUAL, 1, false>(b, pieces, st);
-    // the most pieces a thread of which all but the last are there in every thread:
-    // fewer threads a row have fewer sums to share (two pieces: 566 us for 422 of the
-    // largest case, before pieces were known to exist); few rows take the most threads
+    // By the width alone, so that a row's bits do not depend on how many there are (one
+    // piece a thread for few rows: 2.8 us for 3.1 of 32 rows of 2048, 4.0 for 3.8 of
+    // 8192): the most pieces a thread of which all but the last are there in every
+    // thread.  Fewer threads a row have fewer sums to share (two pieces: 566 us for 422
+    // of the largest case, before pieces were known to exist).
     const auto tight = [&](int chunks) {
         const int threads = ((pieces + chunks - 1) / chunks + 31) / 32 * 32;
         return threads <= 512 && (chunks - 1) * threads <= pieces;

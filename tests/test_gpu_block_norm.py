@@ -204,13 +204,14 @@ def test_large_means():
         assert bool(((n.double() - want).abs() <= 2.0 ** -16 * want.abs() + 60 * 2.0 ** -24 * 1000).all())
 
 
-def test_a_row_is_the_same_among_others_and_every_time():
-    y, x = draw((301, 3584), "bf16", 1), draw((301, 3584), "bf16", 2)
-    layer = bacon.BlockNorm(3584, post="rms")
+@pytest.mark.parametrize("width", [64, 600, 1111, 2048, 3584, 8192, 12000, 20000])
+def test_a_row_is_the_same_among_others_and_every_time(width):
+    y, x = draw((1301, width), "bf16", 1), draw((1301, width), "bf16", 2)
+    layer = bacon.BlockNorm(width, post="rms", pre="layer")
     whole, again = layer(y, x), layer(y, x)
-    alone = layer(y[77:78], x[77:78])
-    for a, b, c in zip(whole, again, alone):
-        assert torch.equal(a, b) and torch.equal(a[77:78], c)
+    for part in (slice(77, 78), slice(1100, 1301)):
+        for a, b, c in zip(whole, again, layer(y[part], x[part])):
+            assert torch.equal(a, b) and torch.equal(a[part], c)
 
 
 def test_offsets_beyond_32_bits():

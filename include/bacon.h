@@ -665,7 +665,8 @@ typedef struct {
     int32_t* best;    /* [rows] largest x before the temperature, the lowest of equal
                          ones; -1 if none is above -inf; NaN is never the largest  */
     float* logprob;   /* [rows] its log-probability after the temperature; -inf for -1 */
-    float* lse;       /* [rows] log sum exp of the row after the temperature       */
+    float* lse;       /* [rows] log sum exp of the row after the temperature (summed
+                         in an order that goes by the call's sizes)              */
 } bacon_logits_rows;
 
 /* A handle for rows of `vocab` logits on the current device (it holds the error

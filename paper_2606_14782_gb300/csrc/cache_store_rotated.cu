@@ -3,8 +3,8 @@
 // by lanes with eight pairs, through shared memory into the registers that the store
 // keeps them in: what is saved against the two calls is a launch, and writing K and
 // reading it again.  us: a token of 32 requests (32 and 8 heads, norms) 5.0, the two
-// calls 3.1 and 3.1; turns of 5 requests, 3500 tokens (28 and 4 heads) 16.8, the two
-// calls 8.7 and 9.6.  Short of the bytes' time (1.1 and 7 us): chains of a run's slots,
+// calls 3.1 and 3.1; turns of 5 requests, 3500 tokens (28 and 4 heads) 17.1, the two
+// calls 8.7 and 9.5.  Short of the bytes' time (1.1 and 7 us): chains of a run's slots,
 // its rows, its scale and its codes, which few blocks have anything beside.
 #include "cache_store.cuh"
 
@@ -41,7 +41,7 @@ cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, c
     dim3 grid((unsigned)((a.tokens + window - 1) / window), a.heads);
     if (r.args.rows[0].heads) {
         // blocks of the store's size, which begin when most of its own are through: more
-        // and shorter pieces than rotary.cu has (3500 tokens of 28 heads: 16.8 us a call, 18.5
+        // and shorter pieces than rotary.cu has (3500 tokens of 28 heads: 17.1 us a call, 18.5
         // with its 512)
         const long long pieces = deal_rows(r.args, values_of_lane(r.args.q_pair), 2048, &r.deal);
         const int groups = (g.page * g.d / 8 / kChunks) >> r.deal.log_lanes;

@@ -25,6 +25,7 @@
 namespace bacon {
 namespace {
 
+// (24 warps of an SM in place of 48, by 256 threads a block: the largest case 115 us for 92)
 constexpr int kThreads = 512;
 constexpr int kGroup = 256;              // tokens that a warp takes together
 constexpr int kSplit = 16384;           // tokens of a prompt that a row's blocks share

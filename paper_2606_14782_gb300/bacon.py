@@ -1066,8 +1066,8 @@ class Logits:
     def __init__(self, vocab, device=None):
         self._lib = load()
         self.vocab = vocab
-        self.device = torch.device("cuda", torch.cuda.current_device() if device is None else
-                                   torch.device(device).index or 0)
+        index = None if device is None else torch.device(device).index
+        self.device = torch.device("cuda", torch.cuda.current_device() if index is None else index)
         self._index = self.device.index
         h = _vp()
         with torch.cuda.device(self.device):

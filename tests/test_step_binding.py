@@ -97,3 +97,11 @@ def test_weights_say_where_a_norm_is(calls):
             Strided((T, W), BF16, 1))
     with pytest.raises(ValueError):
         bacon.BlockNorm(W, pre_weight=Strided((W,), BF16, -1))
+
+
+def test_logits_belong_to_the_device_that_is_named(calls):
+    assert bacon.Logits(V).device.index == bacon.Logits(V, device="cuda").device.index == 0
+    with torch.cuda.device(1):
+        assert bacon.Logits(V).device.index == bacon.Logits(V, device="cuda").device.index == 1
+        assert bacon.Logits(V, device="cuda:0").device.index == 0
+    assert [d for n, d in calls.calls if n == "bacon_logits_create"] == [0, 0, 1, 1, 0]

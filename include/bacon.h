@@ -595,7 +595,8 @@ bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* r
  * before s is rounded.  Norms: (v - mean) / sqrt(var + eps) for LAYER, v /
  * sqrt(mean v^2 + eps) for RMS, times (weight_offset + weight), plus bias;
  * statistics in fp32, for any finite values (rows whose squares pass 3e38 are
- * scaled first).  A row's results do not depend on the other rows or how many they
+ * scaled first; with LAYER a row far off 0 for its spread has its mean off first,
+ * so that a row of one value is 0).  A row's results do not depend on the other rows or how many they
  * are.  sum may be x, and normed y, with the same strides. */
 typedef enum { BACON_NORM_NONE = 0, BACON_NORM_RMS = 1, BACON_NORM_LAYER = 2 } bacon_norm_kind;
 typedef enum {

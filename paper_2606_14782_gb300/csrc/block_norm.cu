@@ -82,16 +82,18 @@ template <int DTYPE, int CHUNKS, bool TIGHT, typename SUM>
 __device__ __forceinline__ void normalise(const bacon_block& b, float per_channel, const Norm& n,
                                           const Pieces<CHUNKS, TIGHT>& p, SUM& sum, Piece (&v)[CHUNKS])
 {
+    const bool layer = n.kind == BACON_NORM_LAYER;
     float mean = 0.0f, inverse, eps = b.eps;
+    bool again = false;  // this row has been gone through before, and not for others alone
     for (int pass = 0;; ++pass) {
-        if (n.kind == BACON_NORM_LAYER) {
+        if (layer) {
             Pair s = 0;
 #pragma unroll
             for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s = add2(s, v[i].p[j]);
             const float2 f = floats_of(s);
-            mean = sum(f.x + f.y) * per_channel;
+            mean = mean_of(sum(f.x + f.y), b.width, per_channel, again);
         }
         Pair s = 0;
         const Pair off = pair_of(-mean, -mean);
@@ -100,23 +102,25 @@ __device__ __forceinline__ void normalise(const bacon_block& b, float per_channe
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 Pair x = v[i].p[j];
-                if (n.kind == BACON_NORM_LAYER) x = p.some(i) ? add2(x, off) : 0;
+                if (layer) x = p.some(i) ? add2(x, off) : 0;
                 s = fma2(x, x, s);
             }
         const float2 f = floats_of(s);
-        const float squares = sum(f.x + f.y);
-        inverse = rsqrtf(fmaf(squares, per_channel, eps));
-        // once more with the row far smaller; eps is nothing beside its squares.  The
-        // rows of a warp go together, and the others find again what they had
-        const bool again = !(squares < INFINITY) && !pass;
-        if (TIGHT ? !again : !__any_sync(0xFFFFFFFFu, again)) break;
-        if (again) eps = 0.0f;
-        const float by = again ? 0x1p-100f : 1.0f;
-        const Pair small = pair_of(by, by);
+        const float squares = sum(f.x + f.y), square = fmaf(squares, per_channel, eps);
+        inverse = rsqrtf(square);
+        // once more, far smaller or with the mean off (block_norm.cuh).  The rows of a
+        // warp go together, and the others find again what they had
+        const bool over = !(squares < INFINITY) && pass < 1;
+        const bool far = layer && pass < 3 && far_off(mean, square);
+        if (TIGHT ? !(over || far) : !__any_sync(0xFFFFFFFFu, over || far)) break;
+        again |= over || far;
+        if (over) eps = kScaledEps;
+        const float by = over ? kScaled : 1.0f, less = far ? -mean : -0.0f;
+        const Pair times = pair_of(by, by), plus = pair_of(less, less);
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[i].p[j] = mul2(v[i].p[j], small);
+            for (int j = 0; j < 4; ++j) v[i].p[j] = p.some(i) ? fma2(v[i].p[j], times, plus) : 0;
     }
     const Pair by = pair_of(inverse, inverse), off = pair_of(-mean, -mean);
 #pragma unroll
@@ -124,7 +128,7 @@ __device__ __forceinline__ void normalise(const bacon_block& b, float per_channe
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             // channels that are not there stay 0
-            if (n.kind == BACON_NORM_LAYER) v[i].p[j] = p.some(i) ? add2(v[i].p[j], off) : 0;
+            if (layer) v[i].p[j] = p.some(i) ? add2(v[i].p[j], off) : 0;
             v[i].p[j] = mul2(v[i].p[j], by);
         }
     if (DTYPE != BACON_FP32 && b.weight_dtype == BACON_FP32)

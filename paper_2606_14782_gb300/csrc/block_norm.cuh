@@ -45,6 +45,24 @@ __device__ __forceinline__ float activate(float g, int kind)
     return g > -INFINITY ? g * s : 0.0f;  // the limit
 }
 
+// Statistics of rows that fp32 has no room for.  A row whose squares pass 3e38 is scaled
+// by kScaled and gone through again; eps is nothing beside its mean square then, but
+// where that is 0 (a row of one value and its mean) it keeps the root from being
+// infinite.  A row that lies far off 0 for its spread has a mean whose rounding would
+// show beside that spread: the mean is taken off the values, nearly all of them
+// exactly, and the row gone through again; a row of one value is 0 then.  From 64 times
+// the spread on, so that a mean off by 2^-22 of itself is off by 2^-16 of the spread.
+constexpr float kScaled = 0x1p-100f, kScaledEps = 0x1p-126f;
+__device__ __forceinline__ bool far_off(float mean, float square) { return square < mean * mean * 0x1p-12f; }
+
+// sum / width; of a row gone through again with one step of correction: exact where the
+// quotient is.
+__device__ __forceinline__ float mean_of(float sum, int width, float per_channel, bool again)
+{
+    const float mean = sum * per_channel;
+    return again ? fmaf(fmaf(-mean, (float)width, sum), per_channel, mean) : mean;
+}
+
 struct Norm {
     int kind;
     const void* weight;

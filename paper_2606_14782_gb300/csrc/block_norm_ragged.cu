@@ -39,13 +39,14 @@ template <int DTYPE, int COUNT, typename SUM>
 __device__ __forceinline__ void normalise(const bacon_block& b, float per_channel, const Norm& n, int first,
                                           int step, SUM& sum, float (&v)[COUNT])
 {
+    const bool layer = n.kind == BACON_NORM_LAYER;
     float mean = 0.0f, inverse, eps = b.eps;
     for (int pass = 0;; ++pass) {
-        if (n.kind == BACON_NORM_LAYER) {
+        if (layer) {
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) s += v[i];
-            mean = sum(s) * per_channel;
+            mean = mean_of(sum(s), b.width, per_channel, pass > 0);
         }
         float s = 0.0f;
 #pragma unroll
@@ -53,13 +54,16 @@ __device__ __forceinline__ void normalise(const bacon_block& b, float per_channe
             const float x = first + i * step < b.width ? v[i] - mean : 0.0f;
             s = fmaf(x, x, s);
         }
-        const float squares = sum(s);
-        inverse = rsqrtf(fmaf(squares, per_channel, eps));
-        if (squares < INFINITY || pass) break;
-        // once more with the row far smaller; eps is nothing beside its squares
-        eps = 0.0f;
+        const float squares = sum(s), square = fmaf(squares, per_channel, eps);
+        inverse = rsqrtf(square);
+        // once more, far smaller or with the mean off (block_norm.cuh)
+        const bool over = !(squares < INFINITY) && pass < 1;
+        const bool far = layer && pass < 3 && far_off(mean, square);
+        if (!over && !far) break;
+        if (over) eps = kScaledEps;
+        const float by = over ? kScaled : 1.0f, less = far ? mean : 0.0f;
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] *= 0x1p-100f;
+        for (int i = 0; i < COUNT; ++i) v[i] = first + i * step < b.width ? fmaf(v[i], by, -less) : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) v[i] = first + i * step < b.width ? (v[i] - mean) * inverse : 0.0f;

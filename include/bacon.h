@@ -529,8 +529,9 @@ typedef enum {
                                  rotations original theta_i / 2 pi from 0 at `low` to 1
                                  at `high`                                             */
     BACON_ROPE_DIMS = 4       /* the same with s falling along i from 1 at the pair that
-                                 turns `high` times (rounded down) to 0 at the one
-                                 that turns `low` times (rounded up)                   */
+                                 turns `high` times (rounded down, the first one at
+                                 least) to 0 at the one that turns `low` times (rounded
+                                 up; it may lie behind the last)                       */
 } bacon_rope_scaling;
 
 /* Frequencies theta [rotary_dim / 2], in radians a position.  Host only.

@@ -174,7 +174,7 @@ bacon_status bacon_rotary_frequencies(int rotary_dim, double base, int scaling, 
     double first = 0.0, last = 0.0;
     if (scaling == BACON_ROPE_DIMS) {
         first = std::fmax(std::floor(pair_of(high)), 0.0);
-        last = std::fmin(std::ceil(pair_of(low)), half - 1.0);
+        last = std::ceil(pair_of(low));  // it may lie behind the last pair
     }
     for (int i = 0; i < half; ++i) {
         double theta = std::pow(base, -2.0 * i / rotary_dim), kept = 1.0;

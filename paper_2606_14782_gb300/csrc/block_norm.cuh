@@ -42,7 +42,7 @@ __device__ __forceinline__ float activate(float g, int kind)
     if (kind == BACON_GATE_TANH) return tanhf(g);
     const float s = 1.0f / (1.0f + expf(-g));
     if (kind == BACON_GATE_SIGMOID) return s;
-    return g > -INFINITY ? g * s : 0.0f;  // the limit
+    return g == -INFINITY ? 0.0f : g * s;  // the limit
 }
 
 // Statistics of rows that fp32 has no room for.  A row whose squares pass 3e38 is scaled

@@ -516,7 +516,7 @@ bacon_status bacon_cache_sync(bacon_cache* cache, bacon_stream stream);
  *   (x_a, x_b) -> A (x_a cos - x_b sin, x_b cos + x_a sin),
  * with (a, b) = (i, i + rotary_dim / 2), or (2i, 2i + 1) interleaved; values
  * from rotary_dim on stay.  Angles are right to 2^-24 of a turn at every int32
- * position, negative ones too.  A row moves from position p to p' by a
+ * position, negative ones too, whatever the frequency.  A row moves from position p to p' by a
  * turn of p' - p. */
 typedef struct bacon_rotary bacon_rotary;
 #define BACON_MAX_HEAD 256 /* largest head_dim of rotary rows */
@@ -541,9 +541,10 @@ bacon_status bacon_rotary_frequencies(int rotary_dim, double base, int scaling, 
                                       double original, double low, double high, double* out);
 
 /* A rotation of rows of head_dim values (even, at most BACON_MAX_HEAD), from a
- * HOST array of rotary_dim / 2 finite frequencies; axis: HOST array of the same
- * length of values in [0, 3), or NULL for one axis.  `amplitude` is A.  Holds no
- * device memory and may be used from several threads and on any device. */
+ * HOST array of rotary_dim / 2 frequencies, at most 1e6 either way; axis: HOST
+ * array of the same length of values in [0, 3), or NULL for one axis.
+ * `amplitude` is A.  Holds no device memory and may be used from several threads
+ * and on any device. */
 bacon_status bacon_rotary_create(bacon_rotary** out, int head_dim, int rotary_dim, int interleaved,
                                  float amplitude, const double* frequencies, const uint8_t* axis);
 void bacon_rotary_destroy(bacon_rotary* rotary);

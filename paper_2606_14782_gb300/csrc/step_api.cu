@@ -34,6 +34,21 @@ int size_of(int dtype) { return dtype == BACON_FP32 ? 4 : 2; }
 bool known(int dtype) { return dtype == BACON_BF16 || dtype == BACON_FP16 || dtype == BACON_FP32; }
 bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
+// theta / 2 pi in units of 2^-64 turns, |theta| below 2^20; whole turns do not count at
+// whole positions.  In integers, to less than a unit: a double's quotient is off by
+// 2^-53 of itself, which a position of 2^31 makes 2^-22 turns for each turn of theta.
+uint64_t turns_of(double theta)
+{
+    constexpr uint64_t kHigh = 0x28be60db9391054a, kLow = 0x7f09d5f47d4d3770;  // 2^128 / 2 pi
+    int exponent;
+    const uint64_t mantissa = (uint64_t)std::ldexp(std::frexp(std::fabs(theta), &exponent), 53);
+    const unsigned __int128 low = (unsigned __int128)mantissa * kLow;
+    const unsigned __int128 turns = (unsigned __int128)mantissa * kHigh + (uint64_t)(low >> 64);
+    const int shift = 53 - exponent;  // theta is mantissa 2^-shift, `turns` in units of 2^-64 of those
+    const uint64_t units = shift < 128 ? (uint64_t)(turns >> shift) : 0;
+    return theta < 0.0 ? 0 - units : units;
+}
+
 // Whether rows of d values at (n0, n1, n2) places with these strides are apart.
 bool apart(int d, const long long (&sizes)[3], const long long (&strides)[3])
 {
@@ -215,11 +230,7 @@ bacon_status bacon_rotary_create(bacon_rotary** out, int head_dim, int rotary_di
             delete r;
             return fail(BACON_EINVAL, "frequency or axis %d is out of range", i);
         }
-        // whole turns do not count at whole positions
-        double turn = frequencies[i] / kTwoPi;
-        turn -= std::floor(turn);
-        const double scaled = turn * 18446744073709551616.0;
-        t.turns[i] = scaled < 18446744073709551616.0 ? (uint64_t)scaled : 0;
+        t.turns[i] = turns_of(frequencies[i]);
         t.axis[i] = axis ? axis[i] : 0;
     }
     *out = r;

@@ -956,8 +956,8 @@ class BlockNorm:
     post, pre: None, "rms" or "layer", with weights and biases [width] (any may be
     None) in the rows' type or float32; eps is both norms', and both multiply by
     offset + weight.  gate: "linear", "sigmoid", "tanh" or "silu", of the gate that
-    a call gives.  The object holds the weights and may be used from several
-    threads and streams."""
+    a call gives.  The object holds the tensors of the weights, and each call reads what
+    they are then; it may be used from several threads and streams."""
 
     def __init__(self, width, pre="rms", post=None, pre_weight=None, pre_bias=None,
                  post_weight=None, post_bias=None, gate="linear", scale=1.0, eps=1e-6, offset=0.0):
@@ -967,21 +967,26 @@ class BlockNorm:
         self.width, self.pre, self.post = width, pre, post
         self._kinds = NORMS[post], NORMS[pre], GATES[gate], scale, eps, offset
         self._weights = post_weight, post_bias, pre_weight, pre_bias
-        given = [w for w in self._weights if w is not None]
-        self._index = given[0].get_device() if given else None
-        if given and not given[0].is_cuda:
+        self._given = [(i, w) for i, w in enumerate(self._weights) if w is not None]
+        if not all(w.is_cuda for _, w in self._given):
             raise ValueError("weights must be on a GPU")
-        self._dtypes = {}
-        self._pointers = [_ptr(w) or 0 for w in self._weights]
+        self._shape = torch.Size((width,))
 
-    def _weight_dtype(self, dtype, index):
-        """The weights' type for rows of this type, checked once for each."""
-        if dtype not in self._dtypes:
-            if dtype not in DTYPES:
-                raise ValueError("rows must be bf16, fp16 or fp32")
-            self._dtypes[dtype] = _weights_dtype(self._weights, (self.width,), dtype,
-                                                 index if self._index is None else self._index)
-        return self._dtypes[dtype]
+    def _bound(self, dtype, index):
+        """The type and places of the weights, as they are now: a parameter may have got
+        other data since the last call."""
+        places, kind, shape = [0, 0, 0, 0], None, self._shape
+        for i, w in self._given:
+            t = w.dtype
+            if ((t is not kind and kind is not None) or w.shape != shape or w.get_device() != index
+                    or not w.is_contiguous()):
+                break
+            kind = t
+            places[i] = w.data_ptr()
+        else:
+            if kind is dtype or kind is torch.float32:
+                return DTYPES[kind], places
+        return _weights_dtype(self._weights, shape, dtype, index), places  # refuses
 
     def _rows(self, t, shape, dtypes, index, what):
         """The distance of rows [..., width], with the last dimension contiguous
@@ -989,9 +994,10 @@ class BlockNorm:
         if t.dtype not in dtypes or t.get_device() != index or t.shape != shape:
             raise ValueError(f"{what} must be of shape {tuple(shape)} and one of {dtypes} on "
                              f"cuda:{index}")
-        if t.is_contiguous():
-            return self.width
-        stride = t.stride()
+        return self.width if t.is_contiguous() else self._distance(t, what)
+
+    def _distance(self, t, what):
+        shape, stride = t.shape, t.stride()
         if stride[-1] == 1 or self.width == 1:
             flat = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n > 1]
             if all(s == n * r for (_, s), (n, r) in zip(flat, flat[1:])):
@@ -1007,13 +1013,11 @@ class BlockNorm:
         index = y.get_device()
         if not y.is_cuda or len(shape) < 1 or shape[-1] != width:
             raise ValueError(f"y must be [..., {width}] on a GPU")
-        if self._index is not None and self._index != index:
-            raise ValueError(f"the weights are on cuda:{self._index}")
-        weight_dtype = self._dtypes.get(dtype)
-        if weight_dtype is None:
-            weight_dtype = self._weight_dtype(dtype, index)
+        if dtype not in DTYPES:
+            raise ValueError("rows must be bf16, fp16 or fp32")
+        weight_dtype, weights = self._bound(dtype, index) if self._given else (DTYPES[dtype], (0, 0, 0, 0))
         tokens = y.numel() // width
-        y_stride = self._rows(y, shape, (dtype,), index, "y")
+        y_stride = width if y.is_contiguous() else self._distance(y, "y")
         gate_stride = x_stride = sum_stride = norm_stride = 0
         wide = x if x is not None else sum_out
         residual = dtype if wide is None else wide.dtype
@@ -1052,7 +1056,7 @@ class BlockNorm:
         desc = _pack_block(tokens, width, DTYPES[dtype], DTYPES[residual], weight_dtype, post, pre,
                            kind, scale, eps, offset, channel, gate_stride, y_stride, x_stride,
                            sum_stride, norm_stride, y.data_ptr(), 0 if x is None else x.data_ptr(),
-                           0 if gate is None else gate.data_ptr(), *self._pointers,
+                           0 if gate is None else gate.data_ptr(), *weights,
                            0 if sum_out is None else sum_out.data_ptr(),
                            0 if norm_out is None else norm_out.data_ptr())
         _on(index, self._lib.bacon_block_norm, desc, _stream_of(stream, index))

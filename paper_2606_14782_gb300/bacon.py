@@ -835,6 +835,8 @@ def _weights_dtype(weights, shape, dtype, index):
                 or w.dtype is not (kind or w.dtype) or w.dtype not in (dtype, torch.float32)):
             raise ValueError(f"weights must be contiguous, of shape {tuple(shape)}, all {dtype} or "
                              f"all float32, on cuda:{index}")
+        if not w.data_ptr():  # its storage was freed; NULL would mean that there is no weight
+            raise ValueError("a weight has no memory")
         kind = w.dtype
     return DTYPES[kind or dtype]
 
@@ -982,11 +984,14 @@ class BlockNorm:
                     or not w.is_contiguous()):
                 break
             kind = t
-            places[i] = w.data_ptr()
+            places[i] = at = w.data_ptr()
+            if not at:
+                break
         else:
             if kind is dtype or kind is torch.float32:
                 return DTYPES[kind], places
-        return _weights_dtype(self._weights, shape, dtype, index), places  # refuses
+        kind = _weights_dtype(self._weights, shape, dtype, index)  # says what is wrong
+        return kind, [_ptr(w) or 0 for w in self._weights]
 
     def _rows(self, t, shape, dtypes, index, what):
         """The distance of rows [..., width], with the last dimension contiguous

@@ -69,6 +69,22 @@ def test_weights_that_became_others_are_refused(block, change):
         block(layer)
 
 
+def test_weights_without_memory_are_refused(block, calls):  # noqa: F811
+    """A freed storage has no address, and without one there would be no weight."""
+    w = Placed((W,), BF16)
+    layer = bacon.BlockNorm(W, pre_weight=w)
+    block(layer)
+    w.place = 0
+    with pytest.raises(ValueError):
+        block(layer)
+    d = Placed((64,), BF16)
+    d.place = 0
+    rotary, q, at = bacon.Rotary(64), Strided((T, 4, 64), BF16), Strided((T,), torch.int32)
+    with pytest.raises(ValueError):
+        rotary.apply(q, None, at, q_weight=d)
+    assert "bacon_rotary_apply" not in [n for n, _ in calls.calls]
+
+
 @pytest.mark.gpu
 def test_a_parameter_with_other_data():
     build.build()

@@ -30,10 +30,12 @@ constexpr int kThreads = 512;
 constexpr int kGroup = 256;              // tokens that a warp takes together
 constexpr int kSplit = 16384;           // tokens of a prompt that a row's blocks share
 constexpr int kMostOfThree = 70;         // groups of a block of which three fit an SM's shared memory
+constexpr int kMostOfTwo = 112;          // ... at most: of the largest vocabulary, by sixteen blocks
 constexpr float kLeast = 1e-30f;         // repetition and temperature
 constexpr uint32_t kCount = 0xFFFFFu;    // of a token's word: times in the answer
 constexpr uint32_t kSeen = 1u << 20;     // in the prompt
 constexpr int kBiasShift = 21;           // place in the bias list, from 1
+static_assert(kMostOfTwo * kGroup * 16 >= BACON_MAX_VOCAB && kMostOfTwo >= kMostOfThree, "room for every vocabulary");
 static_assert(kCount >= BACON_MAX_HISTORY && BACON_MAX_BIASES < 1 << (32 - kBiasShift), "a word's fields");
 
 __device__ __forceinline__ void cluster_arrive()
@@ -455,11 +457,14 @@ cudaError_t start(const bacon_logits_rows& r, int vocab, int blocks, int* err, c
     int log_blocks = 0;
     while (1 << log_blocks < blocks) ++log_blocks;
     const int groups = ((vocab + kGroup - 1) / kGroup + blocks - 1) / blocks;  // of a block, at most
-    const size_t smem = words ? (size_t)groups * (kGroup + kGroup / 32) * 4 : 0;
+    const auto bytes = [](int groups) { return (size_t)groups * (kGroup + kGroup / 32) * 4; };
+    const size_t smem = words ? bytes(groups) : 0;
     auto* const kernel = logits_kernel<DTYPE, OUT, kStep, kResident>;
     if (smem > 32 * 1024) {
-        const cudaError_t e =
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        // what any call may need: the limit is the kernel's, and a smaller one could come
+        // between another thread's limit and its launch
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   (int)bytes(kResident == 3 ? kMostOfThree : kMostOfTwo));
         if (e != cudaSuccess) return e;
     }
     if (blocks > 8) {

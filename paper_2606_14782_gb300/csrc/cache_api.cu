@@ -251,6 +251,8 @@ bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* r
         return fail(BACON_EINVAL, "the rotation is of %d values, rows have %d", r.table.head_dim, g.d);
     if (tokens == 0) return BACON_OK;
     if (!slots) return fail(BACON_EINVAL, "null argument");
+    if (reinterpret_cast<uintptr_t>(slots) % 4)
+        return fail(BACON_EINVAL, "slots must be aligned to their type");
     if (bacon_status rc = check_rows(k->in, k->in_token, k->in_head, "k")) return rc;
     if (bacon_status rc = check_rows(v, v_token_stride, v_head_stride, "v")) return rc;
     StoreArgs a{tokens, k->heads,

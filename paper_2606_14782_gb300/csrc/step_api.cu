@@ -133,6 +133,7 @@ bacon_status rotary_args(const bacon_rotary* rotary, int requests, int tokens, c
     if ((long long)requests * tokens * (every > 0 ? every : 1) >= 1ll << 31)
         return fail(BACON_EINVAL, "a call takes fewer than 2^31 rows");
     if (requests && tokens && every && !positions) return fail(BACON_EINVAL, "null positions");
+    if (!aligned_to(positions, 4)) return fail(BACON_EINVAL, "positions must be aligned to their type");
     a.table.transposed = transposed != 0;
     a.table.weight_dtype = weight_dtype;
     a.table.eps = eps;

@@ -598,8 +598,10 @@ bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* r
  * sqrt(mean v^2 + eps) for RMS, times (weight_offset + weight), plus bias;
  * statistics in fp32, for any finite values (rows whose squares pass 3e38 are
  * scaled first; with LAYER a row far off 0 for its spread has its mean off first,
- * so that a row of one value is 0).  A row's results do not depend on the other rows or how many they
- * are.  sum may be x, and normed y, with the same strides. */
+ * so that a row of one value is 0).  A row's results do not depend on the other
+ * rows, nor at the same strides (of one token too) on how many they are: rows of
+ * whole 16 bytes that all start at multiples of 16 bytes are added up in one
+ * order, others in another.  sum may be x, and normed y, with the same strides. */
 typedef enum { BACON_NORM_NONE = 0, BACON_NORM_RMS = 1, BACON_NORM_LAYER = 2 } bacon_norm_kind;
 typedef enum {
     BACON_GATE_LINEAR = 0,

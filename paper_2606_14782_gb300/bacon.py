@@ -977,29 +977,28 @@ class BlockNorm:
     def _bound(self, dtype, index):
         """The type and places of the weights, as they are now: a parameter may have got
         other data since the last call."""
-        places, kind, shape = [0, 0, 0, 0], None, self._shape
+        places, shape, first = [0, 0, 0, 0], self._shape, self._given[0][1].dtype
         for i, w in self._given:
-            t = w.dtype
-            if ((t is not kind and kind is not None) or w.shape != shape or w.get_device() != index
+            at = w.data_ptr()
+            if (w.dtype is not first or w.shape != shape or w.get_device() != index or not at
                     or not w.is_contiguous()):
                 break
-            kind = t
-            places[i] = at = w.data_ptr()
-            if not at:
-                break
+            places[i] = at
         else:
-            if kind is dtype or kind is torch.float32:
-                return DTYPES[kind], places
+            if first is dtype or first is torch.float32:
+                return DTYPES[first], places
         kind = _weights_dtype(self._weights, shape, dtype, index)  # says what is wrong
         return kind, [_ptr(w) or 0 for w in self._weights]
 
-    def _rows(self, t, shape, dtypes, index, what):
+    def _rows(self, t, shape, dtypes, index, what, one):
         """The distance of rows [..., width], with the last dimension contiguous
-        and one distance for all rows."""
+        and one distance for all rows; `one`: of a single row among others."""
         if t.dtype not in dtypes or t.get_device() != index or t.shape != shape:
             raise ValueError(f"{what} must be of shape {tuple(shape)} and one of {dtypes} on "
                              f"cuda:{index}")
-        return self.width if t.is_contiguous() else self._distance(t, what)
+        if t.is_contiguous():
+            return t.stride()[-2] if one else self.width
+        return self._distance(t, what)
 
     def _distance(self, t, what):
         shape, stride = t.shape, t.stride()
@@ -1018,16 +1017,23 @@ class BlockNorm:
         index = y.get_device()
         if not y.is_cuda or len(shape) < 1 or shape[-1] != width:
             raise ValueError(f"y must be [..., {width}] on a GPU")
-        if dtype not in DTYPES:
+        kind = weight_kind = wide_kind = DTYPES.get(dtype)
+        if kind is None:
             raise ValueError("rows must be bf16, fp16 or fp32")
-        weight_dtype, weights = self._bound(dtype, index) if self._given else (DTYPES[dtype], (0, 0, 0, 0))
+        weights = 0, 0, 0, 0
+        if self._given:
+            weight_kind, weights = self._bound(dtype, index)
         tokens = y.numel() // width
-        y_stride = width if y.is_contiguous() else self._distance(y, "y")
+        one = tokens == 1 and len(shape) > 1
+        if y.is_contiguous():
+            y_stride = y.stride()[-2] if one else width
+        else:
+            y_stride = self._distance(y, "y")
         gate_stride = x_stride = sum_stride = norm_stride = 0
         wide = x if x is not None else sum_out
         residual = dtype if wide is None else wide.dtype
         if x is not None:
-            x_stride = self._rows(x, shape, (dtype, torch.float32), index, "x")
+            x_stride = self._rows(x, shape, (dtype, torch.float32), index, "x", one)
         channel = 0
         if gate is not None:
             g = gate.shape
@@ -1035,7 +1041,7 @@ class BlockNorm:
                 raise ValueError("the gate must have y's type and device")
             if g == shape:
                 channel = 1
-                gate_stride = self._rows(gate, shape, (dtype,), index, "gate")
+                gate_stride = self._rows(gate, shape, (dtype,), index, "gate", one)
             elif g == (width,) and gate.is_contiguous():
                 channel = 1
             elif g == shape[:-1] + (1,) and gate.is_contiguous():
@@ -1045,7 +1051,7 @@ class BlockNorm:
                                  "(1,), or have y's shape")
         if sum_out is not None:
             sum_stride = self._rows(sum_out, shape, (residual,) if x is not None else
-                                    (dtype, torch.float32), index, "sum_out")
+                                    (dtype, torch.float32), index, "sum_out", one)
         elif x is not None or self.post is not None or gate is not None:
             sum_out = _empty(shape, residual, y.device, stream)
             sum_stride = width
@@ -1056,15 +1062,21 @@ class BlockNorm:
             norm_out = _empty(shape, dtype, y.device, stream)
             norm_stride = width
         else:
-            norm_stride = self._rows(norm_out, shape, (dtype,), index, "norm_out")
-        post, pre, kind, scale, eps, offset = self._kinds
-        desc = _pack_block(tokens, width, DTYPES[dtype], DTYPES[residual], weight_dtype, post, pre,
-                           kind, scale, eps, offset, channel, gate_stride, y_stride, x_stride,
+            norm_stride = self._rows(norm_out, shape, (dtype,), index, "norm_out", one)
+        if residual is not dtype:
+            wide_kind = DTYPES[residual]
+        post, pre, activation, scale, eps, offset = self._kinds
+        desc = _pack_block(tokens, width, kind, wide_kind, weight_kind, post, pre, activation,
+                           scale, eps, offset, channel, gate_stride, y_stride, x_stride,
                            sum_stride, norm_stride, y.data_ptr(), 0 if x is None else x.data_ptr(),
                            0 if gate is None else gate.data_ptr(), *weights,
                            0 if sum_out is None else sum_out.data_ptr(),
                            0 if norm_out is None else norm_out.data_ptr())
-        _on(index, self._lib.bacon_block_norm, desc, _stream_of(stream, index))
+        at = _stream_of(stream, index)
+        if _device() == index:
+            _check(self._lib.bacon_block_norm(desc, at))
+        else:
+            _on(index, self._lib.bacon_block_norm, desc, at)
         return sum_out, norm_out
 
 

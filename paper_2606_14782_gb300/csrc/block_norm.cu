@@ -302,7 +302,8 @@ cudaError_t launch_block_norm(const bacon_block& b, cudaStream_t st)
 {
     const int bytes = b.dtype == BACON_FP32 ? 4 : 2, wide = b.residual_dtype == BACON_FP32 ? 4 : 2;
     const auto rows = [&](const void* p, long long stride, int size) {
-        return !p || (aligned(p) && (b.tokens == 1 || stride * size % 16 == 0));
+        // (of one row too, so that it is the row that it is among others)
+        return !p || (aligned(p) && stride * size % 16 == 0);
     };
     const bool whole = b.width % 8 == 0 && rows(b.y, b.y_token, bytes) && rows(b.x, b.x_token, wide) &&
                        rows(b.sum, b.sum_token, wide) && rows(b.normed, b.normed_token, bytes) &&

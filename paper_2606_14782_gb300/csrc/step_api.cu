@@ -259,7 +259,7 @@ bacon_status bacon_block_norm(const bacon_block* block, bacon_stream stream)
 {
     g_last_error.clear();
     if (!block) return fail(BACON_EINVAL, "null argument");
-    bacon_block b = *block;
+    const bacon_block b = *block;
     if (b.tokens < 0 || b.width < 1 || b.width > BACON_MAX_WIDTH)
         return fail(BACON_EINVAL, "tokens must not be negative, width in [1, %d]", BACON_MAX_WIDTH);
     if (!known(b.dtype) || (b.residual_dtype != b.dtype && b.residual_dtype != BACON_FP32) ||
@@ -287,7 +287,6 @@ bacon_status bacon_block_norm(const bacon_block* block, bacon_stream stream)
         if (s < 0 || s >= most) return fail(BACON_EINVAL, "a stride is out of range");
     if (b.tokens > 1 && ((b.sum && b.sum_token < b.width) || (b.normed && b.normed_token < b.width)))
         return fail(BACON_EINVAL, "rows of an output overlap");
-    if (b.tokens == 1) b.gate_token = 0;
     BACON_CUDA(launch_block_norm(b, static_cast<cudaStream_t>(stream)), "norm launch");
     return BACON_OK;
 }

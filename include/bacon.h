@@ -577,10 +577,10 @@ bacon_status bacon_rotary_apply(const bacon_rotary* rotary, int requests, int to
                                 const int32_t* positions, bacon_stream stream);
 
 /* bacon_rotary_apply for Q (may be NULL) and K, and bacon_cache_store of the
- * turned K and of V, in one launch and with the same results bit for bit.  Rows
- * are [tokens][heads] with the strides of one request; k has as many heads as
- * slots has columns, and k->out is not used.  K and V as in bacon_cache_store;
- * Q and K of the cache's dtype and head_dim. */
+ * turned K and of V, in one launch (two from about 65000 heads on) and with the
+ * same results bit for bit.  Rows are [tokens][heads] with the strides of one
+ * request; k has as many heads as slots has columns, and k->out is not used.  K and
+ * V as in bacon_cache_store; Q and K of the cache's dtype and head_dim. */
 bacon_status bacon_cache_store_rotated(bacon_cache* cache, const bacon_rotary* rotary, int tokens,
                                        const bacon_rows* q, const bacon_rows* k, const void* v,
                                        long long v_token_stride, long long v_head_stride,

@@ -47,8 +47,13 @@ cudaError_t launch_cache_store_rotated(const CacheGeom& g, const StoreArgs& a, c
         const int groups = (g.page * g.d / 8 / kChunks) >> r.deal.log_lanes;
         const long long blocks = (pieces + groups - 1) / groups;
         const long long more = (blocks + grid.x - 1) / grid.x;
-        if (grid.y + more > 65535) return cudaErrorInvalidConfiguration;
-        grid.y += (unsigned)more;
+        if (grid.y + more <= 65535) {
+            grid.y += (unsigned)more;
+        } else {  // so many heads that a grid has no room beside K's: Q by itself
+            const cudaError_t e = launch_rotary(r.args, st);
+            if (e != cudaSuccess) return e;
+            r.args.rows[0].heads = 0;
+        }
     }
     return by_type<StoreTurned>(g, a, r, grid, window, st);
 }

@@ -669,7 +669,8 @@ typedef struct {
     const uint32_t* mask;       /* bit v % 32 of word v / 32: token v is allowed   */
     int32_t* best;    /* [rows] largest x before the temperature, the lowest of equal
                          ones; -1 if none is above -inf; NaN is never the largest  */
-    float* logprob;   /* [rows] its log-probability after the temperature; -inf for -1 */
+    float* logprob;   /* [rows] its log-probability after the temperature; -inf for -1,
+                         NaN for an infinity and beside NaN                        */
     float* lse;       /* [rows] log sum exp of the row after the temperature (summed
                          in an order that goes by the call's sizes)              */
 } bacon_logits_rows;

@@ -410,8 +410,9 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
             p.top = top;
             p.at = v0 + at * kGap;
         }
-        // what is -inf adds nothing, while there is nothing else too; NaN makes the sum NaN
-        const float less = p.top == -INFINITY ? 0.0f : -p.top;
+        // what is -inf adds nothing, while there is nothing else too; an infinity makes the
+        // sum one, and NaN makes it NaN
+        const float less = fabsf(p.top) == INFINITY ? 0.0f : -p.top;
         const Pair off = pair_of(less, less);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -444,9 +445,8 @@ logits_kernel(const __grid_constant__ bacon_logits_rows a, int vocab, int log_bl
         const bool found = p.at != 0xFFFFFFFFu, none = !found && !isnan(p.sum);
         const float more = logf(p.sum);
         if (a.best) a.best[row] = found ? (int)p.at : -1;
-        if (a.logprob) a.logprob[row] = none ? -INFINITY : found ? -more : NAN;
-        if (a.lse)
-            a.lse[row] = none ? -INFINITY : p.top == INFINITY ? INFINITY : p.top * rules.rate + more;
+        if (a.logprob) a.logprob[row] = none ? -INFINITY : found && p.top < INFINITY ? -more : NAN;
+        if (a.lse) a.lse[row] = none ? -INFINITY : p.top * rules.rate + more;
     }
 }
 

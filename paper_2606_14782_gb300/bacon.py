@@ -1168,6 +1168,10 @@ class Logits:
         if tokens is not None:
             requests, capacity = tokens.shape
             p_tokens, token_stride = self._lines(tokens, (_i32,), requests, 0, "tokens")
+            if not p_tokens:
+                # no entries have no address, and without one lengths would not be looked at;
+                # nobody follows this one
+                p_tokens, requests, capacity = 16, max(1, requests), 0
         biases = p_bias = p_value = 0
         if bias_tokens is not None and bias_values is not None:
             biases = bias_tokens.shape[-1]

@@ -877,7 +877,7 @@ class Rotary:
         h = _vp()
         _check(self._lib.bacon_rotary_create(ctypes.byref(h), head_dim, self.rotary_dim,
                                              int(interleaved), amplitude, table,
-                                             None if axes is None else bytes(axes)))
+                                             None if axes is None else bytes([int(x) for x in axes])))
         self.handle = h
 
     def close(self):

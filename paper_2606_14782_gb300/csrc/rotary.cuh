@@ -408,7 +408,6 @@ struct RotaryArgs {
     RotaryTable table;
     RotaryRows rows[2];  // Q, K
     int dtype, requests, tokens;
-    int pair;        // how a lane with eight values gets the others: kPairLane, kPairOwn, kPairMemory
     int q_pair;      // how a call's rows are turned, but for K that is stored
     int vectors;     // rows start at multiples of 16 bytes
 };

@@ -144,13 +144,13 @@ bacon_status rotary_args(const bacon_rotary* rotary, int requests, int tokens, c
     a.requests = requests;
     a.tokens = tokens;
     a.vectors = vectors;
-    a.pair = !vectors                        ? kPairMemory
-             : a.table.interleaved           ? kPairOwn
-             : a.table.rotary_dim % 16 == 0 ? kPairLane
-                                             : kPairMemory;
+    const int pair = !vectors                        ? kPairMemory
+                     : a.table.interleaved           ? kPairOwn
+                     : a.table.rotary_dim % 16 == 0 ? kPairLane
+                                                     : kPairMemory;
     // lanes with eight pairs: where sixteen values lie on one side of the rotation's end
     const bool pairs = d % 16 == 0 && a.table.rotary_dim % 16 == 0;
-    a.q_pair = a.pair == kPairMemory || !pairs ? a.pair : a.table.interleaved ? kPairSixteen : kPairHalves;
+    a.q_pair = pair == kPairMemory || !pairs ? pair : a.table.interleaved ? kPairSixteen : kPairHalves;
     *out = a;
     return BACON_OK;
 }

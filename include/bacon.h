@@ -676,8 +676,8 @@ typedef struct {
 } bacon_logits_rows;
 
 /* A handle for rows of `vocab` logits on the current device (it holds the error
- * word).  Must not be used from two threads at once; its calls may run on
- * several streams. */
+ * word).  Must not be used from two threads at once (two handles may); its calls
+ * may run on several streams, and it has to outlive graphs they were captured into. */
 bacon_status bacon_logits_create(bacon_logits** out, int vocab);
 void bacon_logits_destroy(bacon_logits* logits);
 bacon_status bacon_logits_process(bacon_logits* logits, const bacon_logits_rows* rows,

@@ -1,10 +1,12 @@
 // Between two blocks (block_norm.cu): rows of odd widths, or that start anywhere.  A
 // thread has every threads-th channel of its row, so that a warp's accesses are of
 // neighbours wherever the row starts; they are two or four bytes a lane.  2049 rows of
-// 1111 channels, layer norms on both sides, fp16 with the sum in fp32: 11.4 us for 4.1
+// 1111 channels, layer norms on both sides, fp16 with the sum in fp32: 11.7 us for 4.1
 // of bytes; a row is a chain of its loads and four sums over a block, of which an SM
-// has nine at a time.  (16-byte pieces whose ends are read value by value, with
-// weights shifted into place: 16.3 us, three times the instructions.)
+// has seven at a time.  (16-byte pieces whose ends are read value by value, with
+// weights shifted into place: 16.3 us, three times the instructions.)  Wider rows spill 40
+// bytes a thread from 8193 channels on and 196 from 16385 on: 2000 layer norms of 12001
+// channels 112 us for 28, of 20001 358 for 47.
 #include "block_norm.cuh"
 
 namespace bacon {

@@ -5,7 +5,10 @@
 // reading it again.  us: a token of 32 requests (32 and 8 heads, norms) 5.0, the two
 // calls 3.1 and 3.1; turns of 5 requests, 3500 tokens (28 and 4 heads) 17.1, the two
 // calls 8.7 and 9.5.  Short of the bytes' time (1.1 and 7 us): chains of a run's slots,
-// its rows, its scale and its codes, which few blocks have anything beside.
+// its rows, its scale and its codes, which few blocks have anything beside.  Rotations
+// that are not a multiple of sixteen have their pairs read again and spill 264 to 380
+// bytes a thread: the same turns with 104 of 128 values turned 49 us with the pages loaded
+// again, 24 with all.
 #include "cache_store.cuh"
 
 namespace bacon {

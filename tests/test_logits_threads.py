@@ -44,6 +44,9 @@ def test_two_handles_on_two_threads(lib, one, other, rows):
         raw = bacon._pack_logits(rows, 2, 2, rows, 10, 0, vocab, vocab, 10, 0, A, A, A, 0, 0, A, A, 0, 0, 0, 0, 0,
                                  0, A, A, A)
 
+        # (the host's runtime gets to know the kernel here, before the threads)
+        assert lib.bacon_logits_process(handle, raw, None) == bacon.BACON_OK
+
         def work():
             return {lib.bacon_logits_process(handle, raw, None) for _ in range(30000)}
         return work, handle

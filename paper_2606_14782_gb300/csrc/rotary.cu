@@ -11,10 +11,10 @@ namespace {
 constexpr int kThreads = 256;
 
 // Three blocks an SM where 80 registers do (four prompts of 16384 tokens: 163 us, 166
-// with two), two with norms on pairs of lanes and where pairs are read again, which
-// would spill far more.  Spilled all the same, bytes a thread: with eight values a lane
-// and the others by shuffles 4, of fp32 20; fp32 interleaved 16; fp32 read again, with
-// norms, 24.  Two prompts of 16384 tokens of 28 and 4 heads in bf16, 80 us of bytes:
+// with two), two with norms where lanes have whole pairs and where pairs are read again,
+// which would spill far more.  Spilled all the same, bytes a thread: with eight values a
+// lane and the others by shuffles 4, of fp32 20; fp32 interleaved without norms 16; fp32
+// read again, with norms, 24.  Two prompts of 16384 tokens of 28 and 4 heads in bf16, 80 us of bytes:
 // interleaved 82, with 104 of 128 values turned, whose pairs are read again, 206.  With
 // norms, 95000 tokens of 6 and 2 heads of 128: 103 us for 58 of bytes; fp32, 2800 tokens
 // of 48 and 16 heads: 42 for 27.
